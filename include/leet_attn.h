@@ -326,6 +326,185 @@ int leet_attn_query_plan(int B, int H, int N, int d, int dtype, int segments, in
 /* The same for rank r and value width dv given separately (shapes as for leet_attn_forward_rd). */
 int leet_attn_query_plan_rd(int B, int H, int N, int r, int dv, int dtype, int segments, int *nseg, int *kernel);
 
+/* ------------------------------------------------------------------------------------------------
+ * Operators beside the attention: what makes its queries and keys (position rotation, norms of each
+ * head), and the element-wise recurrence with a decay of its own for every token and channel.
+ * Of the conventions above these differ: tensors may have strides (in ELEMENTS; the elements of a
+ * head row, or the channels of a token row, are adjacent), pointers need only their element's
+ * alignment (16-byte aligned rows are faster), and a workspace, where one is needed, is always the
+ * caller's, so that calls on several streams and captured graphs share nothing.
+ * N = 0 is legal everywhere here and writes no rows.
+ * ---------------------------------------------------------------------------------------------- */
+
+/* Element (b, h, n, j) of a [B][H][N][d] tensor is at data + b*batch + h*head + n*token + j.  A
+ * [B][N][H][d] projection is such a view, and so is a part of a wider one.  Rows that are written
+ * must not overlap one another (LEET_ERR_INVALID_ARG for strides that do not keep them apart). */
+typedef struct {
+    void *data;
+    long long batch, head, token;
+} leet_attn_heads;
+
+typedef enum {
+    LEET_ROPE_HALF = 0,       /* element i of the rotated part is paired with i + rot/2 */
+    LEET_ROPE_INTERLEAVED = 1 /* elements 2i and 2i + 1 are paired                      */
+} leet_rope_layout;
+
+/*
+ * Position rotation: pair i of the first `rot` elements of a head row at position p is turned by
+ * theta = p freq[i] and multiplied by `scale`,
+ *     y1 = scale (x1 cos theta - x2 sin theta),   y2 = scale (x2 cos theta + x1 sin theta);
+ * the elements from `rot` on are passed on.  Angles are formed and reduced in fp64, so positions
+ * may be as far out as fp64 counts.
+ *   freq       [rot/2] double, DEVICE memory: radians a position
+ *   rot        even, 2 <= rot <= d
+ *   positions  NULL: token n is at pos0 + n; else 64-bit integers, token n of sequence b at
+ *              positions[b*positions_batch + n] (positions_batch 0: the same for every sequence);
+ *              pos0 is added
+ *   scale      finite; 1 but for contexts stretched by bands
+ */
+typedef struct {
+    const double *freq;
+    int rot;
+    int layout; /* a leet_rope_layout */
+    const long long *positions;
+    long long positions_batch, pos0;
+    float scale;
+} leet_attn_rotation;
+
+/* How a table of frequencies is made for contexts longer than the trained one. */
+typedef enum {
+    LEET_ROPE_SCALING_NONE = 0,   /* f_i = base^(-2i/rot)                                          */
+    LEET_ROPE_SCALING_LINEAR = 1, /* f_i / factor: positions squeezed into the trained range       */
+    LEET_ROPE_SCALING_BASE = 2,   /* base factor^(rot/(rot-2)): the slowest pair is stretched by
+                                     factor, the fastest not at all (rot = 2: no scaling)          */
+    LEET_ROPE_SCALING_BANDS = 3,  /* pairs that turn over `fast` times within the trained length
+                                     keep f_i, those under `slow` times get f_i / factor, with a
+                                     ramp over the pair's index between the two (its ends rounded
+                                     outward to whole indices); *scale = 0.1 ln(factor) + 1        */
+    LEET_ROPE_SCALING_TURNS = 4   /* the same two ends with the ramp over the number of turns
+                                     within the trained length; *scale = 1                         */
+} leet_rope_scaling;
+
+/* Fills freq[rot/2] and *scale (HOST memory, in fp64).  base > 1, factor >= 1; `trained` (tokens) > 0
+ * and 0 < slow < fast for BANDS and TURNS, ignored otherwise.  Touches no device. */
+int leet_attn_rope_frequencies(int rot, double base, int scaling, double factor, int trained, double slow,
+                               double fast, double *freq, float *scale);
+
+/*
+ * Position rotation of queries and, in the same launch, of keys.
+ *   q, k          [B][Hq][N][d], [B][Hk][N][d] of `dtype`; k and out_k may be NULL (Hk is then ignored)
+ *   out_q, out_k  of the same shapes and type; each may be its input itself (same data and strides),
+ *                 and must not overlap anything else
+ *   transposed    non-zero: the transposed map (angles negated, same scale), which takes gradients of
+ *                 the outputs to gradients of the inputs
+ * d even, 2 <= d <= 256.  Rounded once, at the store.
+ */
+int leet_attn_rope(const leet_attn_heads *q, const leet_attn_heads *out_q, int Hq,
+                   const leet_attn_heads *k, const leet_attn_heads *out_k, int Hk,
+                   const leet_attn_rotation *rotation, int B, int N, int d, int dtype, int transposed,
+                   void *stream);
+
+/*
+ * Norm of every query and key head, then the rotation, in one pass:
+ *     y = R (w .* x / sqrt(mean(x^2) + eps)).
+ *   q_weight, k_weight  [d] of weight_dtype (`dtype` or LEET_F32), or NULL: ones
+ *   eps                 >= 0, finite.  A row of zeros with eps = 0 gives NaN, as the formula does
+ * The rest as for leet_attn_rope; fp32 inside, rounded once, at the store.
+ */
+int leet_attn_qk_norm_rope(const leet_attn_heads *q, const leet_attn_heads *out_q, int Hq,
+                           const leet_attn_heads *k, const leet_attn_heads *out_k, int Hk,
+                           const void *q_weight, const void *k_weight, int weight_dtype, float eps,
+                           const leet_attn_rotation *rotation, int B, int N, int d, int dtype, void *stream);
+
+/*
+ * Its backward pass, from the same inputs and the gradients of the outputs.  With u = R^T dy,
+ * r = 1/sqrt(mean(x^2) + eps) and n = x r:
+ *     dx = r (w .* u - n mean(w .* u .* n)),      dw = sum of u .* n over tokens and heads.
+ *   dout_q, dout_k        gradients of the outputs
+ *   dq, dk                gradients of the inputs; each may be the gradient it comes from (same data
+ *                         and strides), and must not overlap anything else
+ *   dq_weight, dk_weight  [d] of weight_dtype, or NULL: not wanted
+ *   workspace             leet_attn_qk_norm_rope_workspace_bytes bytes, 256-byte aligned; may be NULL
+ *                         when neither weight's gradient is wanted.  Its contents are scratch
+ * The sums over tokens and heads are taken in fp32 in a fixed order: no atomics, equal from call to call.
+ */
+int leet_attn_qk_norm_rope_backward(const leet_attn_heads *dout_q, const leet_attn_heads *q,
+                                    const leet_attn_heads *dq, int Hq,
+                                    const leet_attn_heads *dout_k, const leet_attn_heads *k,
+                                    const leet_attn_heads *dk, int Hk,
+                                    const void *q_weight, const void *k_weight, void *dq_weight, void *dk_weight,
+                                    int weight_dtype, float eps, const leet_attn_rotation *rotation,
+                                    void *workspace, size_t workspace_bytes,
+                                    int B, int N, int d, int dtype, void *stream);
+size_t leet_attn_qk_norm_rope_workspace_bytes(int B, int Hq, int Hk, int N, int d);
+
+/*
+ * Gated linear recurrence, element-wise in every channel:
+ *     h_t = a_t h_{t-1} + b_t,
+ * with a_t, b_t from the gate z_t and the input x_t by `mode`.  (A decay that is one constant a head
+ * makes it the discounted cumulative sum that leet_attn_forward_fleet takes per rank.)
+ */
+typedef enum {
+    LEET_GATE_DECAY = 0,  /* a = z,           b = x                                         */
+    LEET_GATE_LOG = 1,    /* a = exp(z),      b = x                                         */
+    LEET_GATE_SIGMOID = 2 /* a = sigmoid(z),  b = (1 - a) x: h is a moving average of x     */
+} leet_gate_mode;
+
+/* Element (b, n, c) of a [B][N][C] tensor is at data + b*batch + n*token + c. */
+typedef struct {
+    void *data;
+    long long batch, token;
+} leet_attn_rows;
+
+/*
+ * Over whole sequences.
+ *   x, out     [B][N][C] of `dtype`;  gate  [B][N][C] of gate_dtype (`dtype` or LEET_F32)
+ *   out        h of every token, rounded once, at the store (the recurrence itself runs in fp32);
+ *              must not overlap an input
+ *   state_in   [S][C] float or NULL (zeros): h before each sequence's first token
+ *   state_out  [S][C] float or NULL; receives h after each sequence's last token; may be state_in
+ *   offsets    NULL: every batch entry is one sequence of N tokens, S = B (`sequences` is ignored).
+ *              Else DEVICE memory, sequences + 1 ints, not falling, offsets[0] = 0 and
+ *              offsets[S] <= N: the sequences lie behind one another in the N rows, sequence s in rows
+ *              offsets[s] .. offsets[s+1]-1, with B = 1.  Empty sequences hand their state on.  Rows
+ *              from offsets[S] on are not read for a result and their outputs are left as they were.
+ *              (The values are not diagnosed; other ones give wrong rows but no access out of range.)
+ *   workspace  leet_attn_gated_scan_workspace_bytes bytes, 256-byte aligned (NULL when that is 0); scratch
+ * Decays are meant to be at most 1 in magnitude: tokens are combined in tiles whose products of decays
+ * are formed in fp32, which larger ones may take out of range.  A non-finite value makes the later values
+ * of its channel and sequence non-finite and no others.
+ */
+int leet_attn_gated_scan(const leet_attn_rows *x, const leet_attn_rows *gate, const leet_attn_rows *out,
+                         const float *state_in, float *state_out, const int *offsets, int sequences,
+                         void *workspace, size_t workspace_bytes,
+                         int B, int N, int C, int dtype, int gate_dtype, int mode, void *stream);
+
+/*
+ * Its backward pass.  h is the forward call's output; with dh the gradient of h,
+ *     D_t = dh_t + g_{t+1},   g_t = a_t D_t,   g behind the last token = dstate_out (zero if NULL),
+ *     dx = D (times 1 - a for LEET_GATE_SIGMOID),
+ *     dgate = D h_{t-1} | g h_{t-1} | D (h_{t-1} - x) a (1 - a)      by mode,
+ *     dstate_in = g of the first token.
+ *   x            read by LEET_GATE_SIGMOID only; may be NULL otherwise
+ *   h, dh, dx    [B][N][C] of `dtype`;  dgate  of gate_dtype; the outputs must not overlap an input
+ *   state_in     what the forward call was given (NULL: zeros)
+ *   dstate_out   [S][C] float or NULL;  dstate_in  [S][C] float or NULL; may be dstate_out
+ * The rest as for leet_attn_gated_scan.
+ */
+int leet_attn_gated_scan_backward(const leet_attn_rows *dh, const leet_attn_rows *x, const leet_attn_rows *gate,
+                                  const leet_attn_rows *h, const leet_attn_rows *dx, const leet_attn_rows *dgate,
+                                  const float *state_in, const float *dstate_out, float *dstate_in,
+                                  const int *offsets, int sequences, void *workspace, size_t workspace_bytes,
+                                  int B, int N, int C, int dtype, int gate_dtype, int mode, void *stream);
+size_t leet_attn_gated_scan_workspace_bytes(int B, int N, int C, int backward);
+
+/*
+ * One token of every sequence: state <- a state + b, out = state (rounded).
+ *   x, gate, out  [B][C], row b at data + b*batch (`token` is ignored);  state  [B][C] float, in place
+ */
+int leet_attn_gated_scan_step(const leet_attn_rows *x, const leet_attn_rows *gate, const leet_attn_rows *out,
+                              float *state, int B, int C, int dtype, int gate_dtype, int mode, void *stream);
+
 /* Static, never-NULL description of a leet_status value. */
 const char *leet_attn_strerror(int status);
 

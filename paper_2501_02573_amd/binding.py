@@ -22,6 +22,9 @@ LEET_MASK_DECAY, LEET_MASK_CAUSAL = 0, 1
 LEET_OK, LEET_ERR_INVALID_ARG, LEET_ERR_UNSUPPORTED, LEET_ERR_LAUNCH, LEET_ERR_TOO_LARGE = 0, 1, 2, 3, 4
 LEET_ERR_CAPTURE, LEET_ERR_SCRATCH_LIMIT = 5, 6
 LEET_CHOICE_DEFAULT = -1
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+ROPE_SCALING_NONE, ROPE_SCALING_LINEAR, ROPE_SCALING_BASE, ROPE_SCALING_BANDS, ROPE_SCALING_TURNS = 0, 1, 2, 3, 4
+GATE_DECAY, GATE_LOG, GATE_SIGMOID = 0, 1, 2
 
 EXPORTED_SYMBOLS = (
     "leet_attn_forward",
@@ -52,6 +55,15 @@ EXPORTED_SYMBOLS = (
     "leet_attn_get_decode_store",
     "leet_attn_workspace_bytes",
     "leet_attn_release_workspace",
+    "leet_attn_rope_frequencies",
+    "leet_attn_rope",
+    "leet_attn_qk_norm_rope",
+    "leet_attn_qk_norm_rope_backward",
+    "leet_attn_qk_norm_rope_workspace_bytes",
+    "leet_attn_gated_scan",
+    "leet_attn_gated_scan_backward",
+    "leet_attn_gated_scan_workspace_bytes",
+    "leet_attn_gated_scan_step",
     "leet_attn_strerror",
     "leet_attn_version",
 )
@@ -61,6 +73,24 @@ class LeetAttnError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
         super().__init__(f"{where}: status {status}: {strerror(status)}")
+
+
+class _Heads(ctypes.Structure):
+    """leet_attn_heads"""
+    _fields_ = [("data", ctypes.c_void_p), ("batch", ctypes.c_longlong), ("head", ctypes.c_longlong),
+                ("token", ctypes.c_longlong)]
+
+
+class _Rotation(ctypes.Structure):
+    """leet_attn_rotation"""
+    _fields_ = [("freq", ctypes.c_void_p), ("rot", ctypes.c_int), ("layout", ctypes.c_int),
+                ("positions", ctypes.c_void_p), ("positions_batch", ctypes.c_longlong), ("pos0", ctypes.c_longlong),
+                ("scale", ctypes.c_float)]
+
+
+class _Rows(ctypes.Structure):
+    """leet_attn_rows"""
+    _fields_ = [("data", ctypes.c_void_p), ("batch", ctypes.c_longlong), ("token", ctypes.c_longlong)]
 
 
 def _load() -> ctypes.CDLL:
@@ -127,6 +157,29 @@ def _load() -> ctypes.CDLL:
     lib.leet_attn_set_decode_store.restype = i
     lib.leet_attn_get_decode_store.argtypes = []
     lib.leet_attn_get_decode_store.restype = i
+    heads, rotation, rows = ctypes.POINTER(_Heads), ctypes.POINTER(_Rotation), ctypes.POINTER(_Rows)
+    d = ctypes.c_double
+    lib.leet_attn_rope_frequencies.argtypes = [i, d, i, d, i, d, d, vp, ctypes.POINTER(ctypes.c_float)]
+    lib.leet_attn_rope_frequencies.restype = i
+    lib.leet_attn_rope.argtypes = [heads, heads, i, heads, heads, i, rotation, i, i, i, i, i, vp]
+    lib.leet_attn_rope.restype = i
+    lib.leet_attn_qk_norm_rope.argtypes = [heads, heads, i, heads, heads, i, vp, vp, i, ctypes.c_float, rotation,
+                                           i, i, i, i, vp]
+    lib.leet_attn_qk_norm_rope.restype = i
+    lib.leet_attn_qk_norm_rope_backward.argtypes = [heads, heads, heads, i, heads, heads, heads, i, vp, vp, vp, vp, i,
+                                                    ctypes.c_float, rotation, vp, sz, i, i, i, i, vp]
+    lib.leet_attn_qk_norm_rope_backward.restype = i
+    lib.leet_attn_qk_norm_rope_workspace_bytes.argtypes = [i, i, i, i, i]
+    lib.leet_attn_qk_norm_rope_workspace_bytes.restype = sz
+    lib.leet_attn_gated_scan.argtypes = [rows, rows, rows, vp, vp, vp, i, vp, sz, i, i, i, i, i, i, vp]
+    lib.leet_attn_gated_scan.restype = i
+    lib.leet_attn_gated_scan_backward.argtypes = [rows, rows, rows, rows, rows, rows, vp, vp, vp, vp, i, vp, sz,
+                                                  i, i, i, i, i, i, vp]
+    lib.leet_attn_gated_scan_backward.restype = i
+    lib.leet_attn_gated_scan_workspace_bytes.argtypes = [i, i, i, i]
+    lib.leet_attn_gated_scan_workspace_bytes.restype = sz
+    lib.leet_attn_gated_scan_step.argtypes = [rows, rows, rows, vp, i, i, i, i, i, vp]
+    lib.leet_attn_gated_scan_step.restype = i
     lib.leet_attn_strerror.argtypes = [i]
     lib.leet_attn_strerror.restype = ctypes.c_char_p
     lib.leet_attn_version.argtypes = []
@@ -650,4 +703,324 @@ def leet_attn_decode_step_rd(q, k, v, gamma: Optional[torch.Tensor], state, out:
                    B, H, r, dv, _dtype_code(q), int(mask), int(store))
     if st != LEET_OK:
         raise LeetAttnError(st, "leet_attn_decode_step_v3" if store is not None else "leet_attn_decode_step_rd")
+    return out
+
+
+# ---- operators beside the attention -------------------------------------------------------------------------------
+# Their tensors may have any strides but for the last dimension's, which must be 1, and outputs that the caller does not
+# bring are dense.  A workspace that the caller does not bring comes from torch's allocator, on the current stream: it
+# belongs to this call alone, also while a graph is captured.
+
+def _on(*tensors: Optional[torch.Tensor]) -> torch.device:
+    """The one device of all tensors that are there."""
+    dev = None
+    for t in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError("all tensors must be GPU tensors")
+        if dev is None:
+            dev = t.device
+        elif t.device != dev:
+            raise ValueError("all tensors must be on one device")
+    return dev
+
+
+def _heads_view(t: torch.Tensor, name: str, shape, dtype: torch.dtype) -> _Heads:
+    """``t`` as a leet_attn_heads; ``shape`` [B, H, N, d] and ``dtype`` are what it has to have."""
+    if t.shape != shape:
+        raise ValueError(f"{name} must have the shape {list(shape)}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}")
+    b, h, n, e = t.stride()
+    if e != 1 and t.shape[3] > 1:
+        raise ValueError(f"{name}: the elements of a head row must be adjacent")
+    return _Heads(t.data_ptr(), b, h, n)
+
+
+def _rows_view(t: torch.Tensor, name: str, shape, dtype: torch.dtype) -> _Rows:
+    """``t`` as a leet_attn_rows; ``shape`` [B, N, C] or [B, C] and ``dtype`` are what it has to have."""
+    if t.shape != shape:
+        raise ValueError(f"{name} must have the shape {list(shape)}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}")
+    strides = t.stride()
+    if strides[-1] != 1 and t.shape[-1] > 1:
+        raise ValueError(f"{name}: the channels of a row must be adjacent")
+    return _Rows(t.data_ptr(), strides[0], strides[1] if len(strides) == 3 else 0)
+
+
+def _scratch(nbytes: int, workspace: Optional[torch.Tensor], dev: torch.device):
+    """(pointer, bytes, tensor to keep until the launch) of a call's workspace."""
+    if workspace is None:
+        if not nbytes:
+            return None, 0, None
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    elif workspace.dtype != torch.uint8 or not workspace.is_contiguous():
+        raise TypeError("workspace must be a contiguous uint8 tensor")
+    return workspace.data_ptr(), workspace.numel(), workspace
+
+
+def rope_frequencies(rot: int, base: float = 10000.0, scaling: int = ROPE_SCALING_NONE, factor: float = 1.0,
+                     trained: int = 0, slow: float = 1.0, fast: float = 32.0):
+    """(float64 CPU tensor [rot / 2] of radians a position, scale): what the rotation takes as ``freq`` (on the GPU) and
+    ``scale``.  ``factor``: how many times longer than ``trained`` tokens the contexts are; see leet_rope_scaling."""
+    if rot < 2 or rot % 2:
+        raise ValueError("rot must be even and positive")
+    freq, scale = torch.empty(rot // 2, dtype=torch.float64), ctypes.c_float(1.0)
+    st = lib.leet_attn_rope_frequencies(int(rot), float(base), int(scaling), float(factor), int(trained), float(slow),
+                                        float(fast), freq.data_ptr(), ctypes.byref(scale))
+    if st != LEET_OK:
+        raise LeetAttnError(st, "leet_attn_rope_frequencies")
+    return freq, scale.value
+
+
+def _rotation(freq: torch.Tensor, layout: int, positions: Optional[torch.Tensor], pos0: int, scale: float, B: int,
+              N: int) -> _Rotation:
+    if freq.dtype != torch.float64 or freq.dim() != 1 or not freq.is_contiguous():
+        raise ValueError("freq must be a contiguous float64 tensor [rot / 2]")
+    at, stride = None, 0
+    if positions is not None:
+        if positions.dtype != torch.int64 or positions.shape not in ((N,), (B, N)):
+            raise ValueError("positions must be int64 [N] or [B, N]")
+        if N > 1 and positions.stride(-1) != 1:
+            raise ValueError("positions of a sequence must be adjacent")
+        at, stride = positions.data_ptr(), positions.stride(0) if positions.dim() == 2 else 0
+    return _Rotation(freq.data_ptr(), 2 * freq.shape[0], layout, at, stride, pos0, scale)
+
+
+def _heads_pair(q: torch.Tensor, k: Optional[torch.Tensor]):
+    """B, Hq, Hk, N, d of queries and keys."""
+    if q.dim() != 4 or (k is not None and k.dim() != 4):
+        raise ValueError("q and k must be [B, H, N, d]")
+    B, Hq, N, d = q.shape
+    Hk = 0
+    if k is not None:
+        if k.shape[0] != B or k.shape[2] != N or k.shape[3] != d:
+            raise ValueError("q and k must agree in B, N and d")
+        if k.dtype != q.dtype:
+            raise TypeError("q and k must share one dtype")
+        Hk = k.shape[1]
+    return B, Hq, Hk, N, d
+
+
+def _new_dense(like: torch.Tensor) -> torch.Tensor:
+    return _new_out(like, like.dtype)
+
+
+def leet_attn_rope(q: torch.Tensor, freq: torch.Tensor, k: Optional[torch.Tensor] = None,
+                   positions: Optional[torch.Tensor] = None, pos0: int = 0, layout: int = ROPE_HALF,
+                   scale: float = 1.0, transposed: bool = False, out_q: Optional[torch.Tensor] = None,
+                   out_k: Optional[torch.Tensor] = None):
+    """Position rotation of q [B, Hq, N, d], and of k [B, Hk, N, d] in the same launch.
+
+    The first ``2 * len(freq)`` elements of each row are rotated by the token's position (``positions`` or the token's
+    number, plus ``pos0``).  ``transposed`` takes gradients of the outputs to gradients of the inputs.  Returns out_q,
+    or (out_q, out_k); an output may be its input."""
+    B, Hq, Hk, N, d = _heads_pair(q, k)
+    if out_q is None:
+        out_q = _new_dense(q)
+    if k is None:
+        if out_k is not None:
+            raise ValueError("out_k without k")
+    elif out_k is None:
+        out_k = _new_dense(k)
+    dev = _on(q, k, out_q, out_k, freq, positions)
+    vk = ok = None
+    if k is not None:
+        vk, ok = _heads_view(k, "k", k.shape, q.dtype), _heads_view(out_k, "out_k", k.shape, q.dtype)
+    st = _call(lib.leet_attn_rope, dev, _heads_view(q, "q", q.shape, q.dtype), _heads_view(out_q, "out_q", q.shape, q.dtype),
+               Hq, vk, ok, Hk, _rotation(freq, layout, positions, pos0, scale, B, N), B, N, d, _dtype_code(q),
+               1 if transposed else 0)
+    if st != LEET_OK:
+        raise LeetAttnError(st, "leet_attn_rope")
+    return out_q if k is None else (out_q, out_k)
+
+
+def _weights(q: torch.Tensor, wq: Optional[torch.Tensor], wk: Optional[torch.Tensor], d: int) -> int:
+    """dtype code of the weights."""
+    dtype = q.dtype
+    for i, w in enumerate((wq, wk)):
+        if w is None:
+            continue
+        if tuple(w.shape) != (d,) or not w.is_contiguous():
+            raise ValueError("weights must be contiguous [d]")
+        if i == 1 and wq is not None and w.dtype != wq.dtype:
+            raise TypeError("q_weight and k_weight must share one dtype")
+        dtype = w.dtype
+    if dtype != q.dtype and dtype != torch.float32:
+        raise TypeError("weights must have the type of q or be float32")
+    return LEET_F32 if dtype == torch.float32 else _dtype_code(q)
+
+
+def leet_attn_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, q_weight: Optional[torch.Tensor],
+                           k_weight: Optional[torch.Tensor], freq: torch.Tensor, eps: float = 1e-6,
+                           positions: Optional[torch.Tensor] = None, pos0: int = 0, layout: int = ROPE_HALF,
+                           scale: float = 1.0, out_q: Optional[torch.Tensor] = None,
+                           out_k: Optional[torch.Tensor] = None):
+    """Norm of every head of q [B, Hq, N, d] and k [B, Hk, N, d], times its weight [d], then the rotation of
+    ``leet_attn_rope``, in one pass.  Returns (out_q, out_k): dense [B, H, N, d], as the prefill reads them, unless given."""
+    B, Hq, Hk, N, d = _heads_pair(q, k)
+    weight_dtype = _weights(q, q_weight, k_weight, d)
+    if out_q is None:
+        out_q = _new_dense(q)
+    if out_k is None:
+        out_k = _new_dense(k)
+    dev = _on(q, k, out_q, out_k, q_weight, k_weight, freq, positions)
+    st = _call(lib.leet_attn_qk_norm_rope, dev, _heads_view(q, "q", q.shape, q.dtype),
+               _heads_view(out_q, "out_q", q.shape, q.dtype), Hq, _heads_view(k, "k", k.shape, q.dtype),
+               _heads_view(out_k, "out_k", k.shape, q.dtype), Hk, _ptr(q_weight), _ptr(k_weight), weight_dtype, eps,
+               _rotation(freq, layout, positions, pos0, scale, B, N), B, N, d, _dtype_code(q))
+    if st != LEET_OK:
+        raise LeetAttnError(st, "leet_attn_qk_norm_rope")
+    return out_q, out_k
+
+
+def qk_norm_rope_workspace_bytes(B: int, Hq: int, Hk: int, N: int, d: int) -> int:
+    return int(lib.leet_attn_qk_norm_rope_workspace_bytes(B, Hq, Hk, N, d))
+
+
+def leet_attn_qk_norm_rope_backward(dout_q: torch.Tensor, dout_k: torch.Tensor, q: torch.Tensor, k: torch.Tensor,
+                                    q_weight: Optional[torch.Tensor], k_weight: Optional[torch.Tensor],
+                                    freq: torch.Tensor, eps: float = 1e-6, positions: Optional[torch.Tensor] = None,
+                                    pos0: int = 0, layout: int = ROPE_HALF, scale: float = 1.0,
+                                    dx_q: Optional[torch.Tensor] = None, dx_k: Optional[torch.Tensor] = None,
+                                    dq_weight: Optional[torch.Tensor] = None, dk_weight: Optional[torch.Tensor] = None,
+                                    workspace: Optional[torch.Tensor] = None):
+    """Gradients of ``leet_attn_qk_norm_rope``: (dx_q, dx_k, dq_weight, dk_weight) from those of its outputs and its
+    inputs.  A weight that is None has the gradient None."""
+    B, Hq, Hk, N, d = _heads_pair(q, k)
+    weight_dtype = _weights(q, q_weight, k_weight, d)
+    grads = []
+    for w, g, name in ((q_weight, dq_weight, "dq_weight"), (k_weight, dk_weight, "dk_weight")):
+        if w is None:
+            if g is not None:
+                raise ValueError(f"{name} without a weight")
+        elif g is None:
+            g = _new_dense(w)
+        elif g.dtype != w.dtype or g.shape != w.shape or not g.is_contiguous():
+            raise ValueError(f"{name} must be contiguous [d] of the weights' type")
+        grads.append(g)
+    dq_weight, dk_weight = grads
+    if dx_q is None:
+        dx_q = _new_dense(q)
+    if dx_k is None:
+        dx_k = _new_dense(k)
+    dev = _on(dout_q, dout_k, q, k, dx_q, dx_k, q_weight, k_weight, dq_weight, dk_weight, freq, positions, workspace)
+    need = 0
+    if workspace is None and (dq_weight is not None or dk_weight is not None):
+        need = qk_norm_rope_workspace_bytes(B, Hq, Hk, N, d)
+    ws, ws_bytes, keep = _scratch(need, workspace, dev)
+    t = q.dtype
+    st = _call(lib.leet_attn_qk_norm_rope_backward, dev, _heads_view(dout_q, "dout_q", q.shape, t),
+               _heads_view(q, "q", q.shape, t), _heads_view(dx_q, "dx_q", q.shape, t), Hq,
+               _heads_view(dout_k, "dout_k", k.shape, t), _heads_view(k, "k", k.shape, t),
+               _heads_view(dx_k, "dx_k", k.shape, t), Hk, _ptr(q_weight), _ptr(k_weight), _ptr(dq_weight),
+               _ptr(dk_weight), weight_dtype, eps, _rotation(freq, layout, positions, pos0, scale, B, N), ws, ws_bytes,
+               B, N, d, _dtype_code(q))
+    if st != LEET_OK:
+        raise LeetAttnError(st, "leet_attn_qk_norm_rope_backward")
+    return dx_q, dx_k, dq_weight, dk_weight
+
+
+def _gate_code(gate: torch.Tensor, x_dtype: torch.dtype) -> int:
+    if gate.dtype != x_dtype and gate.dtype != torch.float32:
+        raise TypeError("gate must have the type of x or be float32")
+    return _dtype_code(gate)
+
+
+def _scan_sequences(shape, offsets: Optional[torch.Tensor]) -> int:
+    """Number of sequences of a [B, N, C] call."""
+    if len(shape) != 3:
+        raise ValueError("x must be [B, N, C]")
+    if offsets is None:
+        return shape[0]
+    if offsets.dtype != torch.int32 or offsets.dim() != 1 or offsets.numel() < 1 or not offsets.is_contiguous():
+        raise ValueError("offsets must be a contiguous int32 tensor [sequences + 1]")
+    if shape[0] != 1:
+        raise ValueError("packed sequences need B = 1")
+    return offsets.numel() - 1
+
+
+def _scan_states(S: int, C: int, **states) -> None:
+    for name, s in states.items():
+        if s is not None and (s.dtype != torch.float32 or tuple(s.shape) != (S, C) or not s.is_contiguous()):
+            raise ValueError(f"{name} must be contiguous float32 [{S}, {C}]")
+
+
+def gated_scan_workspace_bytes(B: int, N: int, C: int, backward: bool = False) -> int:
+    return int(lib.leet_attn_gated_scan_workspace_bytes(B, N, C, 1 if backward else 0))
+
+
+def leet_attn_gated_scan(x: torch.Tensor, gate: torch.Tensor, mode: int = GATE_LOG, out: Optional[torch.Tensor] = None,
+                         state_in: Optional[torch.Tensor] = None, state_out: Optional[torch.Tensor] = None,
+                         offsets: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """Gated linear recurrence ``h_t = a_t h_{t-1} + b_t`` in every channel of x, gate [B, N, C]; returns h in x's type.
+
+    ``mode``: what the gate is (GATE_DECAY a itself, GATE_LOG its logarithm, GATE_SIGMOID its logit with b = (1 - a) x).
+    States are float32 [B, C]; with ``offsets`` (int32 [S + 1], B = 1: packed sequences) [S, C]."""
+    S = _scan_sequences(x.shape, offsets)
+    B, N, C = x.shape
+    _scan_states(S, C, state_in=state_in, state_out=state_out)
+    if out is None:
+        out = _new_dense(x)
+    dev = _on(x, gate, out, state_in, state_out, offsets, workspace)
+    t = x.dtype
+    need = gated_scan_workspace_bytes(B, N, C) if workspace is None else 0
+    ws, ws_bytes, keep = _scratch(need, workspace, dev)
+    st = _call(lib.leet_attn_gated_scan, dev, _rows_view(x, "x", x.shape, t), _rows_view(gate, "gate", x.shape, gate.dtype),
+               _rows_view(out, "out", x.shape, t), _ptr(state_in), _ptr(state_out), _ptr(offsets), S, ws, ws_bytes,
+               B, N, C, _dtype_code(x), _gate_code(gate, t), mode)
+    if st != LEET_OK:
+        raise LeetAttnError(st, "leet_attn_gated_scan")
+    return out
+
+
+def leet_attn_gated_scan_backward(dh: torch.Tensor, x: Optional[torch.Tensor], gate: torch.Tensor, h: torch.Tensor,
+                                  mode: int = GATE_LOG, dx: Optional[torch.Tensor] = None,
+                                  dgate: Optional[torch.Tensor] = None, state_in: Optional[torch.Tensor] = None,
+                                  dstate_out: Optional[torch.Tensor] = None, dstate_in: Optional[torch.Tensor] = None,
+                                  offsets: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """Gradients of ``leet_attn_gated_scan``: (dx, dgate), and dstate_in where given.
+
+    ``h`` is the forward call's output, ``dh`` its gradient, ``dstate_out`` that of state_out (None: zero); ``x`` is
+    read with GATE_SIGMOID only and may be None otherwise."""
+    S = _scan_sequences(h.shape, offsets)
+    B, N, C = h.shape
+    _scan_states(S, C, state_in=state_in, dstate_out=dstate_out, dstate_in=dstate_in)
+    if mode == GATE_SIGMOID and x is None:
+        raise ValueError("GATE_SIGMOID needs x")
+    if dx is None:
+        dx = _new_dense(h)
+    if dgate is None:
+        dgate = _new_dense(gate)
+    dev = _on(dh, x, gate, h, dx, dgate, state_in, dstate_out, dstate_in, offsets, workspace)
+    t, g = h.dtype, gate.dtype
+    need = gated_scan_workspace_bytes(B, N, C, True) if workspace is None else 0
+    ws, ws_bytes, keep = _scratch(need, workspace, dev)
+    st = _call(lib.leet_attn_gated_scan_backward, dev, _rows_view(dh, "dh", h.shape, t),
+               None if x is None else _rows_view(x, "x", h.shape, t), _rows_view(gate, "gate", h.shape, g),
+               _rows_view(h, "h", h.shape, t), _rows_view(dx, "dx", h.shape, t), _rows_view(dgate, "dgate", h.shape, g),
+               _ptr(state_in), _ptr(dstate_out), _ptr(dstate_in), _ptr(offsets), S, ws, ws_bytes, B, N, C,
+               _dtype_code(h), _gate_code(gate, t), mode)
+    if st != LEET_OK:
+        raise LeetAttnError(st, "leet_attn_gated_scan_backward")
+    return dx, dgate
+
+
+def leet_attn_gated_scan_step(x: torch.Tensor, gate: torch.Tensor, state: torch.Tensor, mode: int = GATE_LOG,
+                              out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """One token of every sequence: x, gate [B, C]; ``state`` (float32 [B, C]) is updated in place, ``out`` is it in x's type."""
+    if x.dim() != 2:
+        raise ValueError("x must be [B, C]")
+    B, C = x.shape
+    _scan_states(B, C, state=state)
+    if out is None:
+        out = _new_dense(x)
+    dev = _on(x, gate, out, state)
+    st = _call(lib.leet_attn_gated_scan_step, dev, _rows_view(x, "x", x.shape, x.dtype),
+               _rows_view(gate, "gate", x.shape, gate.dtype), _rows_view(out, "out", x.shape, x.dtype), _ptr(state), B, C,
+               _dtype_code(x), _gate_code(gate, x.dtype), mode)
+    if st != LEET_OK:
+        raise LeetAttnError(st, "leet_attn_gated_scan_step")
     return out

@@ -10,6 +10,7 @@
 #include "../../include/leet_attn.h"
 #include "../../include/leet_attn_bench.h"
 #include "leet_common.hpp"
+#include "leet_host.hpp"
 
 namespace leet {
 hipError_t launch_fwd_16bit_states(const FwdParams& p, int BH, int D, int DV, bool f16, hipStream_t stream);
@@ -308,7 +309,9 @@ constexpr size_t kStaticScratchBytes = (size_t)32 << 20;
 static __device__ __align__(256) unsigned char scratch[kStaticScratchBytes];
 void* g_scratch_ptr[kMaxDevices] = {nullptr};
 
-int current_device(int* dev) {
+}  // namespace
+
+int leet::current_device(int* dev) {
     if (hipGetDevice(dev) != hipSuccess) return LEET_ERR_LAUNCH;
     if (*dev < 0 || *dev >= kMaxDevices) return LEET_ERR_UNSUPPORTED;
     std::lock_guard<std::mutex> lock(g_ws_mutex);
@@ -319,6 +322,10 @@ int current_device(int* dev) {
     }
     return g_arch_ok[*dev] == 1 ? LEET_OK : LEET_ERR_UNSUPPORTED;
 }
+
+namespace {
+
+using leet::current_device;
 
 // Device address of this device's copy of the static scratch (device `dev` is current).
 int static_scratch(int dev, void** out) {
@@ -783,6 +790,6 @@ int leet_attn_set_decode_store(int mode) {
 
 int leet_attn_get_decode_store(void) { return g_decode_store.load(std::memory_order_relaxed); }
 
-const char* leet_attn_version(void) { return "0.8.1"; }
+const char* leet_attn_version(void) { return "0.9.0"; }
 
 }  // extern "C"

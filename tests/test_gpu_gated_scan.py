@@ -1,0 +1,299 @@
+"""The gated linear recurrence on the GPU, against its 64-bit form."""
+import pytest
+import torch
+
+import layer_forms as forms
+
+pytestmark = pytest.mark.gpu
+
+BF16, F16, F32 = torch.bfloat16, torch.float16, torch.float32
+TYPES = [(BF16, BF16), (BF16, F32), (F16, F16), (F16, F32), (F32, F32)]
+
+
+@pytest.fixture(scope="module")
+def leet():
+    from paper_2501_02573_amd import binding
+    return binding
+
+
+def _normal(shape, dtype, seed, sigma=1.0, mean=0.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(shape, generator=g) * sigma + mean).to(dtype).cuda()
+
+
+def _gate(shape, dtype, mode, seed):
+    """Decays from 0.3 to 0.999 and a few that forget everything."""
+    g = torch.Generator().manual_seed(seed)
+    log = -torch.exp(-6.9 * torch.rand(shape, generator=g))
+    log[torch.rand(shape, generator=g) < 0.01] = -200.0
+    z = log.exp() if mode == 0 else log if mode == 1 else torch.randn(shape, generator=g) * 3 + 2
+    return z.to(dtype).cuda()
+
+
+def _f64(t):
+    return None if t is None else t.detach().double().cpu()
+
+
+def _check(leet, B, N, C, types, mode, state, seed=1, x=None, gate=None, into=None):
+    dtype, gdt = types
+    x = _normal((B, N, C), dtype, seed) if x is None else x
+    z = _gate((B, N, C), gdt, mode, seed + 1) if gate is None else gate
+    s = _normal((B, C), F32, seed + 2, 3.0) if state else None
+    left = torch.full((B, C), 9.0, device="cuda") if state else None
+    h = leet.leet_attn_gated_scan(x, z, mode=mode, state_in=s, state_out=left, out=into)
+    want, last = forms.scan(_f64(z), _f64(x), mode, _f64(s))
+    assert forms.close(h, want)
+    assert left is None or forms.close(left, last)
+
+    dh = _normal((B, N, C), dtype, seed + 3)
+    ds = _normal((B, C), F32, seed + 4) if state else None
+    din = torch.full((B, C), 9.0, device="cuda") if state else None
+    dx, dz = leet.leet_attn_gated_scan_backward(dh, x if mode == 2 else None, z, h, mode=mode, state_in=s, dstate_out=ds,
+                                                dstate_in=din)
+    to_x, to_z, to_s = forms.scan_backward(_f64(dh), _f64(z), _f64(x), _f64(h), mode, _f64(s), _f64(ds))
+    assert dx.dtype == dtype and dz.dtype == gdt
+    assert forms.close(dx, to_x)
+    assert forms.close(dz, to_z)
+    assert din is None or forms.close(din, to_s)
+
+
+LENGTHS = [1, 2, 15, 16, 17, 100, 255, 256, 257, 700]
+
+
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("mode", [0, 1, 2])
+@pytest.mark.parametrize("N", LENGTHS)
+def test_lengths(leet, N, mode, types):
+    _check(leet, 2, N, 130 if N % 2 else 64, types, mode, state=N != 100)
+
+
+@pytest.mark.parametrize("types", [(BF16, BF16), (F32, F32), (F16, F32)])
+@pytest.mark.parametrize("C", [1, 2, 3, 63, 65, 127, 128, 255, 258, 1000])
+def test_channels(leet, C, types):
+    _check(leet, 3, 50, C, types, mode=C % 3, state=True)
+
+
+@pytest.mark.parametrize("mode", [0, 1, 2])
+def test_long(leet, mode):
+    _check(leet, 1, 5000, 64, (BF16, F32), mode, state=True)
+    _check(leet, 1, 4099, 66, (F32, F32), mode, state=False)
+
+
+def test_many_sequences(leet):
+    _check(leet, 70, 33, 200, (BF16, BF16), 1, state=True)
+
+
+@pytest.mark.parametrize("shift", [0, 1, 2])
+@pytest.mark.parametrize("types", [(BF16, BF16), (F16, F32), (F32, F32)])
+def test_parts_of_wider_rows(leet, types, shift):
+    """x and the gate as column ranges of one projection, its storage off its alignment; out into a wider buffer."""
+    B, N, C = 2, 90, 70
+    wide = _normal((B * N * 3 * C + shift,), types[0], 5)[shift:].view(B, N, 3 * C)
+    x, gate = wide[:, :, C:2 * C], None
+    if types[0] == types[1]:
+        gate = wide[:, :, 2 * C:]
+        gate.copy_(_gate((B, N, C), types[1], 1, 6))
+    buf = torch.full((B, N, 2 * C + 1), 4.0, dtype=types[0], device="cuda")
+    _check(leet, B, N, C, types, 1, True, x=x, gate=gate, into=buf[:, :, 3:C + 3])
+    assert bool((buf[:, :, :3] == 4).all()) and bool((buf[:, :, C + 3:] == 4).all())
+
+
+def test_rows_of_heads(leet):
+    """Channels of the attention's [B, H, N, d] layout: sequences are (b, h)."""
+    x = _normal((2, 3, 40, 64), BF16, 7)
+    _check(leet, 6, 40, 64, (BF16, BF16), 2, True, x=x.view(6, 40, 64))
+
+
+def _offsets(lengths):
+    return torch.tensor([0] + list(torch.tensor(lengths).cumsum(0)), dtype=torch.int32)
+
+
+PACKS = [[5], [1, 1, 1], [0, 3, 0, 0, 20, 0], [16, 16, 32], [15, 17, 256, 1], [300, 0, 2, 700], [255, 1, 256, 0, 0, 90],
+         [0, 0, 0], [3] * 100, [1000, 24]]
+
+
+@pytest.mark.parametrize("types", [(BF16, BF16), (F16, F32), (F32, F32)])
+@pytest.mark.parametrize("mode", [0, 1, 2])
+@pytest.mark.parametrize("i, lengths", list(enumerate(PACKS)))
+def test_packed(leet, i, lengths, mode, types):
+    dtype, gdt = types
+    off = _offsets(lengths)
+    S, total, C = len(lengths), int(off[-1]), 66 if i % 2 else 129
+    N = total + (0 if i % 3 == 0 and total else 40)   # rows behind the last sequence
+    x, z = _normal((1, N, C), dtype, 60), _gate((1, N, C), gdt, mode, 61)
+    x[:, total:], z[:, total:] = float("nan"), float("nan")
+    s, given = _normal((S, C), F32, 62, 3.0), i % 4 != 3
+    left = torch.full((S, C), 9.0, device="cuda")
+    out = torch.full((1, N, C), 7.0, dtype=dtype, device="cuda")
+    leet.leet_attn_gated_scan(x, z, mode=mode, out=out, state_in=s if given else None, state_out=left, offsets=off.cuda())
+    dh = _normal((1, N, C), dtype, 63)
+    dh[:, total:] = float("nan")
+    ds, din = _normal((S, C), F32, 64), torch.full((S, C), 9.0, device="cuda")
+    dx, dz = torch.full_like(x, 7.0), torch.full_like(z, 7.0)
+    leet.leet_attn_gated_scan_backward(dh, x, z, out, mode=mode, dx=dx, dgate=dz, state_in=s if given else None,
+                                       dstate_out=ds if given else None, dstate_in=din, offsets=off.cuda())
+    assert all(bool((t[:, total:] == 7).all()) for t in (out, dx, dz))
+    for j in range(S):
+        lo, hi = int(off[j]), int(off[j + 1])
+        s_j = _f64(s[j:j + 1]) if given else None
+        want, last = forms.scan(_f64(z[:, lo:hi]), _f64(x[:, lo:hi]), mode, s_j)
+        assert forms.close(out[:, lo:hi], want) and forms.close(left[j:j + 1], last)
+        to_x, to_z, to_s = forms.scan_backward(_f64(dh[:, lo:hi]), _f64(z[:, lo:hi]), _f64(x[:, lo:hi]), _f64(out[:, lo:hi]),
+                                               mode, s_j, _f64(ds[j:j + 1]) if given else None)
+        assert forms.close(dx[:, lo:hi], to_x) and forms.close(dz[:, lo:hi], to_z) and forms.close(din[j:j + 1], to_s)
+
+
+def test_nothing_crosses_from_one_sequence_to_the_next(leet):
+    off, C = _offsets([40, 300, 7]), 64
+    x, z = _normal((1, 347, C), BF16, 70), _gate((1, 347, C), BF16, 1, 71)
+    clean = leet.leet_attn_gated_scan(x, z, offsets=off.cuda())
+    dh = _normal((1, 347, C), BF16, 72)
+    dclean = leet.leet_attn_gated_scan_backward(dh, None, z, clean, offsets=off.cuda())
+    x[:, 100, :32], x[:, 100, 32:] = float("nan"), float("inf")
+    h = leet.leet_attn_gated_scan(x, z, offsets=off.cuda())
+    inside = slice(40, 340)
+    assert not bool(h[:, 100:340].isfinite().any())
+    h[:, inside] = clean[:, inside]
+    assert torch.equal(h, clean)
+    dh[:, 200] = float("inf")
+    dx, dz = leet.leet_attn_gated_scan_backward(dh, None, z, clean, offsets=off.cuda())
+    assert not bool(dx[:, 40:201].isfinite().any())
+    for got, want in zip((dx, dz), dclean):
+        got[:, inside] = want[:, inside]
+        assert torch.equal(got, want)
+
+
+def test_a_channel_that_is_not_finite_stays_by_itself(leet):
+    x, z = _normal((2, 600, 130), F32, 73), _gate((2, 600, 130), F32, 0, 74)
+    clean = leet.leet_attn_gated_scan(x, z, mode=0)
+    x[1, 5, 77] = float("inf")
+    h = leet.leet_attn_gated_scan(x, z, mode=0)
+    assert not bool(h[1, 5:, 77].isfinite().any()) and torch.equal(h[1, :5], clean[1, :5])
+    h[1, :, 77] = clean[1, :, 77]
+    assert torch.equal(h, clean)
+
+
+def test_ends_of_the_gates(leet):
+    """Decays of exactly 0 and 1, logits and logarithms at the ends of their type."""
+    lowest = torch.finfo(F32).min
+    for mode, ends in ((0, (0.0, 1.0, -1.0, -0.0)), (1, (0.0, -float("inf"), lowest, -1e-30)),
+                       (2, (float("inf"), -float("inf"), lowest, 90.0))):
+        z = _gate((1, 300, 64), F32, mode, 75)
+        for j, v in enumerate(ends):
+            z[:, j::7] = v
+        _check(leet, 1, 300, 64, (F32, F32), mode, True, gate=z)
+
+
+@pytest.mark.parametrize("packed", [False, True])
+def test_states_in_place(leet, packed):
+    N, C = 1500, 96
+    off = _offsets([700, 0, 1, 799]).cuda() if packed else None
+    x, z = _normal((1, N, C), BF16, 80), _gate((1, N, C), F32, 1, 81)
+    s = _normal((4 if packed else 1, C), F32, 82)
+    left = torch.empty_like(s)
+    h = leet.leet_attn_gated_scan(x, z, state_in=s, state_out=left, offsets=off)
+    both = s.clone()
+    h2 = leet.leet_attn_gated_scan(x, z, state_in=both, state_out=both, offsets=off)
+    assert torch.equal(h, h2) and torch.equal(both, left)
+    dh, ds = _normal((1, N, C), BF16, 83), _normal(s.shape, F32, 84)
+    din, both = torch.empty_like(s), ds.clone()
+    one = leet.leet_attn_gated_scan_backward(dh, None, z, h, state_in=s, dstate_out=ds, dstate_in=din, offsets=off)
+    two = leet.leet_attn_gated_scan_backward(dh, None, z, h, state_in=s, dstate_out=both, dstate_in=both, offsets=off)
+    assert torch.equal(both, din) and all(torch.equal(a, b) for a, b in zip(one, two))
+
+
+@pytest.mark.parametrize("C", [66, 1, 33])
+def test_no_tokens_hand_the_state_on(leet, C):
+    x = torch.empty((2, 0, C), dtype=BF16, device="cuda")
+    s, left = _normal((2, C), F32, 85), torch.full((2, C), 9.0, device="cuda")
+    leet.leet_attn_gated_scan(x, x, state_in=s, state_out=left)
+    assert torch.equal(s, left)
+    leet.leet_attn_gated_scan(x, x, state_out=left)
+    assert bool((left == 0).all())
+    leet.leet_attn_gated_scan_backward(x, None, x, x, dstate_out=s, dstate_in=left)
+    assert torch.equal(s, left)
+
+
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("mode", [0, 1, 2])
+@pytest.mark.parametrize("B, C", [(1, 1), (3, 64), (2, 130), (5, 1001), (64, 4096)])
+def test_step(leet, B, C, mode, types):
+    dtype, gdt = types
+    x, z, s = _normal((B, C), dtype, 90), _gate((B, C), gdt, mode, 91), _normal((B, C), F32, 92, 3.0)
+    want, last = forms.scan(_f64(z)[:, None], _f64(x)[:, None], mode, _f64(s))
+    out = leet.leet_attn_gated_scan_step(x, z, s, mode=mode)
+    assert forms.close(out, (want[0][:, 0], want[1][:, 0])) and forms.close(s, last)
+
+
+def test_step_on_parts_of_rows(leet):
+    wide = _normal((3, 400), BF16, 93)
+    x, z = wide[:, 8:108], wide[:, 201:301]
+    z.copy_(_gate((3, 100), BF16, 1, 94))
+    s = _normal((3, 100), F32, 95)
+    want, last = forms.scan(_f64(z)[:, None], _f64(x)[:, None], 1, _f64(s))
+    buf = torch.full((3, 150), 4.0, dtype=BF16, device="cuda")
+    out = leet.leet_attn_gated_scan_step(x, z, s, out=buf[:, 20:120])
+    assert forms.close(out, (want[0][:, 0], want[1][:, 0])) and forms.close(s, last)
+    assert bool((buf[:, :20] == 4).all()) and bool((buf[:, 120:] == 4).all())
+
+
+def test_prefill_then_steps_is_one_longer_prefill(leet):
+    B, N, T, C = 2, 301, 5, 128
+    x, z = _normal((B, N + T, C), BF16, 96), _gate((B, N + T, C), BF16, 2, 97)
+    want, last = forms.scan(_f64(z), _f64(x), 2)
+    s = torch.empty((B, C), device="cuda")
+    h = [leet.leet_attn_gated_scan(x[:, :N], z[:, :N], mode=2, state_out=s)]
+    h += [leet.leet_attn_gated_scan_step(x[:, t], z[:, t], s, mode=2)[:, None] for t in range(N, N + T)]
+    assert forms.close(torch.cat(h, 1), want) and forms.close(s, last)
+
+
+def test_gradient_against_differences(leet):
+    """d/de of sum(h(z + e dz, x + e dx, s + e ds) dh) by the kernel's own forward pass, in fp32 over a short run: the
+    difference is off by 2^-24 of the sum's terms over 2 e, and by e^2 of its third derivative."""
+    B, N, C, e = 1, 40, 64, 2.0 ** -7
+    z, x = _gate((B, N, C), F32, 2, 98), _normal((B, N, C), F32, 99)
+    s, dh = _normal((B, C), F32, 100), _normal((B, N, C), F32, 101)
+    step = [_normal(t.shape, F32, 102 + i) for i, t in enumerate((z, x, s))]
+
+    def value(m):
+        h = leet.leet_attn_gated_scan(x + m * step[1], z + m * step[0], mode=2, state_in=s + m * step[2])
+        return (h.double() * dh.double()).sum().item(), (h.double() * dh.double()).abs().sum().item()
+
+    h = leet.leet_attn_gated_scan(x, z, mode=2, state_in=s)
+    din = torch.empty_like(s)
+    dx, dz = leet.leet_attn_gated_scan_backward(dh, x, z, h, mode=2, state_in=s, dstate_in=din)
+    slope = sum((a.double() * b.double()).sum().item() for a, b in zip((dz, dx, din), step))
+    (up, terms), (down, _) = value(e), value(-e)
+    (up2, _), (down2, _) = value(2 * e), value(-2 * e)
+    fine, coarse = (up - down) / (2 * e), (up2 - down2) / (4 * e)
+    # the error of the coarse difference is four times the fine one's, which their distance therefore bounds
+    assert abs(slope - fine) <= abs(coarse - fine) + 2 * N * forms.U * terms / e
+
+
+def test_on_another_stream_and_in_a_graph(leet):
+    x, z = _normal((1, 3000, 128), BF16, 110), _gate((1, 3000, 128), BF16, 1, 111)
+    dh, s = _normal((1, 3000, 128), BF16, 112), _normal((1, 128), F32, 113)
+    left, din = torch.empty_like(s), torch.empty_like(s)
+
+    def both():
+        h = leet.leet_attn_gated_scan(x, z, state_in=s, state_out=left)
+        return (h, left.clone()) + leet.leet_attn_gated_scan_backward(dh, None, z, h, state_in=s, dstate_in=din) + (din.clone(),)
+
+    want = both()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        got = both()
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        kept = both()
+    for sign in (1, -1, 1, -1):
+        x.mul_(sign)
+        graph.replay()
+        torch.cuda.synchronize()
+        seen = [t.clone() for t in kept]
+        eager = both()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(eager, seen))
