@@ -2,6 +2,7 @@
 #pragma once
 
 #include <hip/hip_runtime.h>
+#include <stddef.h>
 
 namespace leet {
 
@@ -24,10 +25,17 @@ struct GatedScanParams {
     const int* offsets;            // [S + 1] or null: S = B sequences of N tokens
     int sequences;                 // S
     int B, N, C;
-    int columns;                   // column blocks of a sequence
+    int vector;                    // channels a lane may hold: 1, 2, 4 or 8
+    int columns;                   // column blocks of a batch entry
     int waves;                     // waves of a workgroup
-    int vector;                    // channels a lane holds
+    int tiles;                     // of a column block's N tokens
+    void* workspace;               // more than one tile: gated_scan_workspace bytes
 };
+
+// Bytes of workspace for these sizes; 0: none is needed.
+size_t gated_scan_workspace(int B, int N, int C, bool backward);
+// Threads that a launch of these sizes has, whatever the rows' alignment.
+long long gated_scan_threads(int B, int N, int C, bool backward);
 
 // elem, gate_elem: 0 = fp32, 1 = bf16, 2 = fp16; gate_elem is elem or 0.  mode: a leet_gate_mode
 hipError_t launch_gated_scan(GatedScanParams p, int elem, int gate_elem, int mode, hipStream_t stream);

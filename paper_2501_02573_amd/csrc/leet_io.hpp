@@ -1,6 +1,8 @@
 // Loads and stores of fp32, bf16 and fp16 elements as fp32 values, for the kernels that are bound by them.
 #pragma once
 
+#include <type_traits>
+
 #include "leet_common.hpp"
 
 namespace leet {
@@ -15,6 +17,24 @@ struct Io {
     static __device__ __forceinline__ uint32_t pack2(float a, float b) {
         return kElem == 1 ? ElemBf16::pack2(a, b) : ElemF16::pack2(a, b);
     }
+
+    // One or two adjacent elements as they lie in memory, so that many can be under way before any is looked at.
+    template <int V>
+    struct Raw {
+        static_assert(V == 1 || V == 2, "one or two elements");
+        using Word = typename std::conditional<kElem == 0, typename std::conditional<V == 1, float, float2>::type,
+                                               typename std::conditional<V == 1, uint16_t, uint32_t>::type>::type;
+        Word word;
+        __device__ __forceinline__ void load(const char* p) { word = *reinterpret_cast<const Word*>(p); }
+        __device__ __forceinline__ void get(float* f) const {
+            if constexpr (kElem == 0 && V == 1) f[0] = word;
+            else if constexpr (kElem == 0) { f[0] = word.x; f[1] = word.y; }
+            else {
+                f[0] = lo(word);
+                if constexpr (V == 2) f[1] = hi(word);
+            }
+        }
+    };
 
     // V adjacent elements at p (aligned to all of them, to 16 bytes at most)
     template <int V>

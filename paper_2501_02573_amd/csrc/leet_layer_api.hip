@@ -142,7 +142,8 @@ int scan_sizes_ok(const int* offsets, int sequences, const void* workspace, size
                   int backward, int* S) {
     if (B <= 0 || N < 0 || C <= 0) return LEET_ERR_INVALID_ARG;
     if (offsets && (B != 1 || sequences < 0 || !aligned(offsets, 4))) return LEET_ERR_INVALID_ARG;
-    if (N > 1 << 30 || C > 1 << 28 || (long long)B * ((C + 63) / 64) * 1024 >= kMaxThreads) return LEET_ERR_TOO_LARGE;
+    if (N > 1 << 30 || C > 1 << 28 || leet::gated_scan_threads(B, N, C, backward != 0) >= kMaxThreads)
+        return LEET_ERR_TOO_LARGE;
     const size_t need = leet_attn_gated_scan_workspace_bytes(B, N, C, backward);
     if (need && (!workspace || workspace_bytes < need || !aligned(workspace, 256))) return LEET_ERR_INVALID_ARG;
     *S = offsets ? sequences : B;
@@ -258,7 +259,8 @@ int leet_attn_qk_norm_rope_backward(const leet_attn_heads *dout_q, const leet_at
 }
 
 size_t leet_attn_gated_scan_workspace_bytes(int B, int N, int C, int backward) {
-    return 0;
+    if (B <= 0 || N <= 0 || C <= 0 || N > 1 << 30 || C > 1 << 28) return 0;
+    return leet::gated_scan_workspace(B, N, C, backward != 0);
 }
 
 int leet_attn_gated_scan(const leet_attn_rows *x, const leet_attn_rows *gate, const leet_attn_rows *out,
@@ -286,6 +288,7 @@ int leet_attn_gated_scan(const leet_attn_rows *x, const leet_attn_rows *gate, co
     p.offsets = offsets;
     p.sequences = S;
     p.B = B; p.N = N; p.C = C;
+    p.workspace = workspace;
     int dev = 0;
     status = leet::current_device(&dev);
     if (status != LEET_OK) return status;
@@ -331,6 +334,7 @@ int leet_attn_gated_scan_backward(const leet_attn_rows *dh, const leet_attn_rows
     p.offsets = offsets;
     p.sequences = S;
     p.B = B; p.N = N; p.C = C;
+    p.workspace = workspace;
     int dev = 0;
     status = leet::current_device(&dev);
     if (status != LEET_OK) return status;

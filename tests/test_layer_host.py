@@ -170,7 +170,7 @@ def test_scan_refused(leet):
             (UNSUPPORTED, dict(dtype=leet.LEET_F32, gd=leet.LEET_BF16))]
     seq = [(INVALID, dict(N=-1)), (INVALID, dict(offsets=P)), (INVALID, dict(offsets=P + 2, B=1)),
            (INVALID, dict(offsets=P, B=1, S=-1)), (INVALID, dict(s_in=P + 2)), (INVALID, dict(s_out=P + 2)),
-           (LARGE, dict(C=1 << 29)), (LARGE, dict(N=(1 << 30) + 1)), (LARGE, dict(B=1 << 20))]
+           (LARGE, dict(C=1 << 29)), (LARGE, dict(N=(1 << 30) + 1)), (LARGE, dict(B=1 << 26))]
     for want, change in both + seq:
         assert _scan(leet, _scan_args(leet, **change)) == want, change
         assert _scan_back(leet, _scan_args(leet, **change)) == want, change
