@@ -22,27 +22,34 @@
 
 namespace leet {
 
-#ifndef SCAN_TOKENS
-#define SCAN_TOKENS 8
-#define SCAN_WAVES 16
-#endif
-constexpr int kScanTokens = SCAN_TOKENS;  // of a wave at a time
-constexpr int kScanWaves = SCAN_WAVES;   // of a workgroup, at most
+// A tile: tokens of a wave, and waves of a workgroup that hold tokens (at most); one more wave links the tile to the others.
+// Whole workgroups of 8 and 12 waves spread evenly over the four SIMDs of a compute unit.  us at B4 N4096 C2048 bf16
+// (forward) and N32768 C4096: 16 x 7 57 and 196, 16 x 5 68 and 230, 12 x 9 71 and 240, 8 x 15 60 and 211; backward at
+// B4 N4096 C2048, sigmoid: 8 x 11 93, 12 x 7 96, 8 x 7 102, 8 x 9 102, 16 x 7 154 (registers: one workgroup a unit).
+struct ForwardTile {
+    static constexpr int kTokens = 16, kWaves = 7;
+};
+struct BackwardTile {
+    static constexpr int kTokens = 8, kWaves = 11;
+};
 
-// The decay a and, for the moving average, 1 - a (as accurate as a itself however near 1 that is).
+// The decay a and, for the moving average, 1 - a (each as accurate as the smaller of the two: the larger one is what that
+// leaves of 1).
 template <int kMode>
 __device__ __forceinline__ void decay(float z, float& a, float& rest) {
     if constexpr (kMode == 0) a = z;
     else if constexpr (kMode == 1) a = expf(z);
     else {
         const float e = expf(-fabsf(z));
-        const float large = 1.0f / (1.0f + e), small = e * large;
+        const float small = e * __builtin_amdgcn_rcpf(1.0f + e), large = 1.0f - small;
         a = z >= 0.0f ? large : small;
         rest = z >= 0.0f ? small : large;
     }
 }
 
-// Where the tokens t0 .. t0 + kScanTokens - 1 lie among packed sequences.  Lane i < kScanTokens looks at token t0 + i.
+// Where the tokens t0 .. t0 + kTokens - 1 lie among packed sequences.  Lane i < kTokens looks at token t0 + i.  A token's
+// sequence is the last one that begins at or before it: of empty ones at one place the one behind them.
+template <int kTokens>
 struct Places {
     int sequence;          // this lane's token's
     uint32_t first, last;  // tokens that begin, end a sequence
@@ -50,16 +57,38 @@ struct Places {
 
     Places() = default;
     __device__ __forceinline__ Places(const int* offsets, int sequences, int t0, int N, int lane) {
-        const int t = t0 + min(lane, kScanTokens - 1);
-        // the last sequence that begins at or before t: of empty ones at one place the one behind them
-        int lo = 0, hi = sequences;  // offsets[lo] <= t < offsets[hi + 1], with offsets[S + 1] infinite
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (offsets[mid] <= t) lo = mid;
-            else hi = mid - 1;
+        // the last s <= sequences with offsets[s] <= t0, 64 of the candidates at a time
+        int s0 = 0, high = sequences;
+        while (s0 < high) {
+            const int step = (high - s0 + 63) / 64, s = s0 + (lane + 1) * step;
+            s0 += step * __popcll(__ballot(s <= high && offsets[s <= high ? s : high] <= t0));
+            high = min(high, s0 + step - 1);
         }
-        const bool in = lo < sequences && t < N && lane < kScanTokens;
-        sequence = min(lo, sequences - 1);
+        const int end = min(t0 + kTokens, N);  // of the tokens that are there
+        sequence = s0;
+        first = last = inside = 0;
+        if (s0 >= sequences || t0 >= N) return;  // behind the last sequence
+        const uint32_t all = (uint32_t)((1u << (end - t0)) - 1u);
+        const int begins = offsets[s0], ends = offsets[s0 + 1];
+        if (ends >= end) {  // one sequence
+            first = begins == t0 ? 1u : 0u;
+            last = ends == end ? 1u << (end - t0 - 1) : 0u;
+            inside = all;
+            return;
+        }
+        // boundaries at or before the lane's token, 64 at a time
+        for (int from = s0 + 1; from <= sequences; from += 64) {
+            const int at = from + lane <= sequences ? offsets[from + lane] : 0x7fffffff;
+#pragma unroll
+            for (int i = 0; i < kTokens; ++i) {
+                const int before = __popcll(__ballot(at <= t0 + i));
+                sequence += lane == i ? before : 0;
+            }
+            if (__ballot(at < end) != ~0ull) break;
+        }
+        const int t = t0 + lane;
+        const bool in = t < end && sequence < sequences;
+        sequence = min(sequence, sequences - 1);
         first = (uint32_t)__ballot(in && offsets[sequence] == t);
         last = (uint32_t)__ballot(in && offsets[sequence + 1] == t + 1);
         inside = (uint32_t)__ballot(in);
@@ -72,10 +101,6 @@ template <int kElem>
 __device__ __forceinline__ const char* row_at(const RowsIn& r, int b, long long t, uint32_t c) {
     return r.data + (b * r.batch + t * r.token) * Io<kElem>::kBytes + c * Io<kElem>::kBytes;
 }
-template <int kElem, int kV>
-__device__ __forceinline__ void load_channels(const RowsIn& r, int b, long long t, uint32_t c, float* f) {
-    Io<kElem>::template load<kV>(row_at<kElem>(r, b, t, c), f);
-}
 template <int kV>
 __device__ __forceinline__ void zero(float* f) {
 #pragma unroll
@@ -83,8 +108,9 @@ __device__ __forceinline__ void zero(float* f) {
 }
 template <int kElem, int kV>
 __device__ __forceinline__ void store_channels(const RowsOut& r, int b, long long t, uint32_t c, const float* f) {
-    char* row = r.data + (b * r.batch + t * r.token) * Io<kElem>::kBytes;
-    Io<kElem>::template store<kV>(row + c * Io<kElem>::kBytes, f);
+    typename Io<kElem>::template Raw<kV> raw;
+    raw.set(f);
+    raw.store(r.data + (b * r.batch + t * r.token) * Io<kElem>::kBytes + c * Io<kElem>::kBytes);
 }
 template <int kV>
 __device__ __forceinline__ void load_state(const float* s, int sequence, int C, uint32_t c, float* f) {
@@ -144,47 +170,77 @@ struct Board {
         publish(states + k * (tile / kV), s[0], s[kV - 1]);
     }
 
-    // The state behind tile k of the chain: looks back over what has been published until it meets an inclusive state,
-    // kWindow tiles at a time, and waits for those that have published nothing.  Every wait ends: a tile publishes its
-    // run (or its state) without waiting for anything, and tiles are taken in the order of the chain, so all that are
-    // waited for belong to workgroups that are running already.
+    // A window of what tiles k, k - 1, .. have published.
     template <int kV>
-    __device__ __forceinline__ void state_behind(int k, bool live, float* state) const {
-        constexpr int kWindow = 4;
-        float A[kV], H[kV];
+    struct Window {
+        static constexpr int kTiles = 4;
+        uint64_t run[kTiles][kV], whole[kTiles];
+        int runs;    // so many, from tile k on, have published their runs ..
+        bool ended;  // .. and the next one its state
+
+        __device__ __forceinline__ void load(const Board& board, int k, bool live) {
 #pragma unroll
-        for (int v = 0; v < kV; ++v) { A[v] = 1.0f; H[v] = 0.0f; }
-        while (true) {
-            uint64_t run[kWindow][kV], whole[kWindow];
+            for (int u = 0; u < kTiles; ++u) {
+                const int j = max(k - u, 0);
+                whole[u] = live ? look(board.states + j * (board.tile / kV)) : 0;
 #pragma unroll
-            for (int u = 0; u < kWindow; ++u) {
-                const int j = k - u < 0 ? 0 : k - u;
-                whole[u] = live ? look(states + j * (tile / kV)) : 0;
-#pragma unroll
-                for (int v = 0; v < kV; ++v) run[u][v] = live ? look(runs + j * tile + v) : 0;
+                for (int v = 0; v < kV; ++v) run[u][v] = live ? look(board.runs + j * board.tile + v) : 0;
             }
-            int seen = 0;
+            runs = 0;
+            ended = false;
 #pragma unroll
-            for (int u = 0; u < kWindow; ++u) {
-                if (seen != u || u > k) continue;  // behind one that has to be waited for, or before the first tile
-                if (__all(is_set(whole[u]))) {
-#pragma unroll
-                    for (int v = 0; v < kV; ++v) state[v] = fmaf(A[v], v ? high(whole[u]) : low(whole[u]), H[v]);
-                    return;
-                }
+            for (int u = 0; u < kTiles; ++u) {
                 bool set = true;
 #pragma unroll
                 for (int v = 0; v < kV; ++v) set = set && is_set(run[u][v]);
-                if (!__all(set)) continue;
+                if (runs == u && !ended) {
+                    if (__all(is_set(whole[u]))) ended = true;
+                    else if (__all(set)) ++runs;  // never the first tile, which publishes its state alone
+                }
+            }
+        }
+        // from the state behind the tile after the window's runs (or the one that ended it) to the state behind tile k
+        __device__ __forceinline__ void fold(float* state) const {
+#pragma unroll
+            for (int u = kTiles - 1; u >= 0; --u)
 #pragma unroll
                 for (int v = 0; v < kV; ++v) {
-                    H[v] = fmaf(A[v], high(run[u][v]), H[v]);
-                    A[v] *= low(run[u][v]);
+                    if (ended && u == runs) state[v] = v ? high(whole[u]) : low(whole[u]);
+                    if (u < runs) state[v] = fmaf(low(run[u][v]), state[v], high(run[u][v]));
                 }
-                ++seen;
-            }
-            k -= seen;
         }
+    };
+
+    // The state behind tile k of the chain: looks back until it meets a tile whose state is known, waiting for those that
+    // have published nothing, and goes forward from there over the runs.  So it is the same chain of fused multiply-adds
+    // whatever was known when: results do not depend on timing.  Every wait ends: a tile publishes its run (or its state)
+    // without waiting for anything, and tiles are taken in the order of the chain, so all that are waited for belong to
+    // workgroups that are running already.
+    template <int kV>
+    __device__ __forceinline__ void state_behind(int k, bool live, float* state) const {
+        constexpr int kTiles = Window<kV>::kTiles;
+        Window<kV> near, far;
+        do near.load(*this, k, live);
+        while (!near.ended && near.runs < kTiles);
+        zero<kV>(state);
+        if (!near.ended) {
+            int j = k - kTiles;
+            while (true) {
+                far.load(*this, j, live);
+                if (far.ended) break;
+                j -= far.runs;
+            }
+            far.fold(state);
+            // tiles j + 1 .. k - kTiles, whose runs have all been seen; the last window of them may be a short one
+            for (j += kTiles; j < k; j += kTiles) {
+                const int top = min(j, k - kTiles), skip = j - top;
+                far.load(*this, top, live);
+                far.ended = false;
+                far.runs = kTiles - skip;
+                far.fold(state);
+            }
+        }
+        near.fold(state);
     }
 };
 
@@ -195,17 +251,17 @@ __global__ __launch_bounds__(256) void gated_scan_clear_kernel(u32x4* words, siz
 }
 
 // Shared by the waves of a workgroup.
-template <int kV>
+template <int kV, int kWaves>
 struct Shared {
-    float A[kScanWaves][64 * kV], H[kScanWaves][64 * kV];  // the waves' runs
-    int cut[kScanWaves];  // a sequence begins (backward: ends) in the run: what came before it does not reach behind it
+    float A[kWaves][64 * kV], H[kWaves][64 * kV];  // the waves' runs
+    int cut[kWaves];  // a sequence begins (backward: ends) in the run: what came before does not reach behind it
     float carry[64 * kV];
     unsigned ticket;
 };
 
 // The tile of a workgroup: column block `block` of all batch entries, tile k of its chain.
-template <int kV>
-__device__ __forceinline__ void take_tile(const GatedScanParams& p, Shared<kV>& shared, int* block, int* k) {
+template <class S>
+__device__ __forceinline__ void take_tile(const GatedScanParams& p, S& shared, int* block, int* k) {
     unsigned ticket = blockIdx.x;
     const unsigned blocks = (unsigned)p.B * (unsigned)p.columns;
     if (p.tiles > 1) {
@@ -218,13 +274,49 @@ __device__ __forceinline__ void take_tile(const GatedScanParams& p, Shared<kV>& 
     *k = (int)(ticket / blocks);
 }
 
-// Joins the runs of a tile's waves in the order of the chain (kBackward: from the last wave to the first).  before[] is
-// the state before this wave's run, after the state behind the whole tile (wave 0 only).  entering: wave 0's, the state
-// before the whole tile where the chain begins.
-template <int kV, bool kBackward, bool kPacked>
-__device__ __forceinline__ void join_runs(const GatedScanParams& p, Shared<kV>& shared, int block, int k, int wave, int lane,
-                                          bool live, const float* A, const float* H, bool cut, const float* entering,
-                                          float* before, float* after) {
+// The wave behind the data waves links the tile to the others: it joins the waves' runs, publishes, looks back, and leaves
+// the state before the tile in shared.carry.  The registers that looking back takes are then not beside a tile's data.
+// kBackward: the chain goes from the last wave to the first.
+template <int kV, bool kBackward, bool kPacked, class S>
+__device__ __forceinline__ void link_tile(const GatedScanParams& p, S& shared, int block, int k, int lane, bool live,
+                                          const float* state_in, float* state_out, int b, uint32_t c) {
+    float carry[kV], A[kV], H[kV];
+    if (!kPacked && k == 0 && live) load_state<kV>(state_in, b, p.C, c, carry);
+    else zero<kV>(carry);
+    __syncthreads();  // the waves' runs are there
+    bool cut = false;
+#pragma unroll
+    for (int v = 0; v < kV; ++v) { A[v] = 1.0f; H[v] = 0.0f; }
+    for (int i = 0; i < p.waves; ++i) {
+        const int w = kBackward ? p.waves - 1 - i : i;
+        const bool here = kPacked && shared.cut[w];
+        cut = cut || here;
+#pragma unroll
+        for (int v = 0; v < kV; ++v) {
+            const float Hw = shared.H[w][lane * kV + v], Aw = shared.A[w][lane * kV + v];
+            H[v] = here ? Hw : fmaf(Aw, H[v], Hw);
+            A[v] *= Aw;
+        }
+    }
+    const Board board = Board::of<kV>(p, block, lane);
+    if (k > 0) {
+        if (live && !cut) board.publish_run<kV>(k, A, H);
+        if (live && cut) board.publish_state<kV>(k, H);
+        board.state_behind<kV>(k - 1, live, carry);
+    }
+#pragma unroll
+    for (int v = 0; v < kV; ++v) shared.carry[lane * kV + v] = carry[v];
+    __syncthreads();  // the state before the tile is there
+#pragma unroll
+    for (int v = 0; v < kV; ++v) H[v] = cut ? H[v] : fmaf(A[v], carry[v], H[v]);
+    if (live && k + 1 < p.tiles && (k == 0 || !cut)) board.publish_state<kV>(k, H);
+    if (!kPacked && live && k == p.tiles - 1) store_state<kV>(state_out, b, p.C, c, H);
+}
+
+// A data wave's part: its run goes to the others; before[] receives the state before it.
+template <int kV, bool kBackward, bool kPacked, class S>
+__device__ __forceinline__ void join_runs(const GatedScanParams& p, S& shared, int wave, int lane, const float* A,
+                                          const float* H, bool cut, float* before) {
 #pragma unroll
     for (int v = 0; v < kV; ++v) {
         shared.A[wave][lane * kV + v] = A[v];
@@ -232,56 +324,35 @@ __device__ __forceinline__ void join_runs(const GatedScanParams& p, Shared<kV>& 
     }
     if (kPacked && lane == 0) shared.cut[wave] = cut;
     __syncthreads();
-    float mineA[kV], mineH[kV], allA[kV], allH[kV];
-    bool mine_cut = false, all_cut = false;
+    float beforeA[kV];
 #pragma unroll
-    for (int v = 0; v < kV; ++v) {
-        allA[v] = mineA[v] = 1.0f;
-        allH[v] = mineH[v] = 0.0f;
-    }
+    for (int v = 0; v < kV; ++v) { beforeA[v] = 1.0f; before[v] = 0.0f; }
+    bool cut_before = false;
     const int ahead = kBackward ? p.waves - 1 - wave : wave;  // runs that come before this wave's
-    const int last = wave == 0 ? p.waves : ahead;             // wave 0 goes on to the end: it joins the tile to the others
-    for (int i = 0; i < last; ++i) {
+    for (int i = 0; i < ahead; ++i) {
         const int w = kBackward ? p.waves - 1 - i : i;
-        if (i == ahead) {
-            mine_cut = all_cut;
-#pragma unroll
-            for (int v = 0; v < kV; ++v) { mineA[v] = allA[v]; mineH[v] = allH[v]; }
-        }
         const bool here = kPacked && shared.cut[w];
-        all_cut = all_cut || here;
+        cut_before = cut_before || here;
 #pragma unroll
         for (int v = 0; v < kV; ++v) {
             const float Hw = shared.H[w][lane * kV + v], Aw = shared.A[w][lane * kV + v];
-            allH[v] = here ? Hw : fmaf(Aw, allH[v], Hw);
-            allA[v] *= Aw;
+            before[v] = here ? Hw : fmaf(Aw, before[v], Hw);
+            beforeA[v] *= Aw;
         }
-    }
-    if (wave != 0) {
-        mine_cut = all_cut;
-#pragma unroll
-        for (int v = 0; v < kV; ++v) { mineA[v] = allA[v]; mineH[v] = allH[v]; }
-    } else {
-        float carry[kV];
-        const Board board = Board::of<kV>(p, block, lane);
-        if (k == 0) {
-#pragma unroll
-            for (int v = 0; v < kV; ++v) carry[v] = entering[v];
-        } else {
-            if (live && !all_cut) board.publish_run<kV>(k, allA, allH);
-            if (live && all_cut) board.publish_state<kV>(k, allH);
-            board.state_behind<kV>(k - 1, live, carry);
-        }
-#pragma unroll
-        for (int v = 0; v < kV; ++v) {
-            after[v] = all_cut ? allH[v] : fmaf(allA[v], carry[v], allH[v]);
-            shared.carry[lane * kV + v] = carry[v];
-        }
-        if (live && p.tiles > 1 && (k == 0 || !all_cut)) board.publish_state<kV>(k, after);
     }
     __syncthreads();
 #pragma unroll
-    for (int v = 0; v < kV; ++v) before[v] = mine_cut ? mineH[v] : fmaf(mineA[v], shared.carry[lane * kV + v], mineH[v]);
+    for (int v = 0; v < kV; ++v)
+        before[v] = cut_before ? before[v] : fmaf(beforeA[v], shared.carry[lane * kV + v], before[v]);
+}
+
+// The first channel of a lane.  The last pair of an odd number of channels begins one channel early: that channel is then
+// computed and stored twice, the same both times.  Lanes past the end (false) load what the last pair loads.
+template <int kV>
+__device__ __forceinline__ bool channel_of(const GatedScanParams& p, int column, int lane, uint32_t* c) {
+    const uint32_t at = (uint32_t)(column * 64 + lane) * kV;
+    *c = min(at, (uint32_t)(p.C - kV));
+    return at < (uint32_t)p.C;
 }
 
 // States of empty packed sequences are handed on; the sequences are spread over the tiles and waves.
@@ -296,36 +367,38 @@ __device__ __forceinline__ void pass_on(const GatedScanParams& p, const float* f
         }
 }
 
-// Workgroup = one tile of waves * kScanTokens tokens x 64 kV channels of one batch entry.
+// Workgroup = one tile of waves * kTokens tokens x 64 kV channels of one batch entry.
 template <int kX, int kG, int kMode, int kV, bool kPacked>
-__global__ __launch_bounds__(64 * kScanWaves) void gated_scan_kernel(GatedScanParams p) {
-    __shared__ Shared<kV> shared;
+__global__ __launch_bounds__(64 * (ForwardTile::kWaves + 1)) void gated_scan_kernel(GatedScanParams p) {
+    constexpr int kTokens = ForwardTile::kTokens;
+    __shared__ Shared<kV, ForwardTile::kWaves> shared;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int block, k;
-    take_tile<kV>(p, shared, &block, &k);
+    take_tile(p, shared, &block, &k);
     const int b = block / p.columns;
-    const uint32_t c = (uint32_t)((block - b * p.columns) * 64 + lane) * kV;
-    const bool live = c < (uint32_t)p.C;
-    const int t0 = (k * p.waves + wave) * kScanTokens, count = min(max(p.N - t0, 0), kScanTokens);
+    uint32_t c;
+    const bool live = channel_of<kV>(p, block - b * p.columns, lane, &c);
+    if (wave == p.waves) {
+        link_tile<kV, false, kPacked>(p, shared, block, k, lane, live, p.state_in, p.state_out, b, c);
+        return;
+    }
+    const int t0 = (k * p.waves + wave) * kTokens, count = min(max(p.N - t0, 0), kTokens);
 
-    typename Io<kG>::template Raw<kV> z[kScanTokens];
-    typename Io<kX>::template Raw<kV> x[kScanTokens];
-    const uint32_t cl = min(c, (uint32_t)(p.C - kV));  // lanes and tokens past the end load what is there and drop it
-    if (p.N > 0)
+    typename Io<kG>::template Raw<kV> z[kTokens];
+    typename Io<kX>::template Raw<kV> x[kTokens];
+    if (p.N > 0)  // tokens past the end load what is there and drop it
 #pragma unroll
-        for (int i = 0; i < kScanTokens; ++i) {
+        for (int i = 0; i < kTokens; ++i) {
             const int t = min(t0 + i, p.N - 1);
-            z[i].load(row_at<kG>(p.gate, b, t, cl));
-            x[i].load(row_at<kX>(p.x, b, t, cl));
+            z[i].load(row_at<kG>(p.gate, b, t, c));
+            x[i].load(row_at<kX>(p.x, b, t, c));
         }
-    const Places at = kPacked ? Places(p.offsets, p.sequences, t0, p.N, lane) : Places{};
-    float entering[kV], a[kScanTokens][kV], h[kScanTokens][kV], A[kV], H[kV];
-    if (!kPacked && k == 0 && wave == 0 && live) load_state<kV>(p.state_in, b, p.C, c, entering);
-    else zero<kV>(entering);
+    const Places<kTokens> at = kPacked ? Places<kTokens>(p.offsets, p.sequences, t0, p.N, lane) : Places<kTokens>{};
+    float a[kTokens][kV], h[kTokens][kV], A[kV], H[kV];
 #pragma unroll
     for (int v = 0; v < kV; ++v) { A[v] = 1.0f; H[v] = 0.0f; }
 #pragma unroll
-    for (int i = 0; i < kScanTokens; ++i) {
+    for (int i = 0; i < kTokens; ++i) {
         if (i >= count) continue;
         const bool first = kPacked && (at.first >> i & 1);
         float enters[kV];
@@ -349,10 +422,10 @@ __global__ __launch_bounds__(64 * kScanWaves) void gated_scan_kernel(GatedScanPa
             }
         }
     }
-    float state[kV], after[kV];
-    join_runs<kV, false, kPacked>(p, shared, block, k, wave, lane, live, A, H, kPacked && at.first != 0, entering, state, after);
+    float state[kV];
+    join_runs<kV, false, kPacked>(p, shared, wave, lane, A, H, kPacked && at.first != 0, state);
 #pragma unroll
-    for (int i = 0; i < kScanTokens; ++i) {
+    for (int i = 0; i < kTokens; ++i) {
         if (i >= count) continue;
         const bool first = kPacked && (at.first >> i & 1);
 #pragma unroll
@@ -365,44 +438,44 @@ __global__ __launch_bounds__(64 * kScanWaves) void gated_scan_kernel(GatedScanPa
             if (kPacked && (at.last >> i & 1)) store_state<kV>(p.state_out, at.of(i), p.C, c, h[i]);
         }
     }
-    if (!live) return;
-    if (kPacked) pass_on<kV>(p, p.state_in, p.state_out, k, wave, c);
-    else if (k == p.tiles - 1 && wave == 0) store_state<kV>(p.state_out, b, p.C, c, after);
+    if (kPacked && live) pass_on<kV>(p, p.state_in, p.state_out, k, wave, c);
 }
 
 // The same from the last tile to the first.  The run of a wave maps the gradient that comes in from behind its last
 // token to the one that goes out before its first.
 template <int kX, int kG, int kMode, int kV, bool kPacked>
-__global__ __launch_bounds__(64 * kScanWaves) void gated_scan_backward_kernel(GatedScanParams p) {
-    __shared__ Shared<kV> shared;
+__global__ __launch_bounds__(64 * (BackwardTile::kWaves + 1)) void gated_scan_backward_kernel(GatedScanParams p) {
+    constexpr int kTokens = BackwardTile::kTokens;
+    __shared__ Shared<kV, BackwardTile::kWaves> shared;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int block, k;
-    take_tile<kV>(p, shared, &block, &k);
+    take_tile(p, shared, &block, &k);
     const int b = block / p.columns;
-    const uint32_t c = (uint32_t)((block - b * p.columns) * 64 + lane) * kV;
-    const bool live = c < (uint32_t)p.C;
-    const int t0 = ((p.tiles - 1 - k) * p.waves + wave) * kScanTokens, count = min(max(p.N - t0, 0), kScanTokens);
+    uint32_t c;
+    const bool live = channel_of<kV>(p, block - b * p.columns, lane, &c);
+    if (wave == p.waves) {
+        link_tile<kV, true, kPacked>(p, shared, block, k, lane, live, p.dstate_out, p.dstate_in, b, c);
+        return;
+    }
+    const int t0 = ((p.tiles - 1 - k) * p.waves + wave) * kTokens, count = min(max(p.N - t0, 0), kTokens);
 
-    typename Io<kG>::template Raw<kV> z[kScanTokens];
-    typename Io<kX>::template Raw<kV> dh[kScanTokens], h[kScanTokens], x[kScanTokens];  // h: of the token before
-    const uint32_t cl = min(c, (uint32_t)(p.C - kV));  // lanes and tokens past the end load what is there and drop it
-    if (p.N > 0)
+    typename Io<kG>::template Raw<kV> z[kTokens];
+    typename Io<kX>::template Raw<kV> dh[kTokens], h[kTokens], x[kTokens];  // h: of the token before
+    if (p.N > 0)  // tokens past the end load what is there and drop it
 #pragma unroll
-        for (int i = 0; i < kScanTokens; ++i) {
+        for (int i = 0; i < kTokens; ++i) {
             const int t = min(t0 + i, p.N - 1);
-            z[i].load(row_at<kG>(p.gate, b, t, cl));
-            dh[i].load(row_at<kX>(p.dh, b, t, cl));
-            h[i].load(row_at<kX>(p.h, b, max(t - 1, 0), cl));
-            if (kMode == 2) x[i].load(row_at<kX>(p.x, b, t, cl));
+            z[i].load(row_at<kG>(p.gate, b, t, c));
+            dh[i].load(row_at<kX>(p.dh, b, t, c));
+            h[i].load(row_at<kX>(p.h, b, max(t - 1, 0), c));
+            if (kMode == 2) x[i].load(row_at<kX>(p.x, b, t, c));
         }
-    const Places at = kPacked ? Places(p.offsets, p.sequences, t0, p.N, lane) : Places{};
-    float entering[kV], a[kScanTokens][kV], d[kScanTokens][kV], rest[kScanTokens][kV], A[kV], G[kV];
-    if (!kPacked && k == 0 && wave == 0 && live) load_state<kV>(p.dstate_out, b, p.C, c, entering);
-    else zero<kV>(entering);
+    const Places<kTokens> at = kPacked ? Places<kTokens>(p.offsets, p.sequences, t0, p.N, lane) : Places<kTokens>{};
+    float a[kTokens][kV], d[kTokens][kV], rest[kTokens][kV], A[kV], G[kV];
 #pragma unroll
     for (int v = 0; v < kV; ++v) { A[v] = 1.0f; G[v] = 0.0f; }
 #pragma unroll
-    for (int i = kScanTokens - 1; i >= 0; --i) {
+    for (int i = kTokens - 1; i >= 0; --i) {
         if (i >= count) continue;
         const bool last = kPacked && (at.last >> i & 1);
         float leaves[kV];
@@ -422,10 +495,10 @@ __global__ __launch_bounds__(64 * kScanWaves) void gated_scan_backward_kernel(Ga
             }
         }
     }
-    float g[kV], after[kV];  // g: the gradient that comes in from behind
-    join_runs<kV, true, kPacked>(p, shared, block, k, wave, lane, live, A, G, kPacked && at.last != 0, entering, g, after);
+    float g[kV];  // the gradient that comes in from behind
+    join_runs<kV, true, kPacked>(p, shared, wave, lane, A, G, kPacked && at.last != 0, g);
 #pragma unroll
-    for (int i = kScanTokens - 1; i >= 0; --i) {
+    for (int i = kTokens - 1; i >= 0; --i) {
         if (i >= count || !live || (kPacked && !(at.inside >> i & 1))) continue;
         const bool last = kPacked && (at.last >> i & 1), first = kPacked ? (at.first >> i & 1) : t0 + i == 0;
         float before[kV], xi[kV], dx[kV], dgate[kV];
@@ -444,9 +517,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void gated_scan_backward_kernel(Ga
         store_channels<kG, kV>(p.dgate, b, t0 + i, c, dgate);
         if (kPacked && first) store_state<kV>(p.dstate_in, at.of(i), p.C, c, g);
     }
-    if (!live) return;
-    if (kPacked) pass_on<kV>(p, p.dstate_out, p.dstate_in, k, wave, c);
-    else if (k == p.tiles - 1 && wave == 0) store_state<kV>(p.dstate_in, b, p.C, c, after);
+    if (kPacked && live) pass_on<kV>(p, p.dstate_out, p.dstate_in, k, wave, c);
 }
 
 // One token of every sequence: state <- a state + b, out = state.  One thread per kV channels.
@@ -456,8 +527,8 @@ __global__ __launch_bounds__(256) void gated_step_kernel(GatedScanParams p) {
     if (c >= (uint32_t)p.C) return;
     for (int b = blockIdx.y; b < p.B; b += gridDim.y) {
         float a[kV], x[kV], s[kV];
-        load_channels<kG, kV>(p.gate, b, 0, c, a);
-        load_channels<kX, kV>(p.x, b, 0, c, x);
+        Io<kG>::template load<kV>(row_at<kG>(p.gate, b, 0, c), a);
+        Io<kX>::template load<kV>(row_at<kX>(p.x, b, 0, c), x);
         char* state = reinterpret_cast<char*>(p.state_out + (size_t)b * p.C + c);
         Io<0>::load<kV>(state, s);
 #pragma unroll
@@ -467,14 +538,14 @@ __global__ __launch_bounds__(256) void gated_step_kernel(GatedScanParams p) {
             s[v] = fmaf(a[v], s[v], kMode == 2 ? rest * x[v] : x[v]);
         }
         Io<0>::store<kV>(state, s);
-        store_channels<kX, kV>(p.out, b, 0, c, s);
+        Io<kX>::template store<kV>(p.out.data + (b * p.out.batch + c) * Io<kX>::kBytes, s);
     }
 }
 
 // which: 0 forward, 1 backward
 template <int kX, int kG, int kMode, int kV>
 static void launch_scan_v(const GatedScanParams& p, int which, hipStream_t stream) {
-    const dim3 grid((unsigned)((long long)p.B * p.columns * p.tiles)), block(64 * (unsigned)p.waves);
+    const dim3 grid((unsigned)((long long)p.B * p.columns * p.tiles)), block(64 * (unsigned)(p.waves + 1));
     if (which == 0) {
         if (p.offsets) hipLaunchKernelGGL((gated_scan_kernel<kX, kG, kMode, kV, true>), grid, block, 0, stream, p);
         else hipLaunchKernelGGL((gated_scan_kernel<kX, kG, kMode, kV, false>), grid, block, 0, stream, p);
@@ -492,7 +563,7 @@ static void launch_scan_m(const GatedScanParams& p, int which, hipStream_t strea
         const dim3 grid(blocks, (unsigned)(p.B < 65535 ? p.B : 65535)), block(256);
         if (v >= 4) hipLaunchKernelGGL((gated_step_kernel<kX, kG, kMode, 4>), grid, block, 0, stream, p);
         else hipLaunchKernelGGL((gated_step_kernel<kX, kG, kMode, 1>), grid, block, 0, stream, p);
-    } else if (p.vector >= 2) launch_scan_v<kX, kG, kMode, 2>(p, which, stream);
+    } else if (p.C > 1) launch_scan_v<kX, kG, kMode, 2>(p, which, stream);
     else launch_scan_v<kX, kG, kMode, 1>(p, which, stream);
 }
 
@@ -511,41 +582,33 @@ static hipError_t launch_scan(const GatedScanParams& p, int elem, int gate_elem,
 }
 
 // Column blocks, waves of a workgroup and tiles of N tokens; returns the bytes of workspace.
-static size_t plan_scan(GatedScanParams* p) {
-    const int v = p->vector >= 2 ? 2 : 1;
+static size_t plan_scan(GatedScanParams* p, bool backward) {
+    const int v = p->C > 1 ? 2 : 1;
+    const int tokens = backward ? BackwardTile::kTokens : ForwardTile::kTokens, most = backward ? BackwardTile::kWaves : ForwardTile::kWaves;
     p->columns = (p->C + 64 * v - 1) / (64 * v);
-    const int need = (p->N + kScanTokens - 1) / kScanTokens;
-    p->waves = need < 1 ? 1 : need < kScanWaves ? need : kScanWaves;  // no tokens: one that hands the states on
-    const int tokens = p->waves * kScanTokens;
-    p->tiles = p->N > 0 ? (p->N + tokens - 1) / tokens : 1;
+    const int need = (p->N + tokens - 1) / tokens;
+    p->waves = need < 1 ? 1 : need < most ? need : most;  // no tokens: one that hands the states on
+    p->tiles = need < 1 ? 1 : (need + p->waves - 1) / p->waves;
     if (p->tiles == 1) return 0;
     const size_t lanes = (size_t)p->B * p->columns * 64 * p->tiles;
     return Board::kHeader + lanes * (8 * v + 8);
 }
 
 size_t gated_scan_workspace(int B, int N, int C, bool backward) {
-    // the two channels a lane of aligned rows, or the one of others, whichever needs more
-    size_t most = 0;
-    for (int v = 1; v <= 2; ++v) {
-        GatedScanParams p = {};
-        p.B = B; p.N = N; p.C = C;
-        p.vector = v;
-        const size_t bytes = plan_scan(&p);
-        if (bytes > most) most = bytes;
-    }
-    return most;
+    GatedScanParams p = {};
+    p.B = B; p.N = N; p.C = C;
+    return plan_scan(&p, backward);
 }
 
 long long gated_scan_threads(int B, int N, int C, bool backward) {
     GatedScanParams p = {};
     p.B = B; p.N = N; p.C = C;
-    p.vector = 1;
-    plan_scan(&p);
-    return (long long)p.B * p.columns * p.tiles * p.waves * 64;
+    plan_scan(&p, backward);
+    return (long long)p.B * p.columns * p.tiles * (p.waves + 1) * 64;
 }
 
 static hipError_t launch_sequences(GatedScanParams& p, int elem, int gate_elem, int mode, int which, hipStream_t stream) {
-    const size_t bytes = plan_scan(&p);
+    const size_t bytes = plan_scan(&p, which != 0);
     if (bytes) {
         const size_t words = (bytes + 15) / 16;
         hipLaunchKernelGGL(gated_scan_clear_kernel, dim3((unsigned)((words + 255) / 256)), dim3(256), 0, stream,

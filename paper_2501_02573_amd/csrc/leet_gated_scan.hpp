@@ -25,7 +25,7 @@ struct GatedScanParams {
     const int* offsets;            // [S + 1] or null: S = B sequences of N tokens
     int sequences;                 // S
     int B, N, C;
-    int vector;                    // channels a lane may hold: 1, 2, 4 or 8
+    int vector;                    // step: channels a thread takes, 1 or 4
     int columns;                   // column blocks of a batch entry
     int waves;                     // waves of a workgroup
     int tiles;                     // of a column block's N tokens
@@ -34,7 +34,7 @@ struct GatedScanParams {
 
 // Bytes of workspace for these sizes; 0: none is needed.
 size_t gated_scan_workspace(int B, int N, int C, bool backward);
-// Threads that a launch of these sizes has, whatever the rows' alignment.
+// Threads that a launch of these sizes has.
 long long gated_scan_threads(int B, int N, int C, bool backward);
 
 // elem, gate_elem: 0 = fp32, 1 = bf16, 2 = fp16; gate_elem is elem or 0.  mode: a leet_gate_mode

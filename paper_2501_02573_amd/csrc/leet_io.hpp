@@ -18,22 +18,34 @@ struct Io {
         return kElem == 1 ? ElemBf16::pack2(a, b) : ElemF16::pack2(a, b);
     }
 
-    // One or two adjacent elements as they lie in memory, so that many can be under way before any is looked at.
+    // One or two adjacent elements as they lie in memory, at any address that suits one (the hardware takes words at any
+    // address), so that many can be under way before any is looked at.
     template <int V>
     struct Raw {
         static_assert(V == 1 || V == 2, "one or two elements");
-        using Word = typename std::conditional<kElem == 0, typename std::conditional<V == 1, float, float2>::type,
+        typedef float Pair __attribute__((ext_vector_type(2)));
+        using Word = typename std::conditional<kElem == 0, typename std::conditional<V == 1, float, Pair>::type,
                                                typename std::conditional<V == 1, uint16_t, uint32_t>::type>::type;
+        typedef Word Anywhere __attribute__((aligned(kElem == 0 ? 4 : 2), may_alias));
         Word word;
-        __device__ __forceinline__ void load(const char* p) { word = *reinterpret_cast<const Word*>(p); }
+
+        __device__ __forceinline__ void load(const char* p) { word = *reinterpret_cast<const Anywhere*>(p); }
         __device__ __forceinline__ void get(float* f) const {
             if constexpr (kElem == 0 && V == 1) f[0] = word;
-            else if constexpr (kElem == 0) { f[0] = word.x; f[1] = word.y; }
+            else if constexpr (kElem == 0) { f[0] = word[0]; f[1] = word[1]; }
             else {
                 f[0] = lo(word);
                 if constexpr (V == 2) f[1] = hi(word);
             }
         }
+        __device__ __forceinline__ void set(const float* f) {
+            if constexpr (kElem == 0 && V == 1) word = f[0];
+            else if constexpr (kElem == 0) word = Word{f[0], f[1]};
+            else if constexpr (V == 1) word = (uint16_t)pack2(f[0], 0.0f);
+            else word = pack2(f[0], f[1]);
+        }
+        // with the nontemporal hint: for outputs that the library does not read again
+        __device__ __forceinline__ void store(char* p) const { __builtin_nontemporal_store(word, reinterpret_cast<Anywhere*>(p)); }
     };
 
     // V adjacent elements at p (aligned to all of them, to 16 bytes at most)

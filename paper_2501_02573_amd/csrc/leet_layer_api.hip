@@ -115,19 +115,15 @@ int done(hipError_t e) { return e == hipSuccess ? LEET_OK : LEET_ERR_LAUNCH; }
 
 // ---- gated scan ----
 
-bool rows_ok(const leet_attn_rows* t, int B, int N, int C, size_t size, bool written, int* vector) {
+bool rows_ok(const leet_attn_rows* t, int B, int N, int C, size_t size, bool written) {
     if (!t || !t->data || !aligned(t->data, size)) return false;
     Dim dims[2] = {{B, t->batch}, {N, t->token}};
-    for (; *vector > 1; *vector /= 2) {
-        bool fits = aligned(t->data, *vector * size);
-        for (const Dim& m : dims) fits = fits && (m.size <= 1 || m.stride % *vector == 0);
-        if (fits) break;
-    }
     return !written || rows_apart(C, dims, 2);
 }
-
-// The most channels that a lane may take of C, before the tensors' alignment is looked at.
-int channels_a_lane(int C) { return C % 8 == 0 ? 8 : C % 4 == 0 ? 4 : C % 2 == 0 ? 2 : 1; }
+// Whether rows can be taken four channels at a time.
+bool by_four(const leet_attn_rows* t, int B, size_t size) {
+    return aligned(t->data, 4 * size) && (B <= 1 || t->batch % 4 == 0);
+}
 
 leet::RowsIn rows_in(const leet_attn_rows* t) { return {static_cast<const char*>(t->data), t->batch, t->token}; }
 leet::RowsOut rows_out(const leet_attn_rows* t) { return {static_cast<char*>(t->data), t->batch, t->token}; }
@@ -271,11 +267,10 @@ int leet_attn_gated_scan(const leet_attn_rows *x, const leet_attn_rows *gate, co
     if (status == LEET_OK) status = scan_sizes_ok(offsets, sequences, workspace, workspace_bytes, B, N, C, 0, &S);
     if (status != LEET_OK) return status;
     leet::GatedScanParams p = {};
-    p.vector = channels_a_lane(C);
     if (N > 0) {
-        if (!rows_ok(x, B, N, C, size_of(dtype), false, &p.vector) ||
-            !rows_ok(gate, B, N, C, size_of(gate_dtype), false, &p.vector) ||
-            !rows_ok(out, B, N, C, size_of(dtype), true, &p.vector) || out->data == x->data || out->data == gate->data)
+        if (!rows_ok(x, B, N, C, size_of(dtype), false) ||
+            !rows_ok(gate, B, N, C, size_of(gate_dtype), false) ||
+            !rows_ok(out, B, N, C, size_of(dtype), true) || out->data == x->data || out->data == gate->data)
             return LEET_ERR_INVALID_ARG;
         p.x = rows_in(x);
         p.gate = rows_in(gate);
@@ -304,15 +299,14 @@ int leet_attn_gated_scan_backward(const leet_attn_rows *dh, const leet_attn_rows
     if (status == LEET_OK) status = scan_sizes_ok(offsets, sequences, workspace, workspace_bytes, B, N, C, 1, &S);
     if (status != LEET_OK) return status;
     leet::GatedScanParams p = {};
-    p.vector = channels_a_lane(C);
     if (N > 0) {
         const size_t size = size_of(dtype), gate_size = size_of(gate_dtype);
-        if (!rows_ok(dh, B, N, C, size, false, &p.vector) || !rows_ok(gate, B, N, C, gate_size, false, &p.vector) ||
-            !rows_ok(h, B, N, C, size, false, &p.vector) || !rows_ok(dx, B, N, C, size, true, &p.vector) ||
-            !rows_ok(dgate, B, N, C, gate_size, true, &p.vector))
+        if (!rows_ok(dh, B, N, C, size, false) || !rows_ok(gate, B, N, C, gate_size, false) ||
+            !rows_ok(h, B, N, C, size, false) || !rows_ok(dx, B, N, C, size, true) ||
+            !rows_ok(dgate, B, N, C, gate_size, true))
             return LEET_ERR_INVALID_ARG;
         if (mode == LEET_GATE_SIGMOID) {
-            if (!rows_ok(x, B, N, C, size, false, &p.vector)) return LEET_ERR_INVALID_ARG;
+            if (!rows_ok(x, B, N, C, size, false)) return LEET_ERR_INVALID_ARG;
             p.x = rows_in(x);
         }
         for (const leet_attn_rows* o : {dx, dgate})
@@ -348,10 +342,11 @@ int leet_attn_gated_scan_step(const leet_attn_rows *x, const leet_attn_rows *gat
     if (B <= 0 || C <= 0 || !state || !aligned(state, 4)) return LEET_ERR_INVALID_ARG;
     if (C > 1 << 28) return LEET_ERR_TOO_LARGE;
     leet::GatedScanParams p = {};
-    p.vector = aligned(state, 16) ? channels_a_lane(C) : 1;
-    if (!rows_ok(x, B, 1, C, size_of(dtype), false, &p.vector) || !rows_ok(gate, B, 1, C, size_of(gate_dtype), false, &p.vector) ||
-        !rows_ok(out, B, 1, C, size_of(dtype), true, &p.vector))
+    if (!rows_ok(x, B, 1, C, size_of(dtype), false) || !rows_ok(gate, B, 1, C, size_of(gate_dtype), false) ||
+        !rows_ok(out, B, 1, C, size_of(dtype), true))
         return LEET_ERR_INVALID_ARG;
+    p.vector = C % 4 == 0 && aligned(state, 16) && by_four(x, B, size_of(dtype)) && by_four(gate, B, size_of(gate_dtype)) &&
+                       by_four(out, B, size_of(dtype)) ? 4 : 1;
     p.x = rows_in(x);
     p.gate = rows_in(gate);
     p.out = rows_out(out);

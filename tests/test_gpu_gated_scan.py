@@ -297,3 +297,49 @@ def test_on_another_stream_and_in_a_graph(leet):
         eager = both()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(eager, seen))
+
+
+@pytest.mark.parametrize("packed", [False, True])
+def test_equal_from_call_to_call(leet, packed):
+    """Which tiles have published what when another looks back is a matter of timing; results are not."""
+    N, C = 20000, 320
+    x, z, dh = _normal((1, N, C), F32, 120), _gate((1, N, C), F32, 1, 121), _normal((1, N, C), F32, 122)
+    off = _offsets([9000, 5, 0, 10000, 995]).cuda() if packed else None
+    s = _normal((5 if packed else 1, C), F32, 123)
+
+    def both():
+        left, din = torch.empty_like(s), torch.empty_like(s)
+        h = leet.leet_attn_gated_scan(x, z, state_in=s, state_out=left, offsets=off)
+        return (h, left, din) + leet.leet_attn_gated_scan_backward(dh, None, z, h, state_in=s, dstate_out=s, dstate_in=din,
+                                                                   offsets=off)
+
+    want = both()
+    for _ in range(10):
+        assert all(torch.equal(a, b) for a, b in zip(want, both()))
+
+
+def test_two_streams_at_once(leet):
+    """Calls that overlap share nothing: every one has a workspace of its own."""
+    x, z = _normal((2, 8000, 512), BF16, 130), _gate((2, 8000, 512), BF16, 1, 131)
+    want = leet.leet_attn_gated_scan(x, z)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    got = []
+    for _ in range(4):
+        for st in streams:
+            with torch.cuda.stream(st):
+                got.append(leet.leet_attn_gated_scan(x, z))
+    torch.cuda.synchronize()
+    assert all(torch.equal(want, h) for h in got)
+
+
+def test_workspace_of_the_callers(leet):
+    x, z = _normal((1, 5000, 130), BF16, 140), _gate((1, 5000, 130), BF16, 1, 141)
+    need = leet.gated_scan_workspace_bytes(1, 5000, 130)
+    assert need > 0 and leet.gated_scan_workspace_bytes(1, 1, 130) == 0
+    ws = torch.full((need,), 255, dtype=torch.uint8, device="cuda")
+    want = leet.leet_attn_gated_scan(x, z)
+    for _ in range(3):
+        assert torch.equal(want, leet.leet_attn_gated_scan(x, z, workspace=ws))
+    with pytest.raises(leet.LeetAttnError):
+        leet.leet_attn_gated_scan(x, z, workspace=ws[:need - 256])
