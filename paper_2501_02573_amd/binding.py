@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional
 
 import torch
@@ -75,22 +76,11 @@ class LeetAttnError(RuntimeError):
         super().__init__(f"{where}: status {status}: {strerror(status)}")
 
 
-class _Heads(ctypes.Structure):
-    """leet_attn_heads"""
-    _fields_ = [("data", ctypes.c_void_p), ("batch", ctypes.c_longlong), ("head", ctypes.c_longlong),
-                ("token", ctypes.c_longlong)]
-
-
-class _Rotation(ctypes.Structure):
-    """leet_attn_rotation"""
-    _fields_ = [("freq", ctypes.c_void_p), ("rot", ctypes.c_int), ("layout", ctypes.c_int),
-                ("positions", ctypes.c_void_p), ("positions_batch", ctypes.c_longlong), ("pos0", ctypes.c_longlong),
-                ("scale", ctypes.c_float)]
-
-
-class _Rows(ctypes.Structure):
-    """leet_attn_rows"""
-    _fields_ = [("data", ctypes.c_void_p), ("batch", ctypes.c_longlong), ("token", ctypes.c_longlong)]
+# The library's small argument structures, packed: a tenth of a ctypes.Structure's time, and a call takes up to seven.
+# A call passes the bytes where the library takes a pointer to the structure.
+_pack_heads = struct.Struct("@P3q").pack      # leet_attn_heads: data, batch, head, token
+_pack_rows = struct.Struct("@P2q").pack       # leet_attn_rows: data, batch, token
+_pack_rotation = struct.Struct("@PiiPqqf4x").pack  # leet_attn_rotation
 
 
 def _load() -> ctypes.CDLL:
@@ -157,7 +147,7 @@ def _load() -> ctypes.CDLL:
     lib.leet_attn_set_decode_store.restype = i
     lib.leet_attn_get_decode_store.argtypes = []
     lib.leet_attn_get_decode_store.restype = i
-    heads, rotation, rows = ctypes.POINTER(_Heads), ctypes.POINTER(_Rotation), ctypes.POINTER(_Rows)
+    heads = rotation = rows = vp  # packed structures
     d = ctypes.c_double
     lib.leet_attn_rope_frequencies.argtypes = [i, d, i, d, i, d, d, vp, ctypes.POINTER(ctypes.c_float)]
     lib.leet_attn_rope_frequencies.restype = i
@@ -711,22 +701,31 @@ def leet_attn_decode_step_rd(q, k, v, gamma: Optional[torch.Tensor], state, out:
 # bring are dense.  A workspace that the caller does not bring comes from torch's allocator, on the current stream: it
 # belongs to this call alone, also while a graph is captured.
 
-def _on(*tensors: Optional[torch.Tensor]) -> torch.device:
-    """The one device of all tensors that are there."""
-    dev = None
+def _on(*tensors: Optional[torch.Tensor]) -> int:
+    """Index of the one device of all tensors that are there."""
+    index = None
     for t in tensors:
         if t is None:
             continue
-        if not t.is_cuda:
+        at = t.get_device()
+        if at < 0 or not t.is_cuda:
             raise ValueError("all tensors must be GPU tensors")
-        if dev is None:
-            dev = t.device
-        elif t.device != dev:
+        if index is None:
+            index = at
+        elif at != index:
             raise ValueError("all tensors must be on one device")
-    return dev
+    return index
 
 
-def _heads_view(t: torch.Tensor, name: str, shape, dtype: torch.dtype) -> _Heads:
+def _call_on(index: int, fn, *args) -> int:
+    """fn(*args, the current stream of device ``index``) with that device current; returns the status."""
+    if index == torch.cuda.current_device():
+        return fn(*args, _raw_stream(index))
+    with torch.cuda.device(index):
+        return fn(*args, _raw_stream(index))
+
+
+def _heads_view(t: torch.Tensor, name: str, shape, dtype: torch.dtype) -> bytes:
     """``t`` as a leet_attn_heads; ``shape`` [B, H, N, d] and ``dtype`` are what it has to have."""
     if t.shape != shape:
         raise ValueError(f"{name} must have the shape {list(shape)}")
@@ -735,10 +734,10 @@ def _heads_view(t: torch.Tensor, name: str, shape, dtype: torch.dtype) -> _Heads
     b, h, n, e = t.stride()
     if e != 1 and t.shape[3] > 1:
         raise ValueError(f"{name}: the elements of a head row must be adjacent")
-    return _Heads(t.data_ptr(), b, h, n)
+    return _pack_heads(t.data_ptr(), b, h, n)
 
 
-def _rows_view(t: torch.Tensor, name: str, shape, dtype: torch.dtype) -> _Rows:
+def _rows_view(t: torch.Tensor, name: str, shape, dtype: torch.dtype) -> bytes:
     """``t`` as a leet_attn_rows; ``shape`` [B, N, C] or [B, C] and ``dtype`` are what it has to have."""
     if t.shape != shape:
         raise ValueError(f"{name} must have the shape {list(shape)}")
@@ -747,15 +746,15 @@ def _rows_view(t: torch.Tensor, name: str, shape, dtype: torch.dtype) -> _Rows:
     strides = t.stride()
     if strides[-1] != 1 and t.shape[-1] > 1:
         raise ValueError(f"{name}: the channels of a row must be adjacent")
-    return _Rows(t.data_ptr(), strides[0], strides[1] if len(strides) == 3 else 0)
+    return _pack_rows(t.data_ptr(), strides[0], strides[1] if len(strides) == 3 else 0)
 
 
-def _scratch(nbytes: int, workspace: Optional[torch.Tensor], dev: torch.device):
+def _scratch(nbytes: int, workspace: Optional[torch.Tensor], index: int):
     """(pointer, bytes, tensor to keep until the launch) of a call's workspace."""
     if workspace is None:
         if not nbytes:
             return None, 0, None
-        workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=torch.device("cuda", index))
     elif workspace.dtype != torch.uint8 or not workspace.is_contiguous():
         raise TypeError("workspace must be a contiguous uint8 tensor")
     return workspace.data_ptr(), workspace.numel(), workspace
@@ -776,17 +775,17 @@ def rope_frequencies(rot: int, base: float = 10000.0, scaling: int = ROPE_SCALIN
 
 
 def _rotation(freq: torch.Tensor, layout: int, positions: Optional[torch.Tensor], pos0: int, scale: float, B: int,
-              N: int) -> _Rotation:
+              N: int) -> bytes:
     if freq.dtype != torch.float64 or freq.dim() != 1 or not freq.is_contiguous():
         raise ValueError("freq must be a contiguous float64 tensor [rot / 2]")
-    at, stride = None, 0
+    at = stride = 0
     if positions is not None:
         if positions.dtype != torch.int64 or positions.shape not in ((N,), (B, N)):
             raise ValueError("positions must be int64 [N] or [B, N]")
         if N > 1 and positions.stride(-1) != 1:
             raise ValueError("positions of a sequence must be adjacent")
         at, stride = positions.data_ptr(), positions.stride(0) if positions.dim() == 2 else 0
-    return _Rotation(freq.data_ptr(), 2 * freq.shape[0], layout, at, stride, pos0, scale)
+    return _pack_rotation(freq.data_ptr(), 2 * freq.shape[0], layout, at, stride, pos0, scale)
 
 
 def _heads_pair(q: torch.Tensor, k: Optional[torch.Tensor]):
@@ -829,7 +828,7 @@ def leet_attn_rope(q: torch.Tensor, freq: torch.Tensor, k: Optional[torch.Tensor
     vk = ok = None
     if k is not None:
         vk, ok = _heads_view(k, "k", k.shape, q.dtype), _heads_view(out_k, "out_k", k.shape, q.dtype)
-    st = _call(lib.leet_attn_rope, dev, _heads_view(q, "q", q.shape, q.dtype), _heads_view(out_q, "out_q", q.shape, q.dtype),
+    st = _call_on(dev, lib.leet_attn_rope, _heads_view(q, "q", q.shape, q.dtype), _heads_view(out_q, "out_q", q.shape, q.dtype),
                Hq, vk, ok, Hk, _rotation(freq, layout, positions, pos0, scale, B, N), B, N, d, _dtype_code(q),
                1 if transposed else 0)
     if st != LEET_OK:
@@ -867,7 +866,7 @@ def leet_attn_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, q_weight: Optional[
     if out_k is None:
         out_k = _new_dense(k)
     dev = _on(q, k, out_q, out_k, q_weight, k_weight, freq, positions)
-    st = _call(lib.leet_attn_qk_norm_rope, dev, _heads_view(q, "q", q.shape, q.dtype),
+    st = _call_on(dev, lib.leet_attn_qk_norm_rope, _heads_view(q, "q", q.shape, q.dtype),
                _heads_view(out_q, "out_q", q.shape, q.dtype), Hq, _heads_view(k, "k", k.shape, q.dtype),
                _heads_view(out_k, "out_k", k.shape, q.dtype), Hk, _ptr(q_weight), _ptr(k_weight), weight_dtype, eps,
                _rotation(freq, layout, positions, pos0, scale, B, N), B, N, d, _dtype_code(q))
@@ -912,7 +911,7 @@ def leet_attn_qk_norm_rope_backward(dout_q: torch.Tensor, dout_k: torch.Tensor, 
         need = qk_norm_rope_workspace_bytes(B, Hq, Hk, N, d)
     ws, ws_bytes, keep = _scratch(need, workspace, dev)
     t = q.dtype
-    st = _call(lib.leet_attn_qk_norm_rope_backward, dev, _heads_view(dout_q, "dout_q", q.shape, t),
+    st = _call_on(dev, lib.leet_attn_qk_norm_rope_backward, _heads_view(dout_q, "dout_q", q.shape, t),
                _heads_view(q, "q", q.shape, t), _heads_view(dx_q, "dx_q", q.shape, t), Hq,
                _heads_view(dout_k, "dout_k", k.shape, t), _heads_view(k, "k", k.shape, t),
                _heads_view(dx_k, "dx_k", k.shape, t), Hk, _ptr(q_weight), _ptr(k_weight), _ptr(dq_weight),
@@ -968,7 +967,7 @@ def leet_attn_gated_scan(x: torch.Tensor, gate: torch.Tensor, mode: int = GATE_L
     t = x.dtype
     need = gated_scan_workspace_bytes(B, N, C) if workspace is None else 0
     ws, ws_bytes, keep = _scratch(need, workspace, dev)
-    st = _call(lib.leet_attn_gated_scan, dev, _rows_view(x, "x", x.shape, t), _rows_view(gate, "gate", x.shape, gate.dtype),
+    st = _call_on(dev, lib.leet_attn_gated_scan, _rows_view(x, "x", x.shape, t), _rows_view(gate, "gate", x.shape, gate.dtype),
                _rows_view(out, "out", x.shape, t), _ptr(state_in), _ptr(state_out), _ptr(offsets), S, ws, ws_bytes,
                B, N, C, _dtype_code(x), _gate_code(gate, t), mode)
     if st != LEET_OK:
@@ -998,7 +997,7 @@ def leet_attn_gated_scan_backward(dh: torch.Tensor, x: Optional[torch.Tensor], g
     t, g = h.dtype, gate.dtype
     need = gated_scan_workspace_bytes(B, N, C, True) if workspace is None else 0
     ws, ws_bytes, keep = _scratch(need, workspace, dev)
-    st = _call(lib.leet_attn_gated_scan_backward, dev, _rows_view(dh, "dh", h.shape, t),
+    st = _call_on(dev, lib.leet_attn_gated_scan_backward, _rows_view(dh, "dh", h.shape, t),
                None if x is None else _rows_view(x, "x", h.shape, t), _rows_view(gate, "gate", h.shape, g),
                _rows_view(h, "h", h.shape, t), _rows_view(dx, "dx", h.shape, t), _rows_view(dgate, "dgate", h.shape, g),
                _ptr(state_in), _ptr(dstate_out), _ptr(dstate_in), _ptr(offsets), S, ws, ws_bytes, B, N, C,
@@ -1018,7 +1017,7 @@ def leet_attn_gated_scan_step(x: torch.Tensor, gate: torch.Tensor, state: torch.
     if out is None:
         out = _new_dense(x)
     dev = _on(x, gate, out, state)
-    st = _call(lib.leet_attn_gated_scan_step, dev, _rows_view(x, "x", x.shape, x.dtype),
+    st = _call_on(dev, lib.leet_attn_gated_scan_step, _rows_view(x, "x", x.shape, x.dtype),
                _rows_view(gate, "gate", x.shape, gate.dtype), _rows_view(out, "out", x.shape, x.dtype), _ptr(state), B, C,
                _dtype_code(x), _gate_code(gate, x.dtype), mode)
     if st != LEET_OK:

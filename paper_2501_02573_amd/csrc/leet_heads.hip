@@ -21,8 +21,12 @@
 
 namespace leet {
 
+// Pieces of four elements: eight bytes of a 16-bit type.  us with pieces of four and of eight (registers: backward 94 and
+// 128 with spills, forward 48 and 75): backward B4 N4096 H16+16 d128 bf16 81 and 107, forward 57 and 64.
+constexpr int kPiece = 4, kPieceLog = 3;  // a row of 64 elements has 2^kPieceLog lanes
 constexpr int kHeadsWaves = 4;  // waves of a workgroup
-constexpr double kInvTwoPi = 0.15915494309189533576888;
+constexpr int kBackwardResident = 5;  // workgroups of the backward kernel on a compute unit
+constexpr int kComputeUnits = 256;
 
 // Sum over the 2^kLog neighbouring lanes that hold a row; every one of them gets it, with the same bits.
 template <int kCtrl>
@@ -40,99 +44,164 @@ __device__ __forceinline__ float row_sum(float v) {
     return v;
 }
 
-// What a lane holds of a row: kK chunks of 2 kV elements, chunk k = elements first(k) .. + kV-1 and second(k) .. + kV-1.
+// What a lane holds of a row: kK chunks of two pieces of kV elements, chunk k = elements first(k) .. + kV-1 and second(k)
+// .. + kV-1.  The lanes' first pieces lie beside one another, and so do their second ones: an access of a wave is whole
+// lines, not every other 16 bytes of them.
 template <int kV, int kK, int kLog, bool kInter>
 struct RowLane {
     int first[kK], second[kK];
     bool valid[kK];
-    int turned[kK];  // pairs of the chunk that are rotated (with the half layout all or none)
+    // Pairs that are rotated: of the half layout's kV pairs (a[j], b[j]) all or none; of the interleaved one's kV / 2 pairs
+    // in each piece so many (one pair (a, b) where a piece is one element).
+    int turned[kK], turned_b[kK];
 
     __device__ __forceinline__ RowLane(int lane, int d, int rot) {
 #pragma unroll
         for (int k = 0; k < kK; ++k) {
-            const int c = (lane & ((1 << kLog) - 1)) + (k << kLog);
+            int c = (lane & ((1 << kLog) - 1)) + (k << kLog);
             valid[k] = c * 2 * kV < d;
-            if (kInter) {
-                first[k] = 2 * kV * c;
-                second[k] = first[k] + kV;
-                turned[k] = min(max(rot / 2 - kV * c, 0), kV);
+            c = valid[k] ? c : 0;  // loads what is there, and drops it
+            if (kInter && kV > 1) {
+                first[k] = kV * c;
+                second[k] = d / 2 + kV * c;
+                turned[k] = min(max((rot - first[k]) / 2, 0), kV / 2);
+                turned_b[k] = min(max((rot - second[k]) / 2, 0), kV / 2);
+            } else if (kInter) {
+                first[k] = 2 * c;
+                second[k] = 2 * c + 1;
+                turned[k] = turned_b[k] = 2 * c < rot;
             } else {
                 const bool in = c * 2 * kV < rot;
-                first[k] = in ? kV * c : 2 * kV * c;
-                second[k] = in ? rot / 2 + kV * c : 2 * kV * c + kV;
-                turned[k] = in ? kV : 0;
+                const int base = in ? 0 : rot, half = (in ? rot : d - rot) / 2;
+                first[k] = base + kV * (in ? c : c - rot / (2 * kV));
+                second[k] = first[k] + half;
+                turned[k] = turned_b[k] = in ? kV : 0;
             }
         }
     }
 };
 
-// Cosines and sines (times the scale) of a lane's pairs at a position.  The angle in turns is a product in fp64; its
-// distance to the nearest quarter turn is at most an eighth and goes on in fp32, where it is off by 2^-28 of a turn at
-// most, so a cosine is off by little more than its own rounding however far out the position is.
+// Sine and cosine of x in [-pi/4, pi/4] by their power series; what is left out is under 2^-28 of the sine and 2^-32.
+__device__ __forceinline__ void sine_cosine(float x, float* s, float* c) {
+    const float y = x * x;
+    *s = x * fmaf(y, fmaf(y, fmaf(y, fmaf(y, 1.0f / 362880, -1.0f / 5040), 1.0f / 120), -1.0f / 6), 1.0f);
+    *c = fmaf(y, fmaf(y, fmaf(y, fmaf(y, fmaf(y, -1.0f / 3628800, 1.0f / 40320), -1.0f / 720), 1.0f / 24), -0.5f), 1.0f);
+}
+
+// Cosines and sines (times the scale) of a lane's pairs at a position.  The angle in quarter turns is a product in fp64;
+// its distance to the nearest whole one goes on in fp32, where it is off by 2^-25 of a quarter turn at most, so a cosine
+// is off by little more than its own rounding however far out the position is.
 template <int kV, int kK, int kLog, bool kInter>
 __device__ __forceinline__ void angles(const RowLane<kV, kK, kLog, kInter>& row, const HeadsParams& p, double position,
                                        float (*cs)[kV], float (*sn)[kV]) {
+    const double quarter_position = position * (2.0 / 3.14159265358979323846);
+    const float sin_scale = p.transposed ? -p.scale : p.scale;
 #pragma unroll
     for (int k = 0; k < kK; ++k)
 #pragma unroll
         for (int j = 0; j < kV; ++j) {
-            cs[k][j] = 1.0f;
-            sn[k][j] = 0.0f;
-            if (j < row.turned[k]) {
-                const int pair = kInter ? row.first[k] / 2 + j : row.first[k] + j;
-                const double quarters = position * (p.freq[pair] * (4.0 * kInvTwoPi));
-                const double whole = rint(quarters);
-                const int quadrant = (int)(long long)whole & 3;
-                float s, c;
-                sincospif(0.5f * (float)(quarters - whole), &s, &c);
-                const float c1 = (quadrant & 1) ? s : c, s1 = (quadrant & 1) ? c : s;
-                cs[k][j] = (quadrant == 1 || quadrant == 2 ? -c1 : c1) * p.scale;
-                const float sv = (quadrant >= 2 ? -s1 : s1) * p.scale;
-                sn[k][j] = p.transposed ? -sv : sv;
-            }
+            const bool in_b = kInter && kV > 1 && j >= kV / 2;
+            const bool in = in_b ? j - kV / 2 < row.turned_b[k] : j < row.turned[k];
+            const int pair = !kInter ? row.first[k] + j : in_b ? row.second[k] / 2 + j - kV / 2 : row.first[k] / 2 + j;
+            const double quarters = quarter_position * p.freq[in ? pair : 0];
+            const double whole = rint(quarters);
+            float s, c;
+            sine_cosine((float)(quarters - whole) * 1.57079632679489661923f, &s, &c);
+            // of the four quadrants only the last two bits count; a product beyond 2^31 keeps them
+            const int quadrant = (int)(long long)whole;
+            const float c1 = (quadrant & 1) ? s : c, s1 = (quadrant & 1) ? c : s;
+            cs[k][j] = ((quadrant + 1) & 2 ? -c1 : c1) * p.scale;
+            sn[k][j] = (quadrant & 2 ? -s1 : s1) * sin_scale;
         }
 }
 
 // Rotates the pairs of one chunk in place.  With the half layout a pair is (a[j], b[j]), with the interleaved one two
 // neighbours of a, then of b.  Elements that are not rotated keep their value, whatever their neighbour holds.
 template <int kV, bool kInter>
-__device__ __forceinline__ void rotate(float* a, float* b, const float* cs, const float* sn, int turned, float sign) {
+__device__ __forceinline__ void rotate(float* a, float* b, const float* cs, const float* sn, int turned, int turned_b,
+                                       float sign) {
 #pragma unroll
     for (int j = 0; j < kV; ++j) {
         float* x1 = kInter ? (2 * j < kV ? a + 2 * j : b + 2 * j - kV) : a + j;
         float* x2 = kInter ? (2 * j + 1 < kV ? a + 2 * j + 1 : b + 2 * j + 1 - kV) : b + j;
         const float s = sign * sn[j];
         const float y1 = *x1 * cs[j] - *x2 * s, y2 = *x2 * cs[j] + *x1 * s;
-        *x1 = j < turned ? y1 : *x1;
-        *x2 = j < turned ? y2 : *x2;
+        const bool in = kInter && kV > 1 && j >= kV / 2 ? j - kV / 2 < turned_b : j < turned;
+        *x1 = in ? y1 : *x1;
+        *x2 = in ? y2 : *x2;
     }
 }
 
-template <int kElem, int kV, int kK>
-__device__ __forceinline__ void load_row(const char* base, const int* first, const int* second, const bool* valid,
-                                         bool live, float (*a)[kV], float (*b)[kV]) {
+// A lane's part of a row as it lies in memory (at any address that suits an element: the hardware takes words anywhere).
+// Loaded one head ahead, looked at when its turn comes.  kStream: with the nontemporal hint.
+template <int kElem, int kV, int kK, bool kStream>
+struct RawRow {
+    static constexpr int kBytes = kV * Io<kElem>::kBytes;  // of a piece
+    using Word = typename std::conditional<kBytes == 16, u32x4, typename std::conditional<kBytes == 8, u32x2,
+                 typename std::conditional<kBytes == 4, uint32_t, uint16_t>::type>::type>::type;
+    typedef Word Anywhere __attribute__((aligned(Io<kElem>::kBytes), may_alias));
+    static_assert(sizeof(Word) == kBytes, "a piece is a word");
+    Word a[kK], b[kK];
+
+    static __device__ __forceinline__ Word fetch(const char* p) {
+        const Anywhere* q = reinterpret_cast<const Anywhere*>(p);
+        return kStream ? __builtin_nontemporal_load(q) : *q;
+    }
+    static __device__ __forceinline__ void put(char* p, Word w) {
+        Anywhere* q = reinterpret_cast<Anywhere*>(p);
+        if (kStream) __builtin_nontemporal_store(w, q);
+        else *q = w;
+    }
+    __device__ __forceinline__ void load(const char* base, const int* first, const int* second) {
 #pragma unroll
-    for (int k = 0; k < kK; ++k) {
-        if (live && valid[k]) {
-            Io<kElem>::template load<kV>(base + (long long)first[k] * Io<kElem>::kBytes, a[k]);
-            Io<kElem>::template load<kV>(base + (long long)second[k] * Io<kElem>::kBytes, b[k]);
-        } else {
-#pragma unroll
-            for (int j = 0; j < kV; ++j) a[k][j] = b[k][j] = 0.0f;
+        for (int k = 0; k < kK; ++k) {
+            a[k] = fetch(base + first[k] * Io<kElem>::kBytes);
+            b[k] = fetch(base + second[k] * Io<kElem>::kBytes);
         }
     }
-}
-
-template <int kElem, int kV, int kK>
-__device__ __forceinline__ void store_row(char* base, const int* first, const int* second, const bool* valid, bool live,
-                                          const float (*a)[kV], const float (*b)[kV]) {
+    static __device__ __forceinline__ void widen(Word w, float* f) {
+        if constexpr (kElem == 0 && kV == 1) f[0] = __builtin_bit_cast(float, w);
+        else if constexpr (kV == 1) f[0] = Io<kElem>::lo(w);
+        else if constexpr (kElem == 0)
 #pragma unroll
-    for (int k = 0; k < kK; ++k)
-        if (live && valid[k]) {
-            Io<kElem>::template store<kV>(base + (long long)first[k] * Io<kElem>::kBytes, a[k]);
-            Io<kElem>::template store<kV>(base + (long long)second[k] * Io<kElem>::kBytes, b[k]);
+            for (int j = 0; j < kV; ++j) f[j] = __builtin_bit_cast(float, (uint32_t)w[j]);
+        else
+#pragma unroll
+            for (int j = 0; j < kV / 2; ++j) {
+                f[2 * j] = Io<kElem>::lo(w[j]);
+                f[2 * j + 1] = Io<kElem>::hi(w[j]);
+            }
+    }
+    static __device__ __forceinline__ Word narrow(const float* f) {
+        if constexpr (kElem == 0 && kV == 1) return __builtin_bit_cast(uint32_t, f[0]);
+        else if constexpr (kV == 1) return (uint16_t)Io<kElem>::pack2(f[0], 0.0f);
+        else if constexpr (kElem == 0) return __builtin_bit_cast(u32x4, f32x4{f[0], f[1], f[2], f[3]});
+        else return u32x2{Io<kElem>::pack2(f[0], f[1]), Io<kElem>::pack2(f[2], f[3])};
+    }
+    // zeros where the lane has no part of the row, or there is no row
+    __device__ __forceinline__ void get(const bool* valid, bool live, float (*fa)[kV], float (*fb)[kV]) const {
+#pragma unroll
+        for (int k = 0; k < kK; ++k) {
+            widen(a[k], fa[k]);
+            widen(b[k], fb[k]);
+            const bool there = live && valid[k];
+#pragma unroll
+            for (int j = 0; j < kV; ++j) {
+                fa[k][j] = there ? fa[k][j] : 0.0f;
+                fb[k][j] = there ? fb[k][j] : 0.0f;
+            }
         }
-}
+    }
+    static __device__ __forceinline__ void store(char* base, const int* first, const int* second, const bool* valid, bool live,
+                                                 const float (*fa)[kV], const float (*fb)[kV]) {
+#pragma unroll
+        for (int k = 0; k < kK; ++k)
+            if (live && valid[k]) {
+                put(base + first[k] * Io<kElem>::kBytes, narrow(fa[k]));
+                put(base + second[k] * Io<kElem>::kBytes, narrow(fb[k]));
+            }
+    }
+};
 
 // A lane's elements of a weight; ones where there is none.
 template <int kElem, int kV, int kK>
@@ -161,7 +230,7 @@ __device__ __forceinline__ double position_of(const HeadsParams& p, int b, int n
 }
 
 // Forward.  Workgroup = 4 waves; wave w takes 64 / L tokens and heads_per_wave heads of the queries or of the keys.
-template <int kElem, int kV, int kK, int kLog, bool kNorm, bool kInter>
+template <int kElem, int kV, int kK, int kLog, bool kNorm, bool kInter, bool kStream>
 __global__ __launch_bounds__(64 * kHeadsWaves) void heads_kernel(HeadsParams p) {
     constexpr int kTokens = 64 >> kLog;
     const int lane = threadIdx.x & 63;
@@ -182,12 +251,15 @@ __global__ __launch_bounds__(64 * kHeadsWaves) void heads_kernel(HeadsParams p) 
 
     float wa[kK][kV], wb[kK][kV];
     if (kNorm) load_weight<kElem, kV, kK>(t.weight, p.weight_f32, row.first, row.second, row.valid, wa, wb);
+    using Raw = RawRow<kElem, kV, kK, kStream>;
+    Raw ahead;
+    ahead.load(in + h0 * t.in_h * Io<kElem>::kBytes, row.first, row.second);
     float cs[kK][kV], sn[kK][kV];
     angles(row, p, position_of(p, b, n), cs, sn);
-
     for (int h = h0; h < h1; ++h) {
         float xa[kK][kV], xb[kK][kV];
-        load_row<kElem, kV, kK>(in + h * t.in_h * Io<kElem>::kBytes, row.first, row.second, row.valid, live, xa, xb);
+        ahead.get(row.valid, live, xa, xb);
+        if (h + 1 < h1) ahead.load(in + (h + 1) * t.in_h * Io<kElem>::kBytes, row.first, row.second);
         if (kNorm) {
             float sum = 0.0f;
 #pragma unroll
@@ -204,16 +276,17 @@ __global__ __launch_bounds__(64 * kHeadsWaves) void heads_kernel(HeadsParams p) 
                 }
         }
 #pragma unroll
-        for (int k = 0; k < kK; ++k) rotate<kV, kInter>(xa[k], xb[k], cs[k], sn[k], row.turned[k], 1.0f);
-        store_row<kElem, kV, kK>(out + h * t.out_h * Io<kElem>::kBytes, row.first, row.second, row.valid, live, xa, xb);
+        for (int k = 0; k < kK; ++k) rotate<kV, kInter>(xa[k], xb[k], cs[k], sn[k], row.turned[k], row.turned_b[k], 1.0f);
+        Raw::store(out + h * t.out_h * Io<kElem>::kBytes, row.first, row.second, row.valid, live, xa, xb);
     }
 }
 
 // Backward.  All waves of a workgroup take the same heads (a unit); workgroup g of a unit takes token groups g, g +
 // groups, ...  The lanes' sums for the weight gradient are joined over the wave's rows, then over the waves, and go to
 // one row of `partial`; heads_weight_kernel adds the rows up in order.
-template <int kElem, int kV, int kK, int kLog, bool kInter>
-__global__ __launch_bounds__(64 * kHeadsWaves) void heads_backward_kernel(HeadsParams p) {
+// Five workgroups a compute unit fit in 102 registers a lane: plan_heads launches so many.
+template <int kElem, int kV, int kK, int kLog, bool kInter, bool kStream>
+__global__ __launch_bounds__(64 * kHeadsWaves, kBackwardResident) void heads_backward_kernel(HeadsParams p) {
     constexpr int kTokens = 64 >> kLog;
     __shared__ float joined[kHeadsWaves][kK][2 * kV][1 << kLog];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -221,6 +294,7 @@ __global__ __launch_bounds__(64 * kHeadsWaves) void heads_backward_kernel(HeadsP
     const bool keys = unit >= p.units_q;
     const HeadRows t = keys ? p.k : p.q;
     const int h0 = (unit - (keys ? p.units_q : 0)) * p.heads_per_wave, h1 = min(h0 + p.heads_per_wave, t.H);
+    using Raw = RawRow<kElem, kV, kK, kStream>;
     const RowLane<kV, kK, kLog, kInter> row(lane, p.d, p.rot);
     float wa[kK][kV], wb[kK][kV], ga[kK][kV], gb[kK][kV];
     load_weight<kElem, kV, kK>(t.weight, p.weight_f32, row.first, row.second, row.valid, wa, wb);
@@ -237,16 +311,23 @@ __global__ __launch_bounds__(64 * kHeadsWaves) void heads_backward_kernel(HeadsP
         const char* in = t.in + (b * t.in_b + n * t.in_n) * Io<kElem>::kBytes;
         const char* grad = t.grad + (b * t.grad_b + n * t.grad_n) * Io<kElem>::kBytes;
         char* out = t.out + (b * t.out_b + n * t.out_n) * Io<kElem>::kBytes;
+        Raw ahead_x, ahead_u;
+        ahead_x.load(in + h0 * t.in_h * Io<kElem>::kBytes, row.first, row.second);
+        ahead_u.load(grad + h0 * t.grad_h * Io<kElem>::kBytes, row.first, row.second);
         float cs[kK][kV], sn[kK][kV];
         angles(row, p, position_of(p, b, n), cs, sn);
         for (int h = h0; h < h1; ++h) {
             float xa[kK][kV], xb[kK][kV], ua[kK][kV], ub[kK][kV];
-            load_row<kElem, kV, kK>(in + h * t.in_h * Io<kElem>::kBytes, row.first, row.second, row.valid, live, xa, xb);
-            load_row<kElem, kV, kK>(grad + h * t.grad_h * Io<kElem>::kBytes, row.first, row.second, row.valid, live, ua, ub);
+            ahead_x.get(row.valid, live, xa, xb);
+            ahead_u.get(row.valid, live, ua, ub);
+            if (h + 1 < h1) {
+                ahead_x.load(in + (h + 1) * t.in_h * Io<kElem>::kBytes, row.first, row.second);
+                ahead_u.load(grad + (h + 1) * t.grad_h * Io<kElem>::kBytes, row.first, row.second);
+            }
             float sum = 0.0f, dot = 0.0f;
 #pragma unroll
             for (int k = 0; k < kK; ++k) {
-                rotate<kV, kInter>(ua[k], ub[k], cs[k], sn[k], row.turned[k], -1.0f);
+                rotate<kV, kInter>(ua[k], ub[k], cs[k], sn[k], row.turned[k], row.turned_b[k], -1.0f);
 #pragma unroll
                 for (int j = 0; j < kV; ++j) {
                     sum = fmaf(xa[k][j], xa[k][j], fmaf(xb[k][j], xb[k][j], sum));
@@ -266,7 +347,7 @@ __global__ __launch_bounds__(64 * kHeadsWaves) void heads_backward_kernel(HeadsP
                     xa[k][j] = r * (ua[k][j] * wa[k][j] - na * mean);
                     xb[k][j] = r * (ub[k][j] * wb[k][j] - nb * mean);
                 }
-            store_row<kElem, kV, kK>(out + h * t.out_h * Io<kElem>::kBytes, row.first, row.second, row.valid, live, xa, xb);
+            Raw::store(out + h * t.out_h * Io<kElem>::kBytes, row.first, row.second, row.valid, live, xa, xb);
         }
     }
     if (!p.partial) return;
@@ -336,74 +417,85 @@ __global__ __launch_bounds__(kSumColumns * kSumGroups) void heads_weight_kernel(
     }
 }
 
-// Lanes of a row: d / 16 with pieces of eight (d a multiple of 16: 1, 2, 4, 8 or 16 lanes, the next power of two), a
-// whole wave with pieces of one.
-static int row_log(const HeadsParams& p) { return !p.vector ? 6 : p.d <= 64 ? 2 : p.d <= 128 ? 3 : 4; }
+// Lanes of a row, as a power of two: d / 8 and more with pieces of four, a whole wave with pieces of one.
+static int row_log(const HeadsParams& p) { return !p.vector ? 6 : kPieceLog + (p.d <= 64 ? 0 : p.d <= 128 ? 1 : 2); }
 
+// Heads a wave takes: the more, the fewer angles are formed twice; the fewer, the more waves there are.  Rows from memory
+// want 64 waves a compute unit (16 and 64: forward B4 N4096 H16+16 d128 57 and 51 us, backward 92 and 78), rows from the
+// cache 16 (forward B3 N1777 H32+8 d64 14.5 and 18).
 void plan_heads(HeadsParams* p, bool backward) {
     const long tokens = 64 >> row_log(*p);
     const long groups = (p->tokens + tokens - 1) / tokens;  // waves that one head a wave needs
-    // Heads a wave: as many as leave about 16 waves a compute unit, 16 at most; the more, the fewer angles are formed twice.
+    const long want = (p->stream ? 64 : 16) * kComputeUnits;
     const int most = p->q.H > p->k.H ? p->q.H : p->k.H;
     int heads = 16;
-    while (heads > 1 && groups * ((p->q.H + heads - 1) / heads + (p->k.H + heads - 1) / heads) < 4096) heads /= 2;
+    while (heads > 1 && groups * ((p->q.H + heads - 1) / heads + (p->k.H + heads - 1) / heads) < want) heads /= 2;
     if (heads > most) heads = most;
     p->heads_per_wave = heads;
     p->units_q = (p->q.H + heads - 1) / heads;
     p->units = p->units_q + (p->k.H + heads - 1) / heads;
     if (backward) {
         const long blocks = (groups + kHeadsWaves - 1) / kHeadsWaves;
-        long want = 1024 / p->units;
-        if (want < 1) want = 1;
-        p->groups = (int)(blocks < want ? blocks : want);
+        long most_groups = kBackwardResident * kComputeUnits / p->units;
+        if (most_groups < 1) most_groups = 1;
+        p->groups = (int)(blocks < most_groups ? blocks : most_groups);
     }
 }
 
-template <int kElem, int kV, int kK, int kLog, bool kNorm>
-static void launch_heads_l(const HeadsParams& p, int layout, unsigned blocks, hipStream_t stream) {
-    const dim3 grid(blocks), block(64 * kHeadsWaves);
-    if (layout) hipLaunchKernelGGL((heads_kernel<kElem, kV, kK, kLog, kNorm, true>), grid, block, 0, stream, p);
-    else hipLaunchKernelGGL((heads_kernel<kElem, kV, kK, kLog, kNorm, false>), grid, block, 0, stream, p);
+template <int kElem, int kV, int kK, int kLog, bool kNorm, bool kStream>
+static void launch_heads_l(const HeadsParams& p, int layout, hipStream_t stream) {
+    const long long waves = (((long long)p.tokens + (64 >> kLog) - 1) >> (6 - kLog)) * p.units;
+    const dim3 grid((unsigned)((waves + kHeadsWaves - 1) / kHeadsWaves)), block(64 * kHeadsWaves);
+    if (layout) hipLaunchKernelGGL((heads_kernel<kElem, kV, kK, kLog, kNorm, true, kStream>), grid, block, 0, stream, p);
+    else hipLaunchKernelGGL((heads_kernel<kElem, kV, kK, kLog, kNorm, false, kStream>), grid, block, 0, stream, p);
+}
+
+template <int kElem, bool kNorm, bool kStream>
+static void launch_heads_s(const HeadsParams& p, int layout, hipStream_t stream) {
+    const int log = row_log(p);
+    if (log == kPieceLog) launch_heads_l<kElem, kPiece, 1, kPieceLog, kNorm, kStream>(p, layout, stream);
+    else if (log == kPieceLog + 1) launch_heads_l<kElem, kPiece, 1, kPieceLog + 1, kNorm, kStream>(p, layout, stream);
+    else launch_heads_l<kElem, kPiece, 1, kPieceLog + 2, kNorm, kStream>(p, layout, stream);
 }
 
 template <int kElem, bool kNorm>
-static void launch_heads_e(const HeadsParams& p, int layout, hipStream_t stream) {
-    const int log = row_log(p);
-    const long long waves = (((long long)p.tokens + (64 >> log) - 1) >> (6 - log)) * p.units;
-    const unsigned blocks = (unsigned)((waves + kHeadsWaves - 1) / kHeadsWaves);
-    if (log == 2) launch_heads_l<kElem, 8, 1, 2, kNorm>(p, layout, blocks, stream);
-    else if (log == 3) launch_heads_l<kElem, 8, 1, 3, kNorm>(p, layout, blocks, stream);
-    else if (log == 4) launch_heads_l<kElem, 8, 1, 4, kNorm>(p, layout, blocks, stream);
-    else launch_heads_l<kElem, 1, 2, 6, kNorm>(p, layout, blocks, stream);
-}
-
-hipError_t launch_heads(const HeadsParams& p, int elem, int layout, bool norm, hipStream_t stream) {
-    if (norm) {
-        if (elem == 0) launch_heads_e<0, true>(p, layout, stream);
-        else if (elem == 1) launch_heads_e<1, true>(p, layout, stream);
-        else launch_heads_e<2, true>(p, layout, stream);
-    } else {
-        if (elem == 0) launch_heads_e<0, false>(p, layout, stream);
-        else if (elem == 1) launch_heads_e<1, false>(p, layout, stream);
-        else launch_heads_e<2, false>(p, layout, stream);
-    }
+static hipError_t launch_heads_e(const HeadsParams& p, int layout, hipStream_t stream) {
+    if (!p.vector) launch_heads_l<kElem, 1, 2, 6, kNorm, false>(p, layout, stream);
+    else if (p.stream) launch_heads_s<kElem, kNorm, true>(p, layout, stream);
+    else launch_heads_s<kElem, kNorm, false>(p, layout, stream);
     return hipGetLastError();
 }
 
-template <int kElem, int kV, int kK, int kLog>
+hipError_t launch_heads(const HeadsParams& p, int elem, int layout, bool norm, hipStream_t stream) {
+    if (norm)
+        return elem == 0 ? launch_heads_e<0, true>(p, layout, stream)
+             : elem == 1 ? launch_heads_e<1, true>(p, layout, stream)
+                         : launch_heads_e<2, true>(p, layout, stream);
+    return elem == 0 ? launch_heads_e<0, false>(p, layout, stream)
+         : elem == 1 ? launch_heads_e<1, false>(p, layout, stream)
+                     : launch_heads_e<2, false>(p, layout, stream);
+}
+
+template <int kElem, int kV, int kK, int kLog, bool kStream>
 static void launch_heads_backward_l(const HeadsParams& p, int layout, hipStream_t stream) {
     const dim3 grid((unsigned)(p.groups * p.units)), block(64 * kHeadsWaves);
-    if (layout) hipLaunchKernelGGL((heads_backward_kernel<kElem, kV, kK, kLog, true>), grid, block, 0, stream, p);
-    else hipLaunchKernelGGL((heads_backward_kernel<kElem, kV, kK, kLog, false>), grid, block, 0, stream, p);
+    if (layout) hipLaunchKernelGGL((heads_backward_kernel<kElem, kV, kK, kLog, true, kStream>), grid, block, 0, stream, p);
+    else hipLaunchKernelGGL((heads_backward_kernel<kElem, kV, kK, kLog, false, kStream>), grid, block, 0, stream, p);
+}
+
+template <int kElem, bool kStream>
+static void launch_heads_backward_s(const HeadsParams& p, int layout, hipStream_t stream) {
+    const int log = row_log(p);
+    if (log == kPieceLog) launch_heads_backward_l<kElem, kPiece, 1, kPieceLog, kStream>(p, layout, stream);
+    else if (log == kPieceLog + 1) launch_heads_backward_l<kElem, kPiece, 1, kPieceLog + 1, kStream>(p, layout, stream);
+    else launch_heads_backward_l<kElem, kPiece, 1, kPieceLog + 2, kStream>(p, layout, stream);
 }
 
 template <int kElem>
 static hipError_t launch_heads_backward_e(const HeadsParams& p, int layout, hipStream_t stream) {
-    const int log = row_log(p);
-    if (log == 2) launch_heads_backward_l<kElem, 8, 1, 2>(p, layout, stream);
-    else if (log == 3) launch_heads_backward_l<kElem, 8, 1, 3>(p, layout, stream);
-    else if (log == 4) launch_heads_backward_l<kElem, 8, 1, 4>(p, layout, stream);
-    else launch_heads_backward_l<kElem, 1, 2, 6>(p, layout, stream);
+    if (!p.vector) launch_heads_backward_l<kElem, 1, 2, 6, false>(p, layout, stream);
+    else if (p.stream) launch_heads_backward_s<kElem, true>(p, layout, stream);
+    else launch_heads_backward_s<kElem, false>(p, layout, stream);
     return hipGetLastError();
 }
 

@@ -28,7 +28,8 @@ struct HeadsParams {
     int tokens;                   // B N
     int weight_f32;               // weights are fp32 whatever the elements are
     int transposed;
-    int vector;                   // rows are 16-byte aligned and cut into pieces of eight elements
+    int vector;                   // rows can be cut into pieces of four elements (else of one)
+    int stream;                   // the rows exceed the last-level cache: nontemporal loads and stores
     int heads_per_wave, units_q, units;  // a wave takes so many heads of a token; waves a token needs
     int groups;                   // backward: workgroups a unit's tokens are spread over
     float* partial;               // backward: [groups * units][d]: sums of weight gradients, one row a workgroup

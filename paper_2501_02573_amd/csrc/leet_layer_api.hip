@@ -41,13 +41,15 @@ bool rows_apart(long long width, Dim* dims, int n) {
 
 // ---- heads ----
 
-// One tensor of rows of heads; vector is cleared where its rows cannot be read sixteen bytes at a time.
-bool heads_ok(const leet_attn_heads* t, int B, int H, int N, int d, size_t size, bool written, int* vector) {
+// Rows read and written beyond this are streamed past the last-level cache (256 MiB, 0.6 of it: where the prefill's inputs
+// begin to fall out of it too).  us with and without, forward B4 H16+16 d128 bf16, the same tensors again and again |
+// four sets in turn: N 2048 (128 MiB in and out) 29 23 | 29 34, N 2816 (176 MiB) 38 33 | 39 48, N 4096 51 52 | 52 63,
+// N 6144 75 88 | 75 88.
+constexpr size_t kStreamBytes = ((size_t)256 << 20) / 5 * 3;
+
+bool heads_ok(const leet_attn_heads* t, int B, int H, int N, int d, size_t size, bool written) {
     if (!t || !t->data || !aligned(t->data, size)) return false;
     Dim dims[3] = {{B, t->batch}, {H, t->head}, {N, t->token}};
-    for (const Dim& m : dims)
-        if (m.size > 1 && (m.stride * (long long)size) % 16 != 0) *vector = 0;
-    if (!aligned(t->data, 16)) *vector = 0;
     return !written || rows_apart(d, dims, 3);
 }
 
@@ -73,12 +75,13 @@ int heads_params(const HeadsCall& q, const HeadsCall& k, const leet_attn_rotatio
     p->tokens = B * N;
     if (N == 0) return LEET_OK;
     const size_t size = size_of(dtype), weight_size = size_of(weight_dtype);
-    p->vector = d % 16 == 0 && (rotation->layout == LEET_ROPE_INTERLEAVED || rotation->rot % 16 == 0);
+    p->vector = d % 8 == 0 && (rotation->layout == LEET_ROPE_INTERLEAVED || rotation->rot % 8 == 0);
+    p->stream = (size_t)B * N * (q.H + (keys ? k.H : 0)) * d * size * (backward ? 3 : 2) > kStreamBytes;
     for (const HeadsCall* c : {&q, &k}) {
         if (c == &k && !keys) continue;
-        if (!heads_ok(c->in, B, c->H, N, d, size, false, &p->vector) ||
-            !heads_ok(c->out, B, c->H, N, d, size, true, &p->vector) ||
-            (backward && !heads_ok(c->grad, B, c->H, N, d, size, false, &p->vector)))
+        if (!heads_ok(c->in, B, c->H, N, d, size, false) ||
+            !heads_ok(c->out, B, c->H, N, d, size, true) ||
+            (backward && !heads_ok(c->grad, B, c->H, N, d, size, false)))
             return LEET_ERR_INVALID_ARG;
         if (!aligned(c->weight, weight_size) || !aligned(c->weight_grad, weight_size)) return LEET_ERR_INVALID_ARG;
         leet::HeadRows& r = c == &q ? p->q : p->k;
@@ -106,7 +109,7 @@ int heads_params(const HeadsCall& q, const HeadsCall& k, const leet_attn_rotatio
     p->weight_f32 = weight_dtype == LEET_F32;
     leet::plan_heads(p, backward);
     // a wave takes 64 lanes of tokens of at least one lane each, for one unit
-    if ((long long)p->tokens * p->units * (p->vector ? 16 : 64) >= kMaxThreads) return LEET_ERR_TOO_LARGE;
+    if ((long long)p->tokens * p->units * 64 >= kMaxThreads) return LEET_ERR_TOO_LARGE;
     int dev = 0;
     return leet::current_device(&dev);
 }
@@ -202,15 +205,16 @@ int leet_attn_qk_norm_rope(const leet_attn_heads *q, const leet_attn_heads *out_
 
 size_t leet_attn_qk_norm_rope_workspace_bytes(int B, int Hq, int Hk, int N, int d) {
     if (B <= 0 || Hq <= 0 || Hk <= 0 || N <= 0 || d < 2 || d > 256 || d % 2 != 0 || (long long)B * N >= 1LL << 31) return 0;
-    // the two cuts of rows give different numbers of workgroups; room for either
+    // the cuts of rows and their way from memory give different numbers of workgroups; room for any
     size_t rows = 0;
-    for (int vector = 0; vector < 2; ++vector) {
+    for (int way = 0; way < 4; ++way) {
         leet::HeadsParams p = {};
         p.q.H = Hq;
         p.k.H = Hk;
         p.tokens = B * N;
         p.d = d;
-        p.vector = vector;
+        p.vector = way & 1;
+        p.stream = way >> 1;
         leet::plan_heads(&p, true);
         const size_t r = (size_t)p.groups * p.units;
         if (r > rows) rows = r;

@@ -343,3 +343,13 @@ def test_workspace_of_the_callers(leet):
         assert torch.equal(want, leet.leet_attn_gated_scan(x, z, workspace=ws))
     with pytest.raises(leet.LeetAttnError):
         leet.leet_attn_gated_scan(x, z, workspace=ws[:need - 256])
+
+
+def test_offsets_beyond_32_bits(leet):
+    """Tokens 2^22 elements apart: the last rows are past 2^32 bytes, and past 2^31 elements."""
+    N, C = 1030, 66
+    wide = torch.empty((N, 1 << 22), dtype=BF16, device="cuda")
+    x, gate, out = wide[None, :, 4:4 + C], wide[None, :, 101:101 + C], wide[None, :, 200:200 + C]
+    x.copy_(_normal((1, N, C), BF16, 150))
+    gate.copy_(_gate((1, N, C), BF16, 1, 151))
+    _check(leet, 1, N, C, (BF16, BF16), 1, True, x=x, gate=gate, into=out)

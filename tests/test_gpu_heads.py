@@ -252,3 +252,50 @@ def test_on_another_stream_and_in_a_graph(leet):
         eager = both()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(eager, kept))
+
+
+@pytest.mark.parametrize("layout", [0, 1])
+@pytest.mark.parametrize("dtype, d, N", [(BF16, 128, 5000), (F16, 64, 9001), (F32, 256, 1203)])
+def test_rows_beyond_the_cache(leet, dtype, d, N, layout):
+    """Rows that are streamed give what the same rows give a few tokens at a time."""
+    B, Hq, Hk = 4, 16, 12
+    q, k = (torch.randn((B, N, H, d), device="cuda").to(dtype).transpose(1, 2) for H in (Hq, Hk))
+    assert 2 * (q.numel() + k.numel()) * q.element_size() > 160 << 20
+    w, freq = _normal((d,), dtype, 60, 0.3, 1.0), _freq(d // 2).cuda()
+    turned = leet.leet_attn_rope(q, freq, k=k, layout=layout)
+    y = leet.leet_attn_qk_norm_rope(q, k, w, w, freq, layout=layout)
+    dx = leet.leet_attn_qk_norm_rope_backward(y[0], y[1], q, k, w, w, freq, layout=layout)
+    sums = [torch.zeros(d, dtype=torch.float64, device="cuda") for _ in range(2)]
+    for lo in range(0, N, 400):
+        some = slice(lo, min(lo + 400, N))
+        part = [t[:, :, some] for t in (q, k)]
+        for whole, few in ((turned, leet.leet_attn_rope(part[0], freq, k=part[1], layout=layout, pos0=lo)),
+                           (y, leet.leet_attn_qk_norm_rope(*part, w, w, freq, layout=layout, pos0=lo))):
+            assert all(torch.equal(a[:, :, some], b) for a, b in zip(whole, few))
+        few = leet.leet_attn_qk_norm_rope_backward(y[0][:, :, some], y[1][:, :, some], *part, w.float(), w.float(), freq,
+                                                   layout=layout, pos0=lo)
+        assert all(torch.equal(a[:, :, some], b) for a, b in zip(dx[:2], few[:2]))
+        for s, g in zip(sums, few[2:]):
+            s += g.double()
+    # with dy = y, u = w n, so terms w n^2 of one sign a column: the sum's error is relative, 96 u of a part's and of the
+    # whole's, which the type's rounding is added to (in fp16 to infinity: the sums of 2e5 rows and more are beyond 65504)
+    for got, s in zip(dx[2:], sums):
+        over = s.abs() > 1.01 * torch.finfo(dtype).max
+        assert bool((got[over] == float("inf")).all())
+        off = (got.double() - s).abs() - (2 * 96 * forms.U * s.abs() + 1.01 * forms.half_step(s, dtype))
+        assert bool((off[~over] <= 0).all())
+
+
+def test_offsets_beyond_32_bits(leet):
+    """Tokens 2^25 elements apart: the last rows are past 2^32 bytes, and past 2^31 elements."""
+    N, d, freq = 70, 64, _freq(64)
+    wide = torch.empty((N, 1 << 25), dtype=BF16, device="cuda")
+    x = wide[:, 128:128 + 2 * d].view(1, N, 2, d).transpose(1, 2)
+    x.copy_(_normal((1, 2, N, d), BF16, 61))
+    w, pos = _normal((d,), BF16, 62, 0.3, 1.0), torch.arange(N).view(1, N)
+    y, z = leet.leet_attn_qk_norm_rope(x[:, :1], x[:, 1:], w, w, freq.cuda())
+    want = forms.norm_rope(_f64(x), _f64(w), freq, pos, 0)
+    assert forms.close(torch.cat((y, z), 1), want)
+    into = wide[:, 1024:1024 + 2 * d].view(1, N, 2, d).transpose(1, 2)
+    leet.leet_attn_rope(x, freq.cuda(), out_q=into)
+    assert forms.close(into, forms.rotate(_f64(x), freq, pos, 0))

@@ -68,9 +68,9 @@ P = 0x100000   # aligned, never touched
 
 def _heads_args(leet, **change):
     """Arguments of the three calls on heads, by name."""
-    H = lambda at=P, b=1 << 20, h=1 << 14, n=128: leet._Heads(at, b, h, n)  # noqa: E731
+    H = lambda at=P, b=1 << 20, h=1 << 14, n=128: leet._pack_heads(at, b, h, n)  # noqa: E731
     a = dict(q=H(), out_q=H(2 * P), Hq=2, k=H(3 * P), out_k=H(4 * P), Hk=2, dq=H(5 * P), dk=H(6 * P), wq=P, wk=P, gq=P, gk=P,
-             wd=leet.LEET_BF16, eps=1e-6, rot=leet._Rotation(P, 64, 0, None, 0, 0, 1.0), ws=P, wsb=1 << 40, B=2, N=16,
+             wd=leet.LEET_BF16, eps=1e-6, rot=leet._pack_rotation(P, 64, 0, 0, 0, 0, 1.0), ws=P, wsb=1 << 40, B=2, N=16,
              d=128, dtype=leet.LEET_BF16)
     a.update(change)
     return a
@@ -93,18 +93,18 @@ def _back(leet, a):
 
 
 def test_heads_refused(leet):
-    H, R = leet._Heads, leet._Rotation
+    H, R = leet._pack_heads, leet._pack_rotation
     INVALID, UNSUPPORTED, LARGE = leet.LEET_ERR_INVALID_ARG, leet.LEET_ERR_UNSUPPORTED, leet.LEET_ERR_TOO_LARGE
     cases = [
         (INVALID, dict(q=None)), (INVALID, dict(out_q=None)), (INVALID, dict(out_k=None)), (INVALID, dict(rot=None)),
-        (INVALID, dict(q=H(None, 0, 0, 0))), (INVALID, dict(q=H(P + 1, 1 << 20, 1 << 14, 128))),
+        (INVALID, dict(q=H(0, 0, 0, 0))), (INVALID, dict(q=H(P + 1, 1 << 20, 1 << 14, 128))),
         (INVALID, dict(B=0)), (INVALID, dict(N=-1)), (INVALID, dict(Hq=0)), (INVALID, dict(Hk=0)),
         (UNSUPPORTED, dict(d=127)), (UNSUPPORTED, dict(d=258)), (UNSUPPORTED, dict(d=0)), (UNSUPPORTED, dict(dtype=7, wd=7)),
-        (INVALID, dict(rot=R(None, 64, 0, None, 0, 0, 1.0))), (INVALID, dict(rot=R(P + 4, 64, 0, None, 0, 0, 1.0))),
-        (INVALID, dict(rot=R(P, 63, 0, None, 0, 0, 1.0))), (INVALID, dict(rot=R(P, 130, 0, None, 0, 0, 1.0))),
-        (INVALID, dict(rot=R(P, 0, 0, None, 0, 0, 1.0))), (INVALID, dict(rot=R(P, 64, 2, None, 0, 0, 1.0))),
-        (INVALID, dict(rot=R(P, 64, 0, P + 4, 0, 0, 1.0))), (INVALID, dict(rot=R(P, 64, 0, None, 0, 0, math.nan))),
-        (INVALID, dict(rot=R(P, 64, 0, None, 0, 0, math.inf))),
+        (INVALID, dict(rot=R(0, 64, 0, 0, 0, 0, 1.0))), (INVALID, dict(rot=R(P + 4, 64, 0, 0, 0, 0, 1.0))),
+        (INVALID, dict(rot=R(P, 63, 0, 0, 0, 0, 1.0))), (INVALID, dict(rot=R(P, 130, 0, 0, 0, 0, 1.0))),
+        (INVALID, dict(rot=R(P, 0, 0, 0, 0, 0, 1.0))), (INVALID, dict(rot=R(P, 64, 2, 0, 0, 0, 1.0))),
+        (INVALID, dict(rot=R(P, 64, 0, P + 4, 0, 0, 1.0))), (INVALID, dict(rot=R(P, 64, 0, 0, 0, 0, math.nan))),
+        (INVALID, dict(rot=R(P, 64, 0, 0, 0, 0, math.inf))),
         (LARGE, dict(B=1 << 16, N=1 << 16)),
         # rows that are written must lie apart: a head stride within a row, a stride of zero, tokens over heads
         (INVALID, dict(out_q=H(2 * P, 1 << 20, 64, 128))), (INVALID, dict(out_q=H(2 * P, 0, 1 << 14, 128))),
@@ -138,7 +138,7 @@ def test_norm_backward_workspace(leet):
 
 
 def _scan_args(leet, **change):
-    R = lambda at=P, b=1 << 20, n=256: leet._Rows(at, b, n)  # noqa: E731
+    R = lambda at=P, b=1 << 20, n=256: leet._pack_rows(at, b, n)  # noqa: E731
     a = dict(x=R(), gate=R(2 * P), out=R(3 * P), h=R(4 * P), dx=R(5 * P), dgate=R(6 * P), s_in=P, s_out=P, ds_in=2 * P,
              offsets=None, S=0, ws=P, wsb=1 << 40, B=2, N=16, C=256, dtype=leet.LEET_BF16, gd=leet.LEET_F32, mode=1)
     a.update(change)
@@ -162,9 +162,9 @@ def _step(leet, a):
 
 
 def test_scan_refused(leet):
-    R = leet._Rows
+    R = leet._pack_rows
     INVALID, UNSUPPORTED, LARGE = leet.LEET_ERR_INVALID_ARG, leet.LEET_ERR_UNSUPPORTED, leet.LEET_ERR_TOO_LARGE
-    both = [(INVALID, dict(gate=None)), (INVALID, dict(out=None)), (INVALID, dict(gate=R(None, 0, 0))),
+    both = [(INVALID, dict(gate=None)), (INVALID, dict(out=None)), (INVALID, dict(gate=R(0, 0, 0))),
             (INVALID, dict(gate=R(2 * P + 2, 1 << 20, 256))), (INVALID, dict(B=0)), (INVALID, dict(C=0)),
             (INVALID, dict(mode=3)), (UNSUPPORTED, dict(dtype=5)), (UNSUPPORTED, dict(gd=leet.LEET_F16)),
             (UNSUPPORTED, dict(dtype=leet.LEET_F32, gd=leet.LEET_BF16))]
