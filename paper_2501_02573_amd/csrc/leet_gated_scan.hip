@@ -23,15 +23,15 @@
 namespace leet {
 
 // A tile: tokens of a wave, and waves of a workgroup that hold tokens (at most); one more wave links the tile to the others.
-// Whole workgroups of 8 and 12 waves spread evenly over the four SIMDs of a compute unit.  us at B4 N4096 C2048 bf16
-// (forward) and N32768 C4096: 16 x 7 57 and 196, 16 x 5 68 and 230, 12 x 9 71 and 240, 8 x 15 60 and 211; backward at
-// B4 N4096 C2048, sigmoid: 8 x 11 93, 12 x 7 96, 8 x 7 102, 8 x 9 102, 16 x 7 154 (registers: one workgroup a unit).
+// Workgroups of 8, 12 or 16 waves spread evenly over the four SIMDs of a compute unit (B4 N4096 C2048 forward: 16 tokens x 7
+// waves 57 us, 16 x 5 68, 12 x 9 71; backward 8 x 11 93, 8 x 9 102).
 struct ForwardTile {
-    static constexpr int kTokens = 16, kWaves = 7;
+    static constexpr int kTokens = 16;
 };
 struct BackwardTile {
-    static constexpr int kTokens = 8, kWaves = 11;
+    static constexpr int kTokens = 8;
 };
+constexpr int kMostWaves = 15;
 
 // The decay a and, for the moving average, 1 - a (each as accurate as the smaller of the two: the larger one is what that
 // leaves of 1).
@@ -127,14 +127,15 @@ __device__ __forceinline__ void store_state(float* s, int sequence, int C, uint3
 // What the tiles of a column block tell one another.  A tile's run (A, H) is known as soon as its inputs are; the state
 // behind it (its inclusive state) when the state before it is.  Each is published by stores of eight bytes that no fence
 // has to order: a word that has not been written holds kUnset, which no value is published as.
-constexpr uint32_t kUnset = 0xffffffffu;  // a NaN that arithmetic does not produce; published as another one
+constexpr uint32_t kUnset = 0xffffffffu;  // a NaN; a value with these bits is published as another one
+constexpr uint32_t kCut = 0xfffffffeu;    // likewise: in the place of A, of a run that nothing before it reaches through
 
 __device__ __forceinline__ uint32_t publishable(float f) {
     const uint32_t u = __builtin_bit_cast(uint32_t, f);
-    return u == kUnset ? 0x7fc00000u : u;
+    return u >= kCut ? 0x7fc00000u : u;
 }
-__device__ __forceinline__ void publish(uint64_t* at, float lo, float hi) {
-    __hip_atomic_store(at, (uint64_t)publishable(hi) << 32 | publishable(lo), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+__device__ __forceinline__ void publish(uint64_t* at, uint32_t lo, uint32_t hi) {
+    __hip_atomic_store(at, (uint64_t)hi << 32 | lo, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 __device__ __forceinline__ uint64_t look(const uint64_t* at) {
     return __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -143,12 +144,18 @@ __device__ __forceinline__ float low(uint64_t w) { return __builtin_bit_cast(flo
 __device__ __forceinline__ float high(uint64_t w) { return __builtin_bit_cast(float, (uint32_t)(w >> 32)); }
 __device__ __forceinline__ bool is_set(uint64_t w) { return (uint32_t)w != kUnset && (uint32_t)(w >> 32) != kUnset; }
 
-// Workspace: a line for the ticket counter, then of every tile the runs of its channels (A, H: eight bytes a channel),
+// The state behind a run that was entered with s.
+__device__ __forceinline__ float through(uint64_t run, float s) {
+    return (uint32_t)run == kCut ? high(run) : fmaf(low(run), s, high(run));
+}
+
+// Workspace: kGroups lines, each with a ticket counter, then of every tile the runs of its channels (A, H: eight bytes a channel),
 // then of every tile the inclusive states of its channels, four bytes a channel in pairs (a lone channel: twice itself).
 struct Board {
     uint64_t *runs, *states;
     long long tile;  // words of a tile's runs
-    static constexpr size_t kHeader = 256;
+    static constexpr int kGroups = 16, kLine = 32;  // most groups; 32-bit words of a line
+    static constexpr size_t kHeader = kGroups * kLine * 4;
 
     template <int kV>
     __device__ __forceinline__ static Board of(const GatedScanParams& p, int block, int lane) {
@@ -161,19 +168,20 @@ struct Board {
         return b;
     }
     template <int kV>
-    __device__ __forceinline__ void publish_run(int k, const float* A, const float* H) const {
+    __device__ __forceinline__ void publish_run(int k, bool cut, const float* A, const float* H) const {
 #pragma unroll
-        for (int v = 0; v < kV; ++v) publish(runs + k * tile + v, A[v], H[v]);
+        for (int v = 0; v < kV; ++v) publish(runs + k * tile + v, cut ? kCut : publishable(A[v]), publishable(H[v]));
     }
     template <int kV>
     __device__ __forceinline__ void publish_state(int k, const float* s) const {
-        publish(states + k * (tile / kV), s[0], s[kV - 1]);
+        publish(states + k * (tile / kV), publishable(s[0]), publishable(s[kV - 1]));
     }
 
-    // A window of what tiles k, k - 1, .. have published.
+    // A window of what tiles k, k - 1, .. have published.  What is looked at in vain costs memory bandwidth: two, four and
+    // eight tiles at a time, B4 N4096 C2048 52, 54 and 55 us.
     template <int kV>
     struct Window {
-        static constexpr int kTiles = 4;
+        static constexpr int kTiles = 2;
         uint64_t run[kTiles][kV], whole[kTiles];
         int runs;    // so many, from tile k on, have published their runs ..
         bool ended;  // .. and the next one its state
@@ -206,7 +214,7 @@ struct Board {
 #pragma unroll
                 for (int v = 0; v < kV; ++v) {
                     if (ended && u == runs) state[v] = v ? high(whole[u]) : low(whole[u]);
-                    if (u < runs) state[v] = fmaf(low(run[u][v]), state[v], high(run[u][v]));
+                    if (u < runs) state[v] = through(run[u][v], state[v]);
                 }
         }
     };
@@ -251,27 +259,34 @@ __global__ __launch_bounds__(256) void gated_scan_clear_kernel(u32x4* words, siz
 }
 
 // Shared by the waves of a workgroup.
-template <int kV, int kWaves>
+template <int kV>
 struct Shared {
-    float A[kWaves][64 * kV], H[kWaves][64 * kV];  // the waves' runs
-    int cut[kWaves];  // a sequence begins (backward: ends) in the run: what came before does not reach behind it
+    float A[kMostWaves][64 * kV], H[kMostWaves][64 * kV];  // the waves' runs
+    int cut[kMostWaves];  // a sequence begins (backward: ends) in the run: what came before does not reach behind it
     float carry[64 * kV];
     unsigned ticket;
 };
 
-// The tile of a workgroup: column block `block` of all batch entries, tile k of its chain.
+// The tile of a workgroup: tile k of the chain of column block `block` (of all batch entries).  Tiles are taken in the order
+// in which workgroups start, whatever that is: workgroup l to start of group g takes tile l groups + g of all, counted
+// chain by chain first and along the chains last.  groups divides the number of chains, so all tiles of a chain belong to
+// one group, and every tile before this one on its chain has been taken.  Eight workgroups in a row, which go to the eight
+// XCDs, belong to one group: chains then advance together and rows are read whole.  us with one counter | sixteen groups |
+// one counter for every chain | sixteen groups of workgroups equal modulo 16, two for each XCD: B4 N4096 C2048 bf16
+// 53 51 52 52, N32768 C4096 197 196 221 221, packed N20011 C1001 fp16 57 54 53 54.  False: a workgroup beyond the last tile.
 template <class S>
-__device__ __forceinline__ void take_tile(const GatedScanParams& p, S& shared, int* block, int* k) {
-    unsigned ticket = blockIdx.x;
+__device__ __forceinline__ bool take_tile(const GatedScanParams& p, S& shared, int* block, int* k) {
     const unsigned blocks = (unsigned)p.B * (unsigned)p.columns;
+    unsigned tile = blockIdx.x;
     if (p.tiles > 1) {
-        // in the order in which workgroups start, whatever that is
-        if (threadIdx.x == 0) shared.ticket = atomicAdd(static_cast<unsigned*>(p.workspace), 1u);
+        const unsigned group = (blockIdx.x >> 3) % (unsigned)p.groups;
+        if (threadIdx.x == 0) shared.ticket = atomicAdd(static_cast<unsigned*>(p.workspace) + group * Board::kLine, 1u);
         __syncthreads();
-        ticket = (unsigned)__builtin_amdgcn_readfirstlane((int)shared.ticket);
+        tile = (unsigned)__builtin_amdgcn_readfirstlane((int)shared.ticket) * p.groups + group;
     }
-    *block = (int)(ticket % blocks);
-    *k = (int)(ticket / blocks);
+    *k = (int)(tile / blocks);
+    *block = (int)(tile - (unsigned)*k * blocks);
+    return *k < p.tiles;
 }
 
 // The wave behind the data waves links the tile to the others: it joins the waves' runs, publishes, looks back, and leaves
@@ -300,7 +315,7 @@ __device__ __forceinline__ void link_tile(const GatedScanParams& p, S& shared, i
     }
     const Board board = Board::of<kV>(p, block, lane);
     if (k > 0) {
-        if (live && !cut) board.publish_run<kV>(k, A, H);
+        if (live) board.publish_run<kV>(k, cut, A, H);
         if (live && cut) board.publish_state<kV>(k, H);
         board.state_behind<kV>(k - 1, live, carry);
     }
@@ -369,12 +384,12 @@ __device__ __forceinline__ void pass_on(const GatedScanParams& p, const float* f
 
 // Workgroup = one tile of waves * kTokens tokens x 64 kV channels of one batch entry.
 template <int kX, int kG, int kMode, int kV, bool kPacked>
-__global__ __launch_bounds__(64 * (ForwardTile::kWaves + 1)) void gated_scan_kernel(GatedScanParams p) {
+__global__ __launch_bounds__(64 * (kMostWaves + 1)) void gated_scan_kernel(GatedScanParams p) {
     constexpr int kTokens = ForwardTile::kTokens;
-    __shared__ Shared<kV, ForwardTile::kWaves> shared;
+    __shared__ Shared<kV> shared;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int block, k;
-    take_tile(p, shared, &block, &k);
+    if (!take_tile(p, shared, &block, &k)) return;
     const int b = block / p.columns;
     uint32_t c;
     const bool live = channel_of<kV>(p, block - b * p.columns, lane, &c);
@@ -444,12 +459,12 @@ __global__ __launch_bounds__(64 * (ForwardTile::kWaves + 1)) void gated_scan_ker
 // The same from the last tile to the first.  The run of a wave maps the gradient that comes in from behind its last
 // token to the one that goes out before its first.
 template <int kX, int kG, int kMode, int kV, bool kPacked>
-__global__ __launch_bounds__(64 * (BackwardTile::kWaves + 1)) void gated_scan_backward_kernel(GatedScanParams p) {
+__global__ __launch_bounds__(64 * (kMostWaves + 1)) void gated_scan_backward_kernel(GatedScanParams p) {
     constexpr int kTokens = BackwardTile::kTokens;
-    __shared__ Shared<kV, BackwardTile::kWaves> shared;
+    __shared__ Shared<kV> shared;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int block, k;
-    take_tile(p, shared, &block, &k);
+    if (!take_tile(p, shared, &block, &k)) return;
     const int b = block / p.columns;
     uint32_t c;
     const bool live = channel_of<kV>(p, block - b * p.columns, lane, &c);
@@ -545,7 +560,9 @@ __global__ __launch_bounds__(256) void gated_step_kernel(GatedScanParams p) {
 // which: 0 forward, 1 backward
 template <int kX, int kG, int kMode, int kV>
 static void launch_scan_v(const GatedScanParams& p, int which, hipStream_t stream) {
-    const dim3 grid((unsigned)((long long)p.B * p.columns * p.tiles)), block(64 * (unsigned)(p.waves + 1));
+    // whole rounds of the groups: each is as many workgroups as the others
+    const long long all = (long long)p.B * p.columns * p.tiles, round = p.tiles > 1 ? 8LL * p.groups : 1;
+    const dim3 grid((unsigned)((all + round - 1) / round * round)), block(64 * (unsigned)(p.waves + 1));
     if (which == 0) {
         if (p.offsets) hipLaunchKernelGGL((gated_scan_kernel<kX, kG, kMode, kV, true>), grid, block, 0, stream, p);
         else hipLaunchKernelGGL((gated_scan_kernel<kX, kG, kMode, kV, false>), grid, block, 0, stream, p);
@@ -581,34 +598,48 @@ static hipError_t launch_scan(const GatedScanParams& p, int elem, int gate_elem,
     return gate_elem ? launch_scan_g<2, 2>(p, mode, which, stream) : launch_scan_g<2, 0>(p, mode, which, stream);
 }
 
-// Column blocks, waves of a workgroup and tiles of N tokens; returns the bytes of workspace.
-static size_t plan_scan(GatedScanParams* p, bool backward) {
+// Waves of a workgroup that hold tokens.  A chain advances a tile every 0.3 us, so where there are few chains long tiles
+// count; else what fits a compute unit twice does.  us with 7 | 11 | 15 waves, bf16: forward N20000 C1024 (8 chains) 65 47
+// 43, C2048 (16) 80 71 69, B2 N4096 C2048 (32) 31 32 33, B4 (64) 50 58 61, N32768 C4096 (32) 176 200 194; backward C1024 125
+// 86 72, B4 N4096 C2048 79 76 74, N32768 C4096 313 267 253; backward with x read too (sigmoid: 80 registers a lane, two
+// workgroups of 12 waves a unit but one of 16) C1024 122 88 77, C2048 151 121 128, B4 N4096 C2048 99 90 105.
+// Packed sequences are chains of their own (37 of them in N20011 C1001 forward: 54 | - | 60).
+constexpr int kForwardWaves = 7, kBackwardWaves = 11;  // the fewest, where there are tokens for them
+static int waves_of(const GatedScanParams& p, bool backward, int mode) {
+    const long long chains = (long long)p.B * p.columns * (p.offsets ? p.sequences : 1);
+    if (!backward) return chains <= 16 ? kMostWaves : kForwardWaves;
+    return mode != 2 || chains <= 8 ? kMostWaves : kBackwardWaves;
+}
+
+// Column blocks, waves of a workgroup and tiles of N tokens; returns the bytes of workspace.  mode < 0: any mode, any
+// sequences, the most bytes.
+static size_t plan_scan(GatedScanParams* p, bool backward, int mode) {
     const int v = p->C > 1 ? 2 : 1;
-    const int tokens = backward ? BackwardTile::kTokens : ForwardTile::kTokens, most = backward ? BackwardTile::kWaves : ForwardTile::kWaves;
+    const int tokens = backward ? BackwardTile::kTokens : ForwardTile::kTokens;
     p->columns = (p->C + 64 * v - 1) / (64 * v);
-    const int need = (p->N + tokens - 1) / tokens;
+    const long long chains = (long long)p->B * p->columns;
+    const int need = (p->N + tokens - 1) / tokens, most = mode >= 0 ? waves_of(*p, backward, mode) : backward ? kBackwardWaves : kForwardWaves;
     p->waves = need < 1 ? 1 : need < most ? need : most;  // no tokens: one that hands the states on
     p->tiles = need < 1 ? 1 : (need + p->waves - 1) / p->waves;
-    if (p->tiles == 1) return 0;
-    const size_t lanes = (size_t)p->B * p->columns * 64 * p->tiles;
-    return Board::kHeader + lanes * (8 * v + 8);
+    for (p->groups = Board::kGroups; chains % p->groups != 0;) p->groups /= 2;
+    return p->tiles == 1 ? 0 : Board::kHeader + (size_t)chains * 64 * p->tiles * (8 * v + 8);
 }
 
 size_t gated_scan_workspace(int B, int N, int C, bool backward) {
     GatedScanParams p = {};
     p.B = B; p.N = N; p.C = C;
-    return plan_scan(&p, backward);
+    return plan_scan(&p, backward, -1);
 }
 
 long long gated_scan_threads(int B, int N, int C, bool backward) {
     GatedScanParams p = {};
     p.B = B; p.N = N; p.C = C;
-    plan_scan(&p, backward);
-    return (long long)p.B * p.columns * p.tiles * (p.waves + 1) * 64;
+    plan_scan(&p, backward, -1);
+    return ((long long)p.B * p.columns * p.tiles + Board::kGroups * 8) * (kMostWaves + 1) * 64;
 }
 
 static hipError_t launch_sequences(GatedScanParams& p, int elem, int gate_elem, int mode, int which, hipStream_t stream) {
-    const size_t bytes = plan_scan(&p, which != 0);
+    const size_t bytes = plan_scan(&p, which != 0, mode);
     if (bytes) {
         const size_t words = (bytes + 15) / 16;
         hipLaunchKernelGGL(gated_scan_clear_kernel, dim3((unsigned)((words + 255) / 256)), dim3(256), 0, stream,

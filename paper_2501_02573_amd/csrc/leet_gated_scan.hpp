@@ -30,6 +30,7 @@ struct GatedScanParams {
     int waves;                     // waves of a workgroup
     int tiles;                     // of a column block's N tokens
     void* workspace;               // more than one tile: gated_scan_workspace bytes
+    int groups;                    // of column blocks, each with a ticket counter of its own
 };
 
 // Bytes of workspace for these sizes; 0: none is needed.
