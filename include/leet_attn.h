@@ -331,8 +331,9 @@ int leet_attn_query_plan_rd(int B, int H, int N, int r, int dv, int dtype, int s
  * head), and the element-wise recurrence with a decay of its own for every token and channel.
  * Of the conventions above these differ: tensors may have strides (in ELEMENTS; the elements of a
  * head row, or the channels of a token row, are adjacent), pointers need only their element's
- * alignment (16-byte aligned rows are faster), and a workspace, where one is needed, is always the
- * caller's, so that calls on several streams and captured graphs share nothing.
+ * alignment, and a workspace, where one is needed, is always the caller's, so that calls on several
+ * streams and captured graphs share nothing.  Calls that may overlap in time need one each (the
+ * recurrence's workgroups find one another through it).
  * N = 0 is legal everywhere here and writes no rows.
  * ---------------------------------------------------------------------------------------------- */
 
@@ -394,7 +395,7 @@ int leet_attn_rope_frequencies(int rot, double base, int scaling, double factor,
  * Position rotation of queries and, in the same launch, of keys.
  *   q, k          [B][Hq][N][d], [B][Hk][N][d] of `dtype`; k and out_k may be NULL (Hk is then ignored)
  *   out_q, out_k  of the same shapes and type; each may be its input itself (same data and strides),
- *                 and must not overlap anything else
+ *                 and must not overlap anything else (the same address is LEET_ERR_INVALID_ARG)
  *   transposed    non-zero: the transposed map (angles negated, same scale), which takes gradients of
  *                 the outputs to gradients of the inputs
  * d even, 2 <= d <= 256.  Rounded once, at the store.
@@ -423,7 +424,7 @@ int leet_attn_qk_norm_rope(const leet_attn_heads *q, const leet_attn_heads *out_
  *   dout_q, dout_k        gradients of the outputs
  *   dq, dk                gradients of the inputs; each may be the gradient it comes from (same data
  *                         and strides), and must not overlap anything else
- *   dq_weight, dk_weight  [d] of weight_dtype, or NULL: not wanted
+ *   dq_weight, dk_weight  [d] of weight_dtype, two of them, or NULL: not wanted
  *   workspace             leet_attn_qk_norm_rope_workspace_bytes bytes, 256-byte aligned; may be NULL
  *                         when neither weight's gradient is wanted.  Its contents are scratch
  * The sums over tokens and heads are taken in fp32 in a fixed order: no atomics, equal from call to call.

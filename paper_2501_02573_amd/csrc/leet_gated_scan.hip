@@ -12,8 +12,12 @@
 // are joined by (A2, H2) after (A1, H1) = (A2 A1, A2 H1 + H2).  A wave takes kTokens tokens of 64 lanes' channels into
 // registers and forms its run's (A, H); the waves of a workgroup lie behind one another in time and exchange their runs
 // through LDS; each then knows the state before its first token and goes over its registers once more.  So inputs are
-// read once and outputs written once, which is all that bounds it: a bf16 forward pass moves 6 bytes a token and channel
-// for some ten operations.
+// read once and outputs written once, which is what bounds it where there are many channels (a bf16 forward pass moves 6
+// bytes a token and channel for some ten operations): N32768 C4096 with fp32 decays 197 us, 5.4 TB/s, where a copy of
+// as many bytes runs at 5.1; B4 N4096 C2048 bf16 52 us, 3.9 TB/s, of which some 5 us are the looks back, 2 the tickets
+// and 2 the clearing of the workspace before it (parts left out, 55.7 -> 50.6 -> 47.0 -> 44.6).  Tried and slower:
+// workgroups that stay and load the next tile during the look back (61 and 227 us: a tile's run is published only when the
+// tile before it is done).
 //
 // Packed sequences: where a sequence begins, the run so far is cut off.  That is decided by the offsets alone, so it
 // is the same for all channels and no arithmetic carries anything over (zero times an infinity would).
@@ -25,13 +29,7 @@ namespace leet {
 // A tile: tokens of a wave, and waves of a workgroup that hold tokens (at most); one more wave links the tile to the others.
 // Workgroups of 8, 12 or 16 waves spread evenly over the four SIMDs of a compute unit (B4 N4096 C2048 forward: 16 tokens x 7
 // waves 57 us, 16 x 5 68, 12 x 9 71; backward 8 x 11 93, 8 x 9 102).
-struct ForwardTile {
-    static constexpr int kTokens = 16;
-};
-struct BackwardTile {
-    static constexpr int kTokens = 8;
-};
-constexpr int kMostWaves = 15;
+constexpr int kForwardTokens = 16, kBackwardTokens = 8, kMostWaves = 15;
 
 // The decay a and, for the moving average, 1 - a (each as accurate as the smaller of the two: the larger one is what that
 // leaves of 1).
@@ -149,8 +147,8 @@ __device__ __forceinline__ float through(uint64_t run, float s) {
     return (uint32_t)run == kCut ? high(run) : fmaf(low(run), s, high(run));
 }
 
-// Workspace: kGroups lines, each with a ticket counter, then of every tile the runs of its channels (A, H: eight bytes a channel),
-// then of every tile the inclusive states of its channels, four bytes a channel in pairs (a lone channel: twice itself).
+// Workspace: kGroups lines, each with a ticket counter, then of every tile the runs of its channels (A, H: eight bytes a
+// channel), then of every tile the inclusive states of its channels, four bytes a channel in pairs (a lone one: twice itself).
 struct Board {
     uint64_t *runs, *states;
     long long tile;  // words of a tile's runs
@@ -221,22 +219,31 @@ struct Board {
 
     // The state behind tile k of the chain: looks back until it meets a tile whose state is known, waiting for those that
     // have published nothing, and goes forward from there over the runs.  So it is the same chain of fused multiply-adds
-    // whatever was known when: results do not depend on timing.  Every wait ends: a tile publishes its run (or its state)
-    // without waiting for anything, and tiles are taken in the order of the chain, so all that are waited for belong to
-    // workgroups that are running already.
+    // whatever was known when: results do not depend on timing.  Every wait ends: a tile publishes its run (the first tile
+    // its state) without waiting for anything, and tiles are taken in the order of the chain, so all that are waited for
+    // belong to workgroups that are running already.  That holds while the workspace is this launch's alone; kPatience
+    // ends the wait, with NaN for the state, where it is not: some seconds of looks, a million times what a wait takes.
+    static constexpr int kPatience = 1 << 22;
     template <int kV>
     __device__ __forceinline__ void state_behind(int k, bool live, float* state) const {
         constexpr int kTiles = Window<kV>::kTiles;
         Window<kV> near, far;
+        int looks = 0;
         do near.load(*this, k, live);
-        while (!near.ended && near.runs < kTiles);
+        while (!near.ended && near.runs < kTiles && ++looks < kPatience);
         zero<kV>(state);
         if (!near.ended) {
             int j = k - kTiles;
-            while (true) {
+            while (looks < kPatience) {
                 far.load(*this, j, live);
                 if (far.ended) break;
                 j -= far.runs;
+                ++looks;
+            }
+            if (looks >= kPatience) {
+#pragma unroll
+                for (int v = 0; v < kV; ++v) state[v] = __builtin_bit_cast(float, 0x7fc00000u);
+                return;
             }
             far.fold(state);
             // tiles j + 1 .. k - kTiles, whose runs have all been seen; the last window of them may be a short one
@@ -385,7 +392,7 @@ __device__ __forceinline__ void pass_on(const GatedScanParams& p, const float* f
 // Workgroup = one tile of waves * kTokens tokens x 64 kV channels of one batch entry.
 template <int kX, int kG, int kMode, int kV, bool kPacked>
 __global__ __launch_bounds__(64 * (kMostWaves + 1)) void gated_scan_kernel(GatedScanParams p) {
-    constexpr int kTokens = ForwardTile::kTokens;
+    constexpr int kTokens = kForwardTokens;
     __shared__ Shared<kV> shared;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int block, k;
@@ -460,7 +467,7 @@ __global__ __launch_bounds__(64 * (kMostWaves + 1)) void gated_scan_kernel(Gated
 // token to the one that goes out before its first.
 template <int kX, int kG, int kMode, int kV, bool kPacked>
 __global__ __launch_bounds__(64 * (kMostWaves + 1)) void gated_scan_backward_kernel(GatedScanParams p) {
-    constexpr int kTokens = BackwardTile::kTokens;
+    constexpr int kTokens = kBackwardTokens;
     __shared__ Shared<kV> shared;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int block, k;
@@ -615,7 +622,7 @@ static int waves_of(const GatedScanParams& p, bool backward, int mode) {
 // sequences, the most bytes.
 static size_t plan_scan(GatedScanParams* p, bool backward, int mode) {
     const int v = p->C > 1 ? 2 : 1;
-    const int tokens = backward ? BackwardTile::kTokens : ForwardTile::kTokens;
+    const int tokens = backward ? kBackwardTokens : kForwardTokens;
     p->columns = (p->C + 64 * v - 1) / (64 * v);
     const long long chains = (long long)p->B * p->columns;
     const int need = (p->N + tokens - 1) / tokens, most = mode >= 0 ? waves_of(*p, backward, mode) : backward ? kBackwardWaves : kForwardWaves;

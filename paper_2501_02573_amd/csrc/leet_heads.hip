@@ -5,17 +5,18 @@
 //     y = R (w .* x r),  r = 1 / sqrt(mean(x^2) + eps)
 //     du = R^T dy,  n = x r:   dx = r (w .* du - n mean(w .* du .* n)),   dw = sum of du .* n over tokens and heads
 //
-// Bound by memory: a row is read once and written once (2 d elements; backward 3 d).  Everything a row needs is
-// arranged so that nothing else is read twice and no value crosses a workgroup:
+// Bound by memory: a row is read once and written once (2 d elements; backward 3 d).  B4 N4096 H16+16 d128 bf16: forward 51
+// us, 5.3 TB/s, backward 78 us, 5.2 TB/s, where a copy of that size runs at 5.1.  Everything a row needs is arranged so
+// that nothing else is read twice and no value crosses a workgroup:
 //
-// * A row of d elements lies in L = d / 16 neighbouring lanes, sixteen elements a lane in two pieces of eight (two
-//   16-byte accesses of a 16-bit type).  With the half layout the pieces are rot / 2 apart, so both elements of every
-//   pair are in one lane; with the interleaved layout they are adjacent.  The sums over a row are then DPP adds over
-//   L lanes.
-// * A wave holds 64 / L tokens and walks over some heads of them, so the cosines and sines, which depend on the token
-//   only, are formed once a wave: in fp64 up to the reduced angle (a product, two roundings), in fp32 from there.
-// * Rows that are not 16-byte aligned, or whose halves cannot be cut into pieces of eight, take the same kernel with
-//   pieces of one element (kV = 1), two pieces a lane and round.
+// * A row of d elements lies in L = d / 8 neighbouring lanes, eight elements a lane in two pieces of four.  With the half
+//   layout the pieces are rot / 2 apart, so both elements of every pair are in one lane; with the interleaved layout a
+//   pair is within a piece.  The sums over a row are then DPP adds over L lanes.
+// * A wave holds 64 / L tokens and walks over some heads of them, the next head's rows under way, so the cosines and sines,
+//   which depend on the token only, are formed once a wave: in fp64 up to the reduced angle (a product, two roundings), in
+//   fp32 from there.
+// * Rows whose halves cannot be cut into pieces of four take the same kernel with pieces of one element (kV = 1), two pieces
+//   a lane and round (rot 34 of d 128: 73, 90 and 143 us where rot 128 takes 49, 51 and 78).
 #include "leet_heads.hpp"
 #include "leet_io.hpp"
 

@@ -97,6 +97,11 @@ int heads_params(const HeadsCall& q, const HeadsCall& k, const leet_attn_rotatio
         r.weight_grad = c->weight_grad;
         r.H = c->H;
     }
+    // the outputs are two, and neither is the other's input
+    if (keys && (q.out->data == k.out->data || q.out->data == k.in->data || k.out->data == q.in->data ||
+                 (backward && (q.out->data == k.grad->data || k.out->data == q.grad->data))))
+        return LEET_ERR_INVALID_ARG;
+    if (q.weight_grad && q.weight_grad == k.weight_grad) return LEET_ERR_INVALID_ARG;
     p->freq = rotation->freq;
     p->positions = rotation->positions;
     p->positions_batch = rotation->positions_batch;

@@ -69,7 +69,7 @@ P = 0x100000   # aligned, never touched
 def _heads_args(leet, **change):
     """Arguments of the three calls on heads, by name."""
     H = lambda at=P, b=1 << 20, h=1 << 14, n=128: leet._pack_heads(at, b, h, n)  # noqa: E731
-    a = dict(q=H(), out_q=H(2 * P), Hq=2, k=H(3 * P), out_k=H(4 * P), Hk=2, dq=H(5 * P), dk=H(6 * P), wq=P, wk=P, gq=P, gk=P,
+    a = dict(q=H(), out_q=H(2 * P), Hq=2, k=H(3 * P), out_k=H(4 * P), Hk=2, dq=H(5 * P), dk=H(6 * P), wq=P, wk=P, gq=P, gk=2 * P,
              wd=leet.LEET_BF16, eps=1e-6, rot=leet._pack_rotation(P, 64, 0, 0, 0, 0, 1.0), ws=P, wsb=1 << 40, B=2, N=16,
              d=128, dtype=leet.LEET_BF16)
     a.update(change)
@@ -124,6 +124,14 @@ def test_heads_refused(leet):
     assert _back(leet, _heads_args(leet, out_q=None)) == INVALID
     assert _back(leet, _heads_args(leet, dq=H(5 * P, 0, 1 << 14, 128))) == INVALID
     assert _back(leet, _heads_args(leet, gk=P + 1)) == INVALID
+    # two outputs at one place, or one over the other's input
+    for call in (_rope, _norm):
+        for change in (dict(out_k=H(2 * P, 1 << 20, 1 << 14, 128)), dict(out_q=H(3 * P, 1 << 20, 1 << 14, 128)),
+                       dict(out_k=H(P, 1 << 20, 1 << 14, 128))):
+            assert call(leet, _heads_args(leet, **change)) == INVALID, change
+    for change in (dict(dk=H(5 * P, 1 << 20, 1 << 14, 128)), dict(dq=H(4 * P, 1 << 20, 1 << 14, 128)),
+                   dict(dk=H(P, 1 << 20, 1 << 14, 128)), dict(gk=P, gq=P)):
+        assert _back(leet, _heads_args(leet, **change)) == INVALID, change
     # no tokens: legal, and nothing to do
     assert _rope(leet, _heads_args(leet, N=0)) == leet.LEET_OK
     assert _norm(leet, _heads_args(leet, N=0)) == leet.LEET_OK
