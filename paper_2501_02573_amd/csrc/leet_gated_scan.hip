@@ -31,19 +31,27 @@ namespace leet {
 // waves 57 us, 16 x 5 68, 12 x 9 71; backward 8 x 11 93, 8 x 9 102).
 constexpr int kForwardTokens = 16, kBackwardTokens = 8, kMostWaves = 15;
 
-// The decay a and, for the moving average, 1 - a (each as accurate as the smaller of the two: the larger one is what that
-// leaves of 1).
+// A gate as it is kept between its two uses, in one register: the decay a itself, or for the moving average the smaller of
+// a and 1 - a with the sign of the logit.  The larger one is what that leaves of 1, so both are as accurate as fp32 has
+// them however near 0 or 1 they are.
 template <int kMode>
-__device__ __forceinline__ void decay(float z, float& a, float& rest) {
-    if constexpr (kMode == 0) a = z;
-    else if constexpr (kMode == 1) a = expf(z);
-    else {
-        const float e = expf(-fabsf(z));
-        const float small = e * __builtin_amdgcn_rcpf(1.0f + e), large = 1.0f - small;
-        a = z >= 0.0f ? large : small;
-        rest = z >= 0.0f ? small : large;
+struct Gate {
+    float g;
+
+    __device__ __forceinline__ void set(float z) {
+        if constexpr (kMode == 0) g = z;
+        else if constexpr (kMode == 1) g = expf(z);
+        else {
+            const float e = expf(-fabsf(z));
+            g = copysignf(e * __builtin_amdgcn_rcpf(1.0f + e), z);
+        }
     }
-}
+    __device__ __forceinline__ bool below() const { return __builtin_bit_cast(int, g) < 0; }  // a logit below 0
+    __device__ __forceinline__ float decay() const { return kMode != 2 ? g : below() ? -g : 1.0f - g; }
+    __device__ __forceinline__ float rest() const { return kMode != 2 ? 1.0f : below() ? 1.0f + g : g; }
+    // b of an input
+    __device__ __forceinline__ float input(float x) const { return kMode != 2 ? x : rest() * x; }
+};
 
 // Where the tokens t0 .. t0 + kTokens - 1 lie among packed sequences.  Lane i < kTokens looks at token t0 + i.  A token's
 // sequence is the last one that begins at or before it: of empty ones at one place the one behind them.
@@ -389,9 +397,11 @@ __device__ __forceinline__ void pass_on(const GatedScanParams& p, const float* f
         }
 }
 
-// Workgroup = one tile of waves * kTokens tokens x 64 kV channels of one batch entry.
+// Workgroup = one tile of waves * kTokens tokens x 64 kV channels of one batch entry.  Six waves a SIMD, three workgroups of
+// eight waves a unit, where the inputs' registers allow it (us with six and four: B4 N4096 C2048 50 51, its sigmoid 55 59,
+// N32768 C4096 sigmoid 185 207; with fp32 gates 206 200).
 template <int kX, int kG, int kMode, int kV, bool kPacked>
-__global__ __launch_bounds__(64 * (kMostWaves + 1)) void gated_scan_kernel(GatedScanParams p) {
+__global__ __launch_bounds__(64 * (kMostWaves + 1), kX != 0 && kG != 0 && !kPacked ? 6 : 4) void gated_scan_kernel(GatedScanParams p) {
     constexpr int kTokens = kForwardTokens;
     __shared__ Shared<kV> shared;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -416,7 +426,11 @@ __global__ __launch_bounds__(64 * (kMostWaves + 1)) void gated_scan_kernel(Gated
             x[i].load(row_at<kX>(p.x, b, t, c));
         }
     const Places<kTokens> at = kPacked ? Places<kTokens>(p.offsets, p.sequences, t0, p.N, lane) : Places<kTokens>{};
-    float a[kTokens][kV], h[kTokens][kV], A[kV], H[kV];
+    Gate<kMode> g[kTokens][kV];
+    // b with what enters a sequence; without packed sequences it is the input, kept as it was loaded (half the registers:
+    // three workgroups a compute unit instead of two)
+    float h[kPacked ? kTokens : 1][kV];
+    float A[kV], H[kV];
 #pragma unroll
     for (int v = 0; v < kV; ++v) { A[v] = 1.0f; H[v] = 0.0f; }
 #pragma unroll
@@ -426,22 +440,24 @@ __global__ __launch_bounds__(64 * (kMostWaves + 1)) void gated_scan_kernel(Gated
         float enters[kV];
         if (first && live) load_state<kV>(p.state_in, at.of(i), p.C, c, enters);
         else zero<kV>(enters);
-        z[i].get(a[i]);
-        x[i].get(h[i]);
+        float zi[kV], xi[kV];
+        z[i].get(zi);
+        x[i].get(xi);
 #pragma unroll
         for (int v = 0; v < kV; ++v) {
-            float rest = 1.0f;
-            decay<kMode>(a[i][v], a[i][v], rest);
-            if (kMode == 2) h[i][v] *= rest;
+            g[i][v].set(zi[v]);
+            const float a = g[i][v].decay();
+            float b = g[i][v].input(xi[v]);
             if (first) {
                 // the only place where the state is read: as soon as this run is known state_out, which may be the
                 // same memory, may be written
-                h[i][v] = fmaf(a[i][v], enters[v], h[i][v]);
-                H[v] = h[i][v];
+                b = fmaf(a, enters[v], b);
+                H[v] = b;
             } else {
-                H[v] = fmaf(a[i][v], H[v], h[i][v]);
-                A[v] *= a[i][v];
+                H[v] = fmaf(a, H[v], b);
+                A[v] *= a;
             }
+            if (kPacked) h[i][v] = b;
         }
     }
     float state[kV];
@@ -450,14 +466,16 @@ __global__ __launch_bounds__(64 * (kMostWaves + 1)) void gated_scan_kernel(Gated
     for (int i = 0; i < kTokens; ++i) {
         if (i >= count) continue;
         const bool first = kPacked && (at.first >> i & 1);
+        float xi[kV];
+        if (!kPacked) x[i].get(xi);
 #pragma unroll
         for (int v = 0; v < kV; ++v) {
-            state[v] = first ? h[i][v] : fmaf(a[i][v], state[v], h[i][v]);
-            h[i][v] = state[v];
+            const float b = kPacked ? h[i][v] : g[i][v].input(xi[v]);
+            state[v] = first ? b : fmaf(g[i][v].decay(), state[v], b);
         }
         if (live && (!kPacked || (at.inside >> i & 1))) {
-            store_channels<kX, kV>(p.out, b, t0 + i, c, h[i]);
-            if (kPacked && (at.last >> i & 1)) store_state<kV>(p.state_out, at.of(i), p.C, c, h[i]);
+            store_channels<kX, kV>(p.out, b, t0 + i, c, state);
+            if (kPacked && (at.last >> i & 1)) store_state<kV>(p.state_out, at.of(i), p.C, c, state);
         }
     }
     if (kPacked && live) pass_on<kV>(p, p.state_in, p.state_out, k, wave, c);
@@ -493,7 +511,8 @@ __global__ __launch_bounds__(64 * (kMostWaves + 1)) void gated_scan_backward_ker
             if (kMode == 2) x[i].load(row_at<kX>(p.x, b, t, c));
         }
     const Places<kTokens> at = kPacked ? Places<kTokens>(p.offsets, p.sequences, t0, p.N, lane) : Places<kTokens>{};
-    float a[kTokens][kV], d[kTokens][kV], rest[kTokens][kV], A[kV], G[kV];
+    Gate<kMode> gate[kTokens][kV];
+    float d[kTokens][kV], A[kV], G[kV];
 #pragma unroll
     for (int v = 0; v < kV; ++v) { A[v] = 1.0f; G[v] = 0.0f; }
 #pragma unroll
@@ -503,17 +522,19 @@ __global__ __launch_bounds__(64 * (kMostWaves + 1)) void gated_scan_backward_ker
         float leaves[kV];
         if (last && live) load_state<kV>(p.dstate_out, at.of(i), p.C, c, leaves);
         else zero<kV>(leaves);
-        z[i].get(a[i]);
+        float zi[kV];
+        z[i].get(zi);
         dh[i].get(d[i]);
 #pragma unroll
         for (int v = 0; v < kV; ++v) {
-            decay<kMode>(a[i][v], a[i][v], rest[i][v]);
+            gate[i][v].set(zi[v]);
+            const float a = gate[i][v].decay();
             if (last) {
                 d[i][v] += leaves[v];
-                G[v] = a[i][v] * d[i][v];
+                G[v] = a * d[i][v];
             } else {
-                G[v] = a[i][v] * (d[i][v] + G[v]);
-                A[v] *= a[i][v];
+                G[v] = a * (d[i][v] + G[v]);
+                A[v] *= a;
             }
         }
     }
@@ -530,10 +551,11 @@ __global__ __launch_bounds__(64 * (kMostWaves + 1)) void gated_scan_backward_ker
 #pragma unroll
         for (int v = 0; v < kV; ++v) {
             const float D = last ? d[i][v] : d[i][v] + g[v];
-            g[v] = a[i][v] * D;
+            const float rest = gate[i][v].rest();
+            g[v] = gate[i][v].decay() * D;
             if (kMode == 0) { dgate[v] = D * before[v]; dx[v] = D; }
             else if (kMode == 1) { dgate[v] = g[v] * before[v]; dx[v] = D; }
-            else { dgate[v] = g[v] * rest[i][v] * (before[v] - xi[v]); dx[v] = D * rest[i][v]; }
+            else { dgate[v] = g[v] * rest * (before[v] - xi[v]); dx[v] = D * rest; }
         }
         store_channels<kX, kV>(p.dx, b, t0 + i, c, dx);
         store_channels<kG, kV>(p.dgate, b, t0 + i, c, dgate);
@@ -548,16 +570,16 @@ __global__ __launch_bounds__(256) void gated_step_kernel(GatedScanParams p) {
     const uint32_t c = (blockIdx.x * 256 + threadIdx.x) * kV;
     if (c >= (uint32_t)p.C) return;
     for (int b = blockIdx.y; b < p.B; b += gridDim.y) {
-        float a[kV], x[kV], s[kV];
-        Io<kG>::template load<kV>(row_at<kG>(p.gate, b, 0, c), a);
+        float z[kV], x[kV], s[kV];
+        Io<kG>::template load<kV>(row_at<kG>(p.gate, b, 0, c), z);
         Io<kX>::template load<kV>(row_at<kX>(p.x, b, 0, c), x);
         char* state = reinterpret_cast<char*>(p.state_out + (size_t)b * p.C + c);
         Io<0>::load<kV>(state, s);
 #pragma unroll
         for (int v = 0; v < kV; ++v) {
-            float rest = 1.0f;
-            decay<kMode>(a[v], a[v], rest);
-            s[v] = fmaf(a[v], s[v], kMode == 2 ? rest * x[v] : x[v]);
+            Gate<kMode> g;
+            g.set(z[v]);
+            s[v] = fmaf(g.decay(), s[v], g.input(x[v]));
         }
         Io<0>::store<kV>(state, s);
         Io<kX>::template store<kV>(p.out.data + (b * p.out.batch + c) * Io<kX>::kBytes, s);
@@ -606,26 +628,25 @@ static hipError_t launch_scan(const GatedScanParams& p, int elem, int gate_elem,
 }
 
 // Waves of a workgroup that hold tokens.  A chain advances a tile every 0.3 us, so where there are few chains long tiles
-// count; else what fits a compute unit twice does.  us with 7 | 11 | 15 waves, bf16: forward N20000 C1024 (8 chains) 65 47
-// 43, C2048 (16) 80 71 69, B2 N4096 C2048 (32) 31 32 33, B4 (64) 50 58 61, N32768 C4096 (32) 176 200 194; backward C1024 125
-// 86 72, B4 N4096 C2048 79 76 74, N32768 C4096 313 267 253; backward with x read too (sigmoid: 80 registers a lane, two
-// workgroups of 12 waves a unit but one of 16) C1024 122 88 77, C2048 151 121 128, B4 N4096 C2048 99 90 105.
-// Packed sequences are chains of their own (37 of them in N20011 C1001 forward: 54 | - | 60).
-constexpr int kForwardWaves = 7, kBackwardWaves = 11;  // the fewest, where there are tokens for them
-static int waves_of(const GatedScanParams& p, bool backward, int mode) {
+// count; else that several workgroups fit a compute unit.  us with 7 | 11 | 15 waves, bf16: forward N20000 C1024 (8 chains)
+// 65 47 43, C2048 (16) 80 71 69, B2 N4096 C2048 (32) 31 32 33, B4 (64) 50 58 61, N32768 C4096 (32) 176 200 194; backward
+// C1024 125 86 72, B4 N4096 C2048 79 76 74, N32768 C4096 313 267 253.  Packed sequences are chains of their own (37 of them
+// in N20011 C1001 forward: 54 - 60).
+constexpr int kForwardWaves = 7;
+static int waves_of(const GatedScanParams& p, bool backward) {
     const long long chains = (long long)p.B * p.columns * (p.offsets ? p.sequences : 1);
-    if (!backward) return chains <= 16 ? kMostWaves : kForwardWaves;
-    return mode != 2 || chains <= 8 ? kMostWaves : kBackwardWaves;
+    return !backward && chains > 16 ? kForwardWaves : kMostWaves;
 }
 
-// Column blocks, waves of a workgroup and tiles of N tokens; returns the bytes of workspace.  mode < 0: any mode, any
-// sequences, the most bytes.
-static size_t plan_scan(GatedScanParams* p, bool backward, int mode) {
+// Column blocks, waves of a workgroup and tiles of N tokens; returns the bytes of workspace.
+// most: the waves, or 0 for what the sizes ask for; the fewest give the most bytes, room for any sequences.
+static size_t plan_scan(GatedScanParams* p, bool backward, int most) {
     const int v = p->C > 1 ? 2 : 1;
     const int tokens = backward ? kBackwardTokens : kForwardTokens;
     p->columns = (p->C + 64 * v - 1) / (64 * v);
     const long long chains = (long long)p->B * p->columns;
-    const int need = (p->N + tokens - 1) / tokens, most = mode >= 0 ? waves_of(*p, backward, mode) : backward ? kBackwardWaves : kForwardWaves;
+    const int need = (p->N + tokens - 1) / tokens;
+    if (most == 0) most = waves_of(*p, backward);
     p->waves = need < 1 ? 1 : need < most ? need : most;  // no tokens: one that hands the states on
     p->tiles = need < 1 ? 1 : (need + p->waves - 1) / p->waves;
     for (p->groups = Board::kGroups; chains % p->groups != 0;) p->groups /= 2;
@@ -635,18 +656,18 @@ static size_t plan_scan(GatedScanParams* p, bool backward, int mode) {
 size_t gated_scan_workspace(int B, int N, int C, bool backward) {
     GatedScanParams p = {};
     p.B = B; p.N = N; p.C = C;
-    return plan_scan(&p, backward, -1);
+    return plan_scan(&p, backward, backward ? kMostWaves : kForwardWaves);
 }
 
 long long gated_scan_threads(int B, int N, int C, bool backward) {
     GatedScanParams p = {};
     p.B = B; p.N = N; p.C = C;
-    plan_scan(&p, backward, -1);
+    plan_scan(&p, backward, backward ? kMostWaves : kForwardWaves);
     return ((long long)p.B * p.columns * p.tiles + Board::kGroups * 8) * (kMostWaves + 1) * 64;
 }
 
 static hipError_t launch_sequences(GatedScanParams& p, int elem, int gate_elem, int mode, int which, hipStream_t stream) {
-    const size_t bytes = plan_scan(&p, which != 0, mode);
+    const size_t bytes = plan_scan(&p, which != 0, 0);
     if (bytes) {
         const size_t words = (bytes + 15) / 16;
         hipLaunchKernelGGL(gated_scan_clear_kernel, dim3((unsigned)((words + 255) / 256)), dim3(256), 0, stream,
