@@ -707,8 +707,8 @@ def _on(*tensors: Optional[torch.Tensor]) -> int:
     for t in tensors:
         if t is None:
             continue
-        at = t.get_device()
-        if at < 0 or not t.is_cuda:
+        at = t.get_device()  # -1 for host memory
+        if at < 0:
             raise ValueError("all tensors must be GPU tensors")
         if index is None:
             index = at

@@ -109,7 +109,7 @@ def _offsets(lengths):
 
 
 PACKS = [[5], [1, 1, 1], [0, 3, 0, 0, 20, 0], [16, 16, 32], [15, 17, 256, 1], [300, 0, 2, 700], [255, 1, 256, 0, 0, 90],
-         [0, 0, 0], [3] * 100, [1000, 24]]
+         [0, 0, 0], [3] * 100, [1000, 24], [0] * 150 + [5] + [0] * 70 + [9, 0, 0, 1] * 20, [0, 1, 2, 3] * 700]
 
 
 @pytest.mark.parametrize("types", [(BF16, BF16), (F16, F32), (F32, F32)])
@@ -184,9 +184,10 @@ def test_ends_of_the_gates(leet):
         _check(leet, 1, 300, 64, (F32, F32), mode, True, gate=z)
 
 
+@pytest.mark.parametrize("C", [96, 97])
 @pytest.mark.parametrize("packed", [False, True])
-def test_states_in_place(leet, packed):
-    N, C = 1500, 96
+def test_states_in_place(leet, packed, C):
+    N = 1500
     off = _offsets([700, 0, 1, 799]).cuda() if packed else None
     x, z = _normal((1, N, C), BF16, 80), _gate((1, N, C), F32, 1, 81)
     s = _normal((4 if packed else 1, C), F32, 82)
@@ -353,3 +354,43 @@ def test_offsets_beyond_32_bits(leet):
     x.copy_(_normal((1, N, C), BF16, 150))
     gate.copy_(_gate((1, N, C), BF16, 1, 151))
     _check(leet, 1, N, C, (BF16, BF16), 1, True, x=x, gate=gate, into=out)
+
+
+def test_a_gate_shared_by_the_batch(leet):
+    B, N, C = 3, 70, 66
+    gate = _gate((1, N, C), BF16, 1, 160).expand(B, N, C)
+    _check(leet, B, N, C, (BF16, BF16), 1, True, gate=gate)
+
+
+def test_a_hundred_thousand_sequences(leet):
+    _check(leet, 100000, 2, 3, (BF16, F32), 0, True)
+    x, z, s = _normal((100000, 3), BF16, 161), _gate((100000, 3), BF16, 2, 162), _normal((100000, 3), F32, 163)
+    want, last = forms.scan(_f64(z)[:, None], _f64(x)[:, None], 2, _f64(s))
+    out = leet.leet_attn_gated_scan_step(x, z, s, mode=2)
+    assert forms.close(out, (want[0][:, 0], want[1][:, 0])) and forms.close(s, last)
+
+
+def test_no_sequences(leet):
+    x = _normal((1, 20, 8), BF16, 164)
+    out, off = torch.full_like(x, 7.0), torch.zeros(1, dtype=torch.int32, device="cuda")
+    leet.leet_attn_gated_scan(x, x, out=out, offsets=off, state_in=torch.empty((0, 8), device="cuda"))
+    assert bool((out == 7).all())
+
+
+def test_offsets_that_no_sequences_have(leet):
+    """Falling offsets, ones beyond the rows and below zero: wrong rows, but nothing outside them is touched and the call
+    ends."""
+    N, C = 600, 70
+    x, z = _normal((1, N, C), BF16, 165), _gate((1, N, C), BF16, 1, 166)
+    for bad in ([0, 500, 100, 600], [0, 10, 100000, 200000], [-50, -20, 300, 600], [400, 300, 200, 100], [600, 600, 600, 600]):
+        off = torch.tensor(bad, dtype=torch.int32, device="cuda")
+        room = torch.full((1, N + 64, C), 7.0, dtype=BF16, device="cuda")
+        states = torch.full((3 + 4, C), 5.0, device="cuda")
+        leet.leet_attn_gated_scan(x, z, out=room[:, 32:N + 32], state_out=states[2:5], offsets=off)
+        h = room[:, 32:N + 32]
+        dx, dz = torch.full_like(room, 7.0), torch.full_like(room, 7.0)
+        leet.leet_attn_gated_scan_backward(x, None, z, h, dx=dx[:, 32:N + 32], dgate=dz[:, 32:N + 32], offsets=off,
+                                           dstate_in=states[2:5])
+        for t in (room, dx, dz):
+            assert bool((t[:, :32] == 7).all()) and bool((t[:, N + 32:] == 7).all())
+        assert bool((states[:2] == 5).all()) and bool((states[5:] == 5).all())
