@@ -804,6 +804,9 @@ def _heads_pair(q: torch.Tensor, k: Optional[torch.Tensor]):
 
 
 def _new_dense(like: torch.Tensor) -> torch.Tensor:
+    """A fresh dense tensor of ``like``'s shape, device and type."""
+    if type(like) is _Tensor and like.is_contiguous():  # the least that torch has to look at
+        return _empty_like(like)
     return _new_out(like, like.dtype)
 
 

@@ -14,10 +14,11 @@
 // through LDS; each then knows the state before its first token and goes over its registers once more.  So inputs are
 // read once and outputs written once, which is what bounds it where there are many channels (a bf16 forward pass moves 6
 // bytes a token and channel for some ten operations): N32768 C4096 with fp32 decays 197 us, 5.4 TB/s, where a copy of
-// as many bytes runs at 5.1; B4 N4096 C2048 bf16 52 us, 3.9 TB/s, of which some 5 us are the looks back, 2 the tickets
-// and 2 the clearing of the workspace before it (parts left out, 55.7 -> 50.6 -> 47.0 -> 44.6).  Tried and slower:
-// workgroups that stay and load the next tile during the look back (61 and 227 us: a tile's run is published only when the
-// tile before it is done).
+// as many bytes runs at 5.1; B4 N4096 C2048 bf16 51 us, 3.9 TB/s, of which some 5 us are the looks back, 1 the tickets
+// and 2 the clearing of the workspace before it (measured by leaving parts out).  Tried and slower: workgroups that stay
+// and load the next tile during the look back (61 and 227 us: a tile's run is published only when the tile before it is
+// done); a copy of both passes without branches for waves whose tokens are all there (51 us, but backward 105 instead of
+// 92: registers).
 //
 // Packed sequences: where a sequence begins, the run so far is cut off.  That is decided by the offsets alone, so it
 // is the same for all channels and no arithmetic carries anything over (zero times an infinity would).
@@ -33,7 +34,7 @@ constexpr int kForwardTokens = 16, kBackwardTokens = 8, kMostWaves = 15;
 
 // A gate as it is kept between its two uses, in one register: the decay a itself, or for the moving average the smaller of
 // a and 1 - a with the sign of the logit.  The larger one is what that leaves of 1, so both are as accurate as fp32 has
-// them however near 0 or 1 they are.
+// them however near 0 or 1 they are (the quotient is v_rcp_f32's, within a step).
 template <int kMode>
 struct Gate {
     float g;

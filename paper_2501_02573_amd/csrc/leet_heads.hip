@@ -423,11 +423,13 @@ static int row_log(const HeadsParams& p) { return !p.vector ? 6 : kPieceLog + (p
 
 // Heads a wave takes: the more, the fewer angles are formed twice; the fewer, the more waves there are.  Rows from memory
 // want 64 waves a compute unit (16 and 64: forward B4 N4096 H16+16 d128 57 and 51 us, backward 92 and 78), rows from the
-// cache 16 (forward B3 N1777 H32+8 d64 14.5 and 18).
+// cache 16 (forward B3 N1777 H32+8 d64 with 4, 16, 64: 14.8 13.3 18, B4 N1024 H16+16 d128 15.3 13.7 -) or, backward, where a
+// workgroup ends with a sum over its waves, 4 (B2 N2047 H8+8 d64 fp32 with 4, 16, 32: 14.8 18.4 20.7, B4 N1024 H16+16 d128
+// 24.3 23.7 23.4).
 void plan_heads(HeadsParams* p, bool backward) {
     const long tokens = 64 >> row_log(*p);
     const long groups = (p->tokens + tokens - 1) / tokens;  // waves that one head a wave needs
-    const long want = (p->stream ? 64 : 16) * kComputeUnits;
+    const long want = (p->stream ? 64 : backward ? 4 : 16) * kComputeUnits;
     const int most = p->q.H > p->k.H ? p->q.H : p->k.H;
     int heads = 16;
     while (heads > 1 && groups * ((p->q.H + heads - 1) / heads + (p->k.H + heads - 1) / heads) < want) heads /= 2;
