@@ -378,12 +378,20 @@ __device__ __forceinline__ void join_runs(const GatedScanParams& p, S& shared, i
 }
 
 // The first channel of a lane.  The last pair of an odd number of channels begins one channel early: that channel is then
-// computed and stored twice, the same both times.  Lanes past the end (false) load what the last pair loads.
+// computed and stored twice, the same both times.  The lane before does so too, and has to be in the same wave: where states
+// are updated in place, another workgroup could have written that channel's before this one reads it.  So where the last
+// column has one channel, it takes the last pair of the column before it over.  Lanes past the end (false) load what the last
+// pair loads.
 template <int kV>
 __device__ __forceinline__ bool channel_of(const GatedScanParams& p, int column, int lane, uint32_t* c) {
-    const uint32_t at = (uint32_t)(column * 64 + lane) * kV;
-    *c = min(at, (uint32_t)(p.C - kV));
-    return at < (uint32_t)p.C;
+    int at = (column * 64 + lane) * kV;
+    bool live = true;
+    if (kV == 2 && p.C % (64 * kV) == 1) {
+        if (column == p.columns - 1) at -= kV;
+        else live = column < p.columns - 2 || lane < 63;
+    }
+    *c = min((uint32_t)at, (uint32_t)(p.C - kV));
+    return live && at < p.C;
 }
 
 // States of empty packed sequences are handed on; the sequences are spread over the tiles and waves.

@@ -300,6 +300,27 @@ def test_on_another_stream_and_in_a_graph(leet):
         assert all(torch.equal(a, b) for a, b in zip(eager, seen))
 
 
+@pytest.mark.parametrize("C", [129, 257, 127])
+@pytest.mark.parametrize("packed", [False, True])
+def test_many_states_in_place_where_a_lone_channel_is_left(leet, packed, C):
+    """An odd number of channels leaves one without a neighbour.  Whoever takes it must not go by a neighbour's state that
+    another workgroup may have written already."""
+    S, N = 30000, 3
+    shape = (1, S * N, C) if packed else (S, N, C)
+    off = (torch.arange(S + 1, dtype=torch.int32) * N).cuda() if packed else None
+    x, z, dh = _normal(shape, BF16, 150), _gate(shape, BF16, 1, 151), _normal(shape, BF16, 152)
+    s, ds = _normal((S, C), F32, 153, 3.0), _normal((S, C), F32, 154, 3.0)
+    left, din = torch.empty_like(s), torch.empty_like(s)
+    h = leet.leet_attn_gated_scan(x, z, state_in=s, state_out=left, offsets=off)
+    dx, dz = leet.leet_attn_gated_scan_backward(dh, None, z, h, state_in=s, dstate_out=ds, dstate_in=din, offsets=off)
+    for _ in range(3):
+        kept, dkept = s.clone(), ds.clone()
+        got = leet.leet_attn_gated_scan(x, z, state_in=kept, state_out=kept, offsets=off)
+        dgot = leet.leet_attn_gated_scan_backward(dh, None, z, h, state_in=s, dstate_out=dkept, dstate_in=dkept, offsets=off)
+        assert torch.equal(got, h) and torch.equal(kept, left)
+        assert torch.equal(dgot[0], dx) and torch.equal(dgot[1], dz) and torch.equal(dkept, din)
+
+
 @pytest.mark.parametrize("packed", [False, True])
 def test_equal_from_call_to_call(leet, packed):
     """Which tiles have published what when another looks back is a matter of timing; results are not."""
