@@ -503,6 +503,7 @@ size_t leet_attn_gated_scan_workspace_bytes(int B, int N, int C, int backward);
 /*
  * One token of every sequence: state <- a state + b, out = state (rounded).
  *   x, gate, out  [B][C], row b at data + b*batch (`token` is ignored);  state  [B][C] float, in place
+ *   out may be x, or a gate of its type (same data and stride), and must not overlap anything else
  */
 int leet_attn_gated_scan_step(const leet_attn_rows *x, const leet_attn_rows *gate, const leet_attn_rows *out,
                               float *state, int B, int C, int dtype, int gate_dtype, int mode, void *stream);

@@ -788,7 +788,14 @@ def _rotation(freq: torch.Tensor, layout: int, positions: Optional[torch.Tensor]
     return _pack_rotation(freq.data_ptr(), 2 * freq.shape[0], layout, at, stride, pos0, scale)
 
 
-def _heads_pair(q: torch.Tensor, k: Optional[torch.Tensor]):
+def _sizes(where: str, *sizes: int) -> None:
+    """Refuses sizes that would not arrive at the library as they are."""
+    for n in sizes:
+        if n > 0x7fffffff:
+            raise LeetAttnError(LEET_ERR_TOO_LARGE, where)
+
+
+def _heads_pair(q: torch.Tensor, k: Optional[torch.Tensor], where: str):
     """B, Hq, Hk, N, d of queries and keys."""
     if q.dim() != 4 or (k is not None and k.dim() != 4):
         raise ValueError("q and k must be [B, H, N, d]")
@@ -800,6 +807,7 @@ def _heads_pair(q: torch.Tensor, k: Optional[torch.Tensor]):
         if k.dtype != q.dtype:
             raise TypeError("q and k must share one dtype")
         Hk = k.shape[1]
+    _sizes(where, B, Hq, Hk, N, d)
     return B, Hq, Hk, N, d
 
 
@@ -819,7 +827,7 @@ def leet_attn_rope(q: torch.Tensor, freq: torch.Tensor, k: Optional[torch.Tensor
     The first ``2 * len(freq)`` elements of each row are rotated by the token's position (``positions`` or the token's
     number, plus ``pos0``).  ``transposed`` takes gradients of the outputs to gradients of the inputs.  Returns out_q,
     or (out_q, out_k); an output may be its input."""
-    B, Hq, Hk, N, d = _heads_pair(q, k)
+    B, Hq, Hk, N, d = _heads_pair(q, k, "leet_attn_rope")
     if out_q is None:
         out_q = _new_dense(q)
     if k is None:
@@ -862,7 +870,7 @@ def leet_attn_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, q_weight: Optional[
                            out_k: Optional[torch.Tensor] = None):
     """Norm of every head of q [B, Hq, N, d] and k [B, Hk, N, d], times its weight [d], then the rotation of
     ``leet_attn_rope``, in one pass.  Returns (out_q, out_k): dense [B, H, N, d], as the prefill reads them, unless given."""
-    B, Hq, Hk, N, d = _heads_pair(q, k)
+    B, Hq, Hk, N, d = _heads_pair(q, k, "leet_attn_qk_norm_rope")
     weight_dtype = _weights(q, q_weight, k_weight, d)
     if out_q is None:
         out_q = _new_dense(q)
@@ -891,7 +899,7 @@ def leet_attn_qk_norm_rope_backward(dout_q: torch.Tensor, dout_k: torch.Tensor, 
                                     workspace: Optional[torch.Tensor] = None):
     """Gradients of ``leet_attn_qk_norm_rope``: (dx_q, dx_k, dq_weight, dk_weight) from those of its outputs and its
     inputs.  A weight that is None has the gradient None."""
-    B, Hq, Hk, N, d = _heads_pair(q, k)
+    B, Hq, Hk, N, d = _heads_pair(q, k, "leet_attn_qk_norm_rope_backward")
     weight_dtype = _weights(q, q_weight, k_weight, d)
     grads = []
     for w, g, name in ((q_weight, dq_weight, "dq_weight"), (k_weight, dk_weight, "dk_weight")):
@@ -963,6 +971,7 @@ def leet_attn_gated_scan(x: torch.Tensor, gate: torch.Tensor, mode: int = GATE_L
     States are float32 [B, C]; with ``offsets`` (int32 [S + 1], B = 1: packed sequences) [S, C]."""
     S = _scan_sequences(x.shape, offsets)
     B, N, C = x.shape
+    _sizes("leet_attn_gated_scan", B, N, C, S)
     _scan_states(S, C, state_in=state_in, state_out=state_out)
     if out is None:
         out = _new_dense(x)
@@ -989,6 +998,7 @@ def leet_attn_gated_scan_backward(dh: torch.Tensor, x: Optional[torch.Tensor], g
     read with GATE_SIGMOID only and may be None otherwise."""
     S = _scan_sequences(h.shape, offsets)
     B, N, C = h.shape
+    _sizes("leet_attn_gated_scan_backward", B, N, C, S)
     _scan_states(S, C, state_in=state_in, dstate_out=dstate_out, dstate_in=dstate_in)
     if mode == GATE_SIGMOID and x is None:
         raise ValueError("GATE_SIGMOID needs x")
@@ -1016,6 +1026,7 @@ def leet_attn_gated_scan_step(x: torch.Tensor, gate: torch.Tensor, state: torch.
     if x.dim() != 2:
         raise ValueError("x must be [B, C]")
     B, C = x.shape
+    _sizes("leet_attn_gated_scan_step", B, C)
     _scan_states(B, C, state=state)
     if out is None:
         out = _new_dense(x)

@@ -672,7 +672,9 @@ long long gated_scan_threads(int B, int N, int C, bool backward) {
     GatedScanParams p = {};
     p.B = B; p.N = N; p.C = C;
     plan_scan(&p, backward, backward ? kMostWaves : kForwardWaves);
-    return ((long long)p.B * p.columns * p.tiles + Board::kGroups * 8) * (kMostWaves + 1) * 64;
+    const long long chains = (long long)p.B * p.columns, wide = (kMostWaves + 1) * 64;
+    if (chains >= 1LL << 22) return chains * wide;  // too many by themselves; times the tiles might not fit
+    return (chains * p.tiles + Board::kGroups * 8) * wide;
 }
 
 static hipError_t launch_sequences(GatedScanParams& p, int elem, int gate_elem, int mode, int which, hipStream_t stream) {

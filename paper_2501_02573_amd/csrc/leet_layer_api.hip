@@ -10,6 +10,8 @@ namespace {
 
 // A launch has fewer than 2^32 threads.
 constexpr long long kMaxThreads = 1LL << 32;
+// Sums of heads, and of sequences, stay within an int.
+constexpr int kMaxHeads = 1 << 28, kMaxSequences = 1 << 30;
 
 int elem_of(int dtype) { return dtype == LEET_F32 ? 0 : dtype == LEET_BF16 ? 1 : 2; }
 bool dtype_ok(int dtype) { return dtype == LEET_F32 || dtype == LEET_BF16 || dtype == LEET_F16; }
@@ -53,6 +55,12 @@ bool heads_ok(const leet_attn_heads* t, int B, int H, int N, int d, size_t size,
     return !written || rows_apart(d, dims, 3);
 }
 
+// Whether an output at an input's address is that input, stride for stride.
+bool same_place_or_none(const leet_attn_heads* out, const leet_attn_heads* in, int B, int H, int N) {
+    return out->data != in->data || ((B == 1 || out->batch == in->batch) && (H == 1 || out->head == in->head) &&
+                                     (N == 1 || out->token == in->token));
+}
+
 struct HeadsCall {
     const leet_attn_heads *in, *grad, *out;
     int H;
@@ -70,7 +78,7 @@ int heads_params(const HeadsCall& q, const HeadsCall& k, const leet_attn_rotatio
     if (rotation->rot < 2 || rotation->rot > d || rotation->rot % 2 != 0) return LEET_ERR_INVALID_ARG;
     if (rotation->layout != LEET_ROPE_HALF && rotation->layout != LEET_ROPE_INTERLEAVED) return LEET_ERR_INVALID_ARG;
     if (!isfinite(rotation->scale) || !isfinite(eps) || eps < 0.0f) return LEET_ERR_INVALID_ARG;
-    if ((long long)B * N >= 1LL << 31) return LEET_ERR_TOO_LARGE;
+    if ((long long)B * N >= 1LL << 31 || q.H > kMaxHeads || (keys && k.H > kMaxHeads)) return LEET_ERR_TOO_LARGE;
     *p = leet::HeadsParams{};
     p->tokens = B * N;
     if (N == 0) return LEET_OK;
@@ -81,7 +89,9 @@ int heads_params(const HeadsCall& q, const HeadsCall& k, const leet_attn_rotatio
         if (c == &k && !keys) continue;
         if (!heads_ok(c->in, B, c->H, N, d, size, false) ||
             !heads_ok(c->out, B, c->H, N, d, size, true) ||
-            (backward && !heads_ok(c->grad, B, c->H, N, d, size, false)))
+            (backward && !heads_ok(c->grad, B, c->H, N, d, size, false)) ||
+            !same_place_or_none(c->out, c->in, B, c->H, N) ||
+            (backward && !same_place_or_none(c->out, c->grad, B, c->H, N)))
             return LEET_ERR_INVALID_ARG;
         if (!aligned(c->weight, weight_size) || !aligned(c->weight_grad, weight_size)) return LEET_ERR_INVALID_ARG;
         leet::HeadRows& r = c == &q ? p->q : p->k;
@@ -146,7 +156,8 @@ int scan_sizes_ok(const int* offsets, int sequences, const void* workspace, size
                   int backward, int* S) {
     if (B <= 0 || N < 0 || C <= 0) return LEET_ERR_INVALID_ARG;
     if (offsets && (B != 1 || sequences < 0 || !aligned(offsets, 4))) return LEET_ERR_INVALID_ARG;
-    if (N > 1 << 30 || C > 1 << 28 || leet::gated_scan_threads(B, N, C, backward != 0) >= kMaxThreads)
+    if (N > 1 << 30 || C > 1 << 28 || (offsets && sequences > kMaxSequences) ||
+        leet::gated_scan_threads(B, N, C, backward != 0) >= kMaxThreads)
         return LEET_ERR_TOO_LARGE;
     const size_t need = leet_attn_gated_scan_workspace_bytes(B, N, C, backward);
     if (need && (!workspace || workspace_bytes < need || !aligned(workspace, 256))) return LEET_ERR_INVALID_ARG;
@@ -209,7 +220,9 @@ int leet_attn_qk_norm_rope(const leet_attn_heads *q, const leet_attn_heads *out_
 }
 
 size_t leet_attn_qk_norm_rope_workspace_bytes(int B, int Hq, int Hk, int N, int d) {
-    if (B <= 0 || Hq <= 0 || Hk <= 0 || N <= 0 || d < 2 || d > 256 || d % 2 != 0 || (long long)B * N >= 1LL << 31) return 0;
+    if (B <= 0 || Hq <= 0 || Hk <= 0 || N <= 0 || d < 2 || d > 256 || d % 2 != 0 || (long long)B * N >= 1LL << 31 ||
+        Hq > kMaxHeads || Hk > kMaxHeads)
+        return 0;
     // the cuts of rows and their way from memory give different numbers of workgroups; room for any
     size_t rows = 0;
     for (int way = 0; way < 4; ++way) {
@@ -264,7 +277,9 @@ int leet_attn_qk_norm_rope_backward(const leet_attn_heads *dout_q, const leet_at
 }
 
 size_t leet_attn_gated_scan_workspace_bytes(int B, int N, int C, int backward) {
-    if (B <= 0 || N <= 0 || C <= 0 || N > 1 << 30 || C > 1 << 28) return 0;
+    if (B <= 0 || N <= 0 || C <= 0 || N > 1 << 30 || C > 1 << 28 ||
+        leet::gated_scan_threads(B, N, C, backward != 0) >= kMaxThreads)
+        return 0;
     return leet::gated_scan_workspace(B, N, C, backward != 0);
 }
 
@@ -353,6 +368,10 @@ int leet_attn_gated_scan_step(const leet_attn_rows *x, const leet_attn_rows *gat
     leet::GatedScanParams p = {};
     if (!rows_ok(x, B, 1, C, size_of(dtype), false) || !rows_ok(gate, B, 1, C, size_of(gate_dtype), false) ||
         !rows_ok(out, B, 1, C, size_of(dtype), true))
+        return LEET_ERR_INVALID_ARG;
+    // in place only element for element
+    if ((out->data == x->data && B > 1 && out->batch != x->batch) ||
+        (out->data == gate->data && (gate_dtype != dtype || (B > 1 && out->batch != gate->batch))) || out->data == state)
         return LEET_ERR_INVALID_ARG;
     p.vector = C % 4 == 0 && aligned(state, 16) && by_four(x, B, size_of(dtype)) && by_four(gate, B, size_of(gate_dtype)) &&
                        by_four(out, B, size_of(dtype)) ? 4 : 1;

@@ -238,6 +238,17 @@ def test_step_on_parts_of_rows(leet):
     assert bool((buf[:, :20] == 4).all()) and bool((buf[:, 120:] == 4).all())
 
 
+@pytest.mark.parametrize("C", [100, 33])
+def test_step_over_its_input(leet, C):
+    for over in (0, 1):
+        xz = [_normal((5, C), BF16, 160), _gate((5, C), BF16, 1, 161)]
+        s = _normal((5, C), F32, 162)
+        kept = s.clone()
+        want = leet.leet_attn_gated_scan_step(*xz, s)
+        got = leet.leet_attn_gated_scan_step(*xz, kept, out=xz[over])
+        assert got is xz[over] and torch.equal(got, want) and torch.equal(kept, s)
+
+
 def test_prefill_then_steps_is_one_longer_prefill(leet):
     B, N, T, C = 2, 301, 5, 128
     x, z = _normal((B, N + T, C), BF16, 96), _gate((B, N + T, C), BF16, 2, 97)

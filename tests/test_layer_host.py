@@ -236,6 +236,56 @@ def test_binding_refuses_before_the_library(leet):
         leet._rotation(freq, 0, torch.zeros(4, dtype=torch.int64), 0, 1.0, 1, 3)
 
 
+def test_sizes_beyond_an_int_are_refused(leet):
+    """Sizes whose products pass 32 or 64 bits, and tensors longer than the library counts, never come to a launch."""
+    LARGE, most = leet.LEET_ERR_TOO_LARGE, (1 << 31) - 1
+    for Hq, Hk in ((most, most), (most, 1), (1, most), (most - 14, most - 15)):
+        for call in (_rope, _norm, _back):
+            assert call(leet, _heads_args(leet, B=1, N=1, Hq=Hq, Hk=Hk)) == LARGE
+        assert leet.qk_norm_rope_workspace_bytes(1, Hq, Hk, 1, 128) == 0
+    for B, N, C in ((most, 1 << 30, 1 << 28), (1 << 30, 1 << 30, 1 << 28), (1 << 22, 1, 1), (1 << 10, 1 << 28, 1 << 26)):
+        for call, backward in ((_scan, False), (_scan_back, True)):
+            assert call(leet, _scan_args(leet, B=B, N=N, C=C)) == LARGE
+            assert leet.gated_scan_workspace_bytes(B, N, C, backward) == 0
+    for call in (_scan, _scan_back):
+        assert call(leet, _scan_args(leet, B=1, offsets=P, S=(1 << 30) + 1)) == LARGE
+    wide = torch.zeros(1)
+    freq = torch.ones(1, dtype=torch.float64)
+    for big in ((1 << 32) + 1, 1 << 31):
+        for shape in ((big, 1, 1, 2), (1, big, 1, 2), (1, 1, big, 2)):
+            q = wide.expand(shape)
+            for call in (lambda: leet.leet_attn_rope(q, freq), lambda: leet.leet_attn_qk_norm_rope(q, q, None, None, freq),
+                         lambda: leet.leet_attn_qk_norm_rope_backward(q, q, q, q, None, None, freq)):
+                with pytest.raises(leet.LeetAttnError, match="exceed"):
+                    call()
+        for shape in ((big, 1, 1), (1, big, 1), (1, 1, big)):
+            x = wide.expand(shape)
+            for call in (lambda: leet.leet_attn_gated_scan(x, x), lambda: leet.leet_attn_gated_scan_backward(x, None, x, x)):
+                with pytest.raises(leet.LeetAttnError, match="exceed"):
+                    call()
+        for shape in ((big, 1), (1, big)):
+            x = wide.expand(shape)
+            with pytest.raises(leet.LeetAttnError, match="exceed"):
+                leet.leet_attn_gated_scan_step(x, x, wide)
+
+
+def test_an_output_over_its_input_has_its_strides(leet):
+    """In place is the same data and strides; the same address with others would be written before it is read."""
+    H, INVALID = leet._pack_heads, leet.LEET_ERR_INVALID_ARG
+    for strides in ((1 << 20, 128, 256), (1 << 20, 1 << 13, 128), (1 << 19, 1 << 14, 128), (1 << 20, 1 << 14, 256)):
+        other = H(P, *strides)
+        for call in (_rope, _norm):
+            assert call(leet, _heads_args(leet, out_q=other)) == INVALID, strides
+        assert _back(leet, _heads_args(leet, dq=other)) == INVALID, strides
+        assert _back(leet, _heads_args(leet, dq=H(2 * P, *strides))) == INVALID, strides    # over dout_q
+        assert _back(leet, _heads_args(leet, dk=H(4 * P, *strides))) == INVALID, strides    # over dout_k
+    R = leet._pack_rows
+    assert _step(leet, _scan_args(leet, out=R(P, 1 << 19, 0), s_out=7 * P)) == INVALID        # over x
+    assert _step(leet, _scan_args(leet, out=R(2 * P, 1 << 20, 0), s_out=7 * P)) == INVALID    # over a gate of another type
+    assert _step(leet, _scan_args(leet, out=R(2 * P, 1 << 19, 0), gd=leet.LEET_BF16, s_out=7 * P)) == INVALID
+    assert _step(leet, _scan_args(leet, out=R(7 * P, 1 << 20, 0), s_out=7 * P)) == INVALID    # over the state
+
+
 # ---- the forms themselves: gradients against differences ----
 
 def _difference(f, x, dx, e=1e-6):
