@@ -29,7 +29,9 @@ namespace leet {
 
 // A tile: tokens of a wave, and waves of a workgroup that hold tokens (at most); one more wave links the tile to the others.
 // Workgroups of 8, 12 or 16 waves spread evenly over the four SIMDs of a compute unit (B4 N4096 C2048 forward: 16 tokens x 7
-// waves 57 us, 16 x 5 68, 12 x 9 71; backward 8 x 11 93, 8 x 9 102).
+// waves 57 us, 16 x 5 68, 12 x 9 71; backward 8 x 11 93, 8 x 9 102).  24 tokens x 7 waves, five waves a SIMD, are
+// better where sequences are very long and worse elsewhere (16 | 24 tokens: N32768 C4096 178 157, B32 N512 C4096 82 97,
+// N1000 C1024 12 14; of a moving average 186 187, 89 105, 16 20).
 constexpr int kForwardTokens = 16, kBackwardTokens = 8, kMostWaves = 15;
 
 // A gate as it is kept between its two uses, in one register: the decay a itself, or for the moving average the smaller of
