@@ -575,15 +575,16 @@ __global__ __launch_bounds__(64 * (kMostWaves + 1)) void gated_scan_backward_ker
     if (kPacked && live) pass_on<kV>(p, p.dstate_out, p.dstate_in, k, wave, c);
 }
 
-// One token of every sequence: state <- a state + b, out = state.  One thread per kV channels.
+// One token of every sequence: state <- a state + b, out = state.  One thread per kV channels.  Sequences are counted
+// without a sign: a stride of the grid behind the last of 2^31 - 1 is still a number.
 template <int kX, int kG, int kMode, int kV>
 __global__ __launch_bounds__(256) void gated_step_kernel(GatedScanParams p) {
     const uint32_t c = (blockIdx.x * 256 + threadIdx.x) * kV;
     if (c >= (uint32_t)p.C) return;
-    for (int b = blockIdx.y; b < p.B; b += gridDim.y) {
+    for (unsigned b = blockIdx.y; b < (unsigned)p.B; b += gridDim.y) {
         float z[kV], x[kV], s[kV];
-        Io<kG>::template load<kV>(row_at<kG>(p.gate, b, 0, c), z);
-        Io<kX>::template load<kV>(row_at<kX>(p.x, b, 0, c), x);
+        Io<kG>::template load<kV>(row_at<kG>(p.gate, (int)b, 0, c), z);
+        Io<kX>::template load<kV>(row_at<kX>(p.x, (int)b, 0, c), x);
         char* state = reinterpret_cast<char*>(p.state_out + (size_t)b * p.C + c);
         Io<0>::load<kV>(state, s);
 #pragma unroll

@@ -426,3 +426,20 @@ def test_offsets_that_no_sequences_have(leet):
         for t in (room, dx, dz):
             assert bool((t[:, :32] == 7).all()) and bool((t[:, N + 32:] == 7).all())
         assert bool((states[:2] == 5).all()) and bool((states[5:] == 5).all())
+
+
+def test_step_of_as_many_sequences_as_an_int_counts(leet):
+    """The last round of the grid's stride over 2^31 - 1 sequences ends behind what an int holds."""
+    B = (1 << 31) - 1
+    pattern = torch.arange(1024, dtype=F32, device="cuda")       # exact, and so are its halves
+    state = pattern.repeat(1 << 21)[:B].view(B, 1)
+    out = torch.full((B, 1), 7.0, dtype=F16, device="cuda")
+    x = torch.ones((1, 1), dtype=F16, device="cuda").expand(B, 1)
+    gate = torch.full((1, 1), 0.5, dtype=F16, device="cuda").expand(B, 1)
+    leet.leet_attn_gated_scan_step(x, gate, state, mode=leet.GATE_DECAY, out=out)
+    step = 1 << 28
+    want = (0.5 * pattern + 1).repeat(step // 1024)
+    for lo in range(0, B, step):
+        n = min(step, B - lo)
+        assert torch.equal(state[lo:lo + n, 0], want[:n])
+        assert torch.equal(out[lo:lo + n, 0], want[:n].half())
