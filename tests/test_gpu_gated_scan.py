@@ -443,3 +443,55 @@ def test_step_of_as_many_sequences_as_an_int_counts(leet):
         n = min(step, B - lo)
         assert torch.equal(state[lo:lo + n, 0], want[:n])
         assert torch.equal(out[lo:lo + n, 0], want[:n].half())
+
+
+@pytest.mark.parametrize("types", [(BF16, BF16), (F16, F32), (F32, F32)])
+@pytest.mark.parametrize("mode", [0, 1, 2])
+@pytest.mark.parametrize("B, N, C", [(16, 700, 130),   # 32 chains: seven data waves, 7 tiles forward, 16 ticket groups
+                                     (9, 500, 258),    # 27 chains: one ticket group
+                                     (17, 113, 64),    # a second tile of one token
+                                     (70, 241, 66),    # 70 chains, two groups; backward a third tile of one token
+                                     (3, 1000, 2816)])  # 66 chains, twenty-two column blocks a sequence
+def test_many_chains_of_several_tiles(leet, B, N, C, mode, types):
+    """More than sixteen chains take the short tiles that large jobs take, from as many ticket counters."""
+    _check(leet, B, N, C, types, mode, state=True)
+
+
+@pytest.mark.parametrize("lengths", [[300, 0, 17, 1, 900, 2, 280] + [7] * 20, [1500]])
+@pytest.mark.parametrize("C", [130, 1100])
+def test_packed_sequences_of_many_chains(leet, C, lengths):
+    """The same for packed sequences: columns times sequences are more than sixteen chains, or fewer."""
+    off, mode = _offsets(lengths), 2
+    S, N = len(lengths), int(off[-1])
+    x, z, dh = _normal((1, N, C), BF16, 170), _gate((1, N, C), BF16, mode, 171), _normal((1, N, C), BF16, 172)
+    s, ds = _normal((S, C), F32, 173, 3.0), _normal((S, C), F32, 174)
+    left, din = torch.full((S, C), 9.0, device="cuda"), torch.full((S, C), 9.0, device="cuda")
+    h = leet.leet_attn_gated_scan(x, z, mode=mode, state_in=s, state_out=left, offsets=off.cuda())
+    dx, dz = leet.leet_attn_gated_scan_backward(dh, x, z, h, mode=mode, state_in=s, dstate_out=ds, dstate_in=din,
+                                                offsets=off.cuda())
+    for j in range(S):
+        at = slice(int(off[j]), int(off[j + 1]))
+        s_j, ds_j = _f64(s[j:j + 1]), _f64(ds[j:j + 1])
+        want, last = forms.scan(_f64(z[:, at]), _f64(x[:, at]), mode, s_j)
+        assert forms.close(h[:, at], want) and forms.close(left[j:j + 1], last)
+        to_x, to_z, to_s = forms.scan_backward(_f64(dh[:, at]), _f64(z[:, at]), _f64(x[:, at]), _f64(h[:, at]), mode, s_j, ds_j)
+        assert forms.close(dx[:, at], to_x) and forms.close(dz[:, at], to_z) and forms.close(din[j:j + 1], to_s)
+
+
+@pytest.mark.parametrize("backward", [False, True])
+def test_the_sizes_of_a_batch_of_prompts(leet, backward):
+    """B4 N4096 C2048: 64 chains of 35 to 37 tiles over all compute units, on some channels of every column block."""
+    B, N, C, mode = 4, 4096, 2048, 1
+    some = torch.tensor([0, 1, 63, 64, 126, 127, 128, 700, 1023, 1024, 1500, 2046, 2047])
+    x, z = _normal((B, N, C), BF16, 180), _gate((B, N, C), BF16, mode, 181)
+    s, left = _normal((B, C), F32, 182, 3.0), torch.full((B, C), 9.0, device="cuda")
+    part = lambda t: _f64(t[..., some.cuda()])  # noqa: E731
+    h = leet.leet_attn_gated_scan(x, z, mode=mode, state_in=s, state_out=left)
+    if not backward:
+        want, last = forms.scan(part(z), part(x), mode, part(s))
+        assert forms.close(part(h), want, BF16) and forms.close(part(left), last, F32)
+        return
+    dh, ds, din = _normal((B, N, C), BF16, 183), _normal((B, C), F32, 184), torch.full((B, C), 9.0, device="cuda")
+    dx, dz = leet.leet_attn_gated_scan_backward(dh, None, z, h, mode=mode, state_in=s, dstate_out=ds, dstate_in=din)
+    to_x, to_z, to_s = forms.scan_backward(part(dh), part(z), part(x), part(h), mode, part(s), part(ds))
+    assert forms.close(part(dx), to_x, BF16) and forms.close(part(dz), to_z, BF16) and forms.close(part(din), to_s, F32)
