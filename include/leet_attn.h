@@ -471,9 +471,11 @@ typedef struct {
  *              from offsets[S] on are not read for a result and their outputs are left as they were.
  *              (The values are not diagnosed; other ones give wrong rows but no access out of range.)
  *   workspace  leet_attn_gated_scan_workspace_bytes bytes, 256-byte aligned (NULL when that is 0); scratch
- * Decays are meant to be at most 1 in magnitude: tokens are combined in tiles of up to 240 whose products
- * of decays are formed in fp32, which larger ones may take out of range, and of whose entering state
- * nothing is left where the product is under 2^-149.  A non-finite value makes the later values of its
+ * Decays may have any values.  Tokens are combined in tiles of up to 240 tokens and 128 channels by the
+ * products of their decays, formed in fp32: of the state that enters a tile nothing is left where that
+ * product is under 2^-149.  A tile that holds a decay above 1 in magnitude is taken token by token from the
+ * state before it instead, and the tiles behind it wait: the recurrence as it stands, at 5 to 30 times the
+ * time where every tile does (the longer the sequences and the fewer the channels, the slower).  A non-finite value makes the later values of its
  * channel and sequence non-finite and no others (once such a state has decayed to nothing it is NaN).
  */
 int leet_attn_gated_scan(const leet_attn_rows *x, const leet_attn_rows *gate, const leet_attn_rows *out,

@@ -20,6 +20,13 @@
 // done); a copy of both passes without branches for waves whose tokens are all there (51 us, but backward 105 instead of
 // 92: registers).
 //
+// That holds for decays of at most 1 in magnitude.  Larger ones (none of a moving average's are) can take a product, and
+// what it leaves of a zero state, out of fp32's range where the state itself is small, or cancel all but their rounding:
+// zeros with decays of 4 would be infinity times zero from token 64 on.  So a tile that holds one is no run: its tokens are
+// taken one after the other from the state before it, and the tiles behind it wait for that: some 8 us a tile of 112 tokens
+// (every decay above 1: B4 N4096 C2048 forward 305 us, N32768 C4096 2447; one token in a thousand: 78 and 374).  Watching for
+// them costs other calls 1 to 2 % (B4 N4096 C2048 52 -> 53 us, N32768 C4096 200 -> 205).
+//
 // Packed sequences: where a sequence begins, the run so far is cut off.  That is decided by the offsets alone, so it
 // is the same for all channels and no arithmetic carries anything over (zero times an infinity would).
 #include "leet_gated_scan.hpp"
@@ -231,8 +238,9 @@ struct Board {
     // The state behind tile k of the chain: looks back until it meets a tile whose state is known, waiting for those that
     // have published nothing, and goes forward from there over the runs.  So it is the same chain of fused multiply-adds
     // whatever was known when: results do not depend on timing.  Every wait ends: a tile publishes its run (the first tile
-    // its state) without waiting for anything, and tiles are taken in the order of the chain, so all that are waited for
-    // belong to workgroups that are running already.  That holds while the workspace is this launch's alone; kPatience
+    // its state) without waiting for anything, or, where its tokens are taken one after the other, its state after waiting
+    // for tiles before it alone; and tiles are taken in the order of the chain, so all that are waited for belong to
+    // workgroups that are running already.  That holds while the workspace is this launch's alone; kPatience
     // ends the wait, with NaN for the state, where it is not: some seconds of looks, a million times what a wait takes.
     static constexpr int kPatience = 1 << 22;
     template <int kV>
@@ -280,8 +288,10 @@ __global__ __launch_bounds__(256) void gated_scan_clear_kernel(u32x4* words, siz
 template <int kV>
 struct Shared {
     float A[kMostWaves][64 * kV], H[kMostWaves][64 * kV];  // the waves' runs
-    int cut[kMostWaves];  // a sequence begins (backward: ends) in the run: what came before does not reach behind it
+    int cut[kMostWaves];    // a sequence begins (backward: ends) in the run: what came before does not reach behind it
+    int grows[kMostWaves];  // a decay above 1 in magnitude in the run
     float carry[64 * kV];
+    int serial;  // one of the runs has such a decay: the waves go on one after the other
     unsigned ticket;
 };
 
@@ -309,8 +319,10 @@ __device__ __forceinline__ bool take_tile(const GatedScanParams& p, S& shared, i
 
 // The wave behind the data waves links the tile to the others: it joins the waves' runs, publishes, looks back, and leaves
 // the state before the tile in shared.carry.  The registers that looking back takes are then not beside a tile's data.
+// Of a tile whose tokens are taken one after the other it publishes the state alone, when the last data wave has left it in
+// shared.carry.
 // kBackward: the chain goes from the last wave to the first.
-template <int kV, bool kBackward, bool kPacked, class S>
+template <int kMode, int kV, bool kBackward, bool kPacked, class S>
 __device__ __forceinline__ void link_tile(const GatedScanParams& p, S& shared, int block, int k, int lane, bool live,
                                           const float* state_in, float* state_out, int b, uint32_t c) {
     float carry[kV], A[kV], H[kV];
@@ -318,12 +330,14 @@ __device__ __forceinline__ void link_tile(const GatedScanParams& p, S& shared, i
     else zero<kV>(carry);
     __syncthreads();  // the waves' runs are there
     bool cut = false;
+    int grows = 0;
 #pragma unroll
     for (int v = 0; v < kV; ++v) { A[v] = 1.0f; H[v] = 0.0f; }
     for (int i = 0; i < p.waves; ++i) {
         const int w = kBackward ? p.waves - 1 - i : i;
         const bool here = kPacked && shared.cut[w];
         cut = cut || here;
+        if (kMode != 2) grows |= shared.grows[w];
 #pragma unroll
         for (int v = 0; v < kV; ++v) {
             const float Hw = shared.H[w][lane * kV + v], Aw = shared.A[w][lane * kV + v];
@@ -331,31 +345,40 @@ __device__ __forceinline__ void link_tile(const GatedScanParams& p, S& shared, i
             A[v] *= Aw;
         }
     }
+    const bool serial = kMode != 2 && __builtin_expect(__builtin_amdgcn_readfirstlane(grows), 0);
     const Board board = Board::of<kV>(p, block, lane);
     if (k > 0) {
-        if (live) board.publish_run<kV>(k, cut, A, H);
-        if (live && cut) board.publish_state<kV>(k, H);
+        if (live && !serial) board.publish_run<kV>(k, cut, A, H);
+        if (live && !serial && cut) board.publish_state<kV>(k, H);
         board.state_behind<kV>(k - 1, live, carry);
     }
 #pragma unroll
     for (int v = 0; v < kV; ++v) shared.carry[lane * kV + v] = carry[v];
+    if (kMode != 2 && lane == 0) shared.serial = serial;
     __syncthreads();  // the state before the tile is there
 #pragma unroll
     for (int v = 0; v < kV; ++v) H[v] = cut ? H[v] : fmaf(A[v], carry[v], H[v]);
-    if (live && k + 1 < p.tiles && (k == 0 || !cut)) board.publish_state<kV>(k, H);
+    if (__builtin_expect(serial, 0)) {
+        for (int i = 0; i < p.waves; ++i) __syncthreads();  // the data waves, one after the other
+#pragma unroll
+        for (int v = 0; v < kV; ++v) H[v] = shared.carry[lane * kV + v];
+    }
+    if (live && k + 1 < p.tiles && (k == 0 || !cut || serial)) board.publish_state<kV>(k, H);
     if (!kPacked && live && k == p.tiles - 1) store_state<kV>(state_out, b, p.C, c, H);
 }
 
-// A data wave's part: its run goes to the others; before[] receives the state before it.
-template <int kV, bool kBackward, bool kPacked, class S>
-__device__ __forceinline__ void join_runs(const GatedScanParams& p, S& shared, int wave, int lane, const float* A,
-                                          const float* H, bool cut, float* before) {
+// A data wave's part: its run goes to the others; before[] receives the state before it.  True: the waves go on one after
+// the other, and this one has to hand its state on.
+template <int kMode, int kV, bool kBackward, bool kPacked, class S>
+__device__ __forceinline__ bool join_runs(const GatedScanParams& p, S& shared, int wave, int lane, const float* A,
+                                          const float* H, bool cut, bool grows, float* before) {
 #pragma unroll
     for (int v = 0; v < kV; ++v) {
         shared.A[wave][lane * kV + v] = A[v];
         shared.H[wave][lane * kV + v] = H[v];
     }
     if (kPacked && lane == 0) shared.cut[wave] = cut;
+    if (kMode != 2 && lane == 0) shared.grows[wave] = grows;
     __syncthreads();
     float beforeA[kV];
 #pragma unroll
@@ -374,9 +397,24 @@ __device__ __forceinline__ void join_runs(const GatedScanParams& p, S& shared, i
         }
     }
     __syncthreads();
+    if (kMode != 2 && __builtin_expect(__builtin_amdgcn_readfirstlane(shared.serial), 0)) {
+        for (int i = 0; i < ahead; ++i) __syncthreads();
+#pragma unroll
+        for (int v = 0; v < kV; ++v) before[v] = shared.carry[lane * kV + v];
+        return true;
+    }
 #pragma unroll
     for (int v = 0; v < kV; ++v)
         before[v] = cut_before ? before[v] : fmaf(beforeA[v], shared.carry[lane * kV + v], before[v]);
+    return false;
+}
+
+// The end of a data wave's turn in a tile whose waves go on one after the other: its state is the next one's.
+template <int kV, bool kBackward, class S>
+__device__ __forceinline__ void hand_on(const GatedScanParams& p, S& shared, int wave, int lane, const float* state) {
+#pragma unroll
+    for (int v = 0; v < kV; ++v) shared.carry[lane * kV + v] = state[v];
+    for (int i = kBackward ? p.waves - 1 - wave : wave; i < p.waves; ++i) __syncthreads();
 }
 
 // The first channel of a lane.  The last pair of an odd number of channels begins one channel early: that channel is then
@@ -422,7 +460,7 @@ __global__ __launch_bounds__(64 * (kMostWaves + 1), kX != 0 && kG != 0 && !kPack
     uint32_t c;
     const bool live = channel_of<kV>(p, block - b * p.columns, lane, &c);
     if (wave == p.waves) {
-        link_tile<kV, false, kPacked>(p, shared, block, k, lane, live, p.state_in, p.state_out, b, c);
+        link_tile<kMode, kV, false, kPacked>(p, shared, block, k, lane, live, p.state_in, p.state_out, b, c);
         return;
     }
     const int t0 = (k * p.waves + wave) * kTokens, count = min(max(p.N - t0, 0), kTokens);
@@ -442,6 +480,7 @@ __global__ __launch_bounds__(64 * (kMostWaves + 1), kX != 0 && kG != 0 && !kPack
     // three workgroups a compute unit instead of two)
     float h[kPacked ? kTokens : 1][kV];
     float A[kV], H[kV];
+    bool grows = false;  // a decay above 1 in magnitude
 #pragma unroll
     for (int v = 0; v < kV; ++v) { A[v] = 1.0f; H[v] = 0.0f; }
 #pragma unroll
@@ -459,6 +498,7 @@ __global__ __launch_bounds__(64 * (kMostWaves + 1), kX != 0 && kG != 0 && !kPack
             g[i][v].set(zi[v]);
             const float a = g[i][v].decay();
             float b = g[i][v].input(xi[v]);
+            if (kMode != 2) grows |= fabsf(a) > 1.0f;
             if (first) {
                 // the only place where the state is read: as soon as this run is known state_out, which may be the
                 // same memory, may be written
@@ -472,7 +512,8 @@ __global__ __launch_bounds__(64 * (kMostWaves + 1), kX != 0 && kG != 0 && !kPack
         }
     }
     float state[kV];
-    join_runs<kV, false, kPacked>(p, shared, wave, lane, A, H, kPacked && at.first != 0, state);
+    const bool serial = join_runs<kMode, kV, false, kPacked>(p, shared, wave, lane, A, H, kPacked && at.first != 0,
+                                                             __any(grows) && (!kPacked || at.inside), state);
 #pragma unroll
     for (int i = 0; i < kTokens; ++i) {
         if (i >= count) continue;
@@ -489,6 +530,7 @@ __global__ __launch_bounds__(64 * (kMostWaves + 1), kX != 0 && kG != 0 && !kPack
             if (kPacked && (at.last >> i & 1)) store_state<kV>(p.state_out, at.of(i), p.C, c, state);
         }
     }
+    if (__builtin_expect(serial, 0)) hand_on<kV, false>(p, shared, wave, lane, state);
     if (kPacked && live) pass_on<kV>(p, p.state_in, p.state_out, k, wave, c);
 }
 
@@ -505,7 +547,7 @@ __global__ __launch_bounds__(64 * (kMostWaves + 1)) void gated_scan_backward_ker
     uint32_t c;
     const bool live = channel_of<kV>(p, block - b * p.columns, lane, &c);
     if (wave == p.waves) {
-        link_tile<kV, true, kPacked>(p, shared, block, k, lane, live, p.dstate_out, p.dstate_in, b, c);
+        link_tile<kMode, kV, true, kPacked>(p, shared, block, k, lane, live, p.dstate_out, p.dstate_in, b, c);
         return;
     }
     const int t0 = ((p.tiles - 1 - k) * p.waves + wave) * kTokens, count = min(max(p.N - t0, 0), kTokens);
@@ -524,6 +566,7 @@ __global__ __launch_bounds__(64 * (kMostWaves + 1)) void gated_scan_backward_ker
     const Places<kTokens> at = kPacked ? Places<kTokens>(p.offsets, p.sequences, t0, p.N, lane) : Places<kTokens>{};
     Gate<kMode> gate[kTokens][kV];
     float d[kTokens][kV], A[kV], G[kV];
+    bool grows = false;  // a decay above 1 in magnitude
 #pragma unroll
     for (int v = 0; v < kV; ++v) { A[v] = 1.0f; G[v] = 0.0f; }
 #pragma unroll
@@ -540,6 +583,7 @@ __global__ __launch_bounds__(64 * (kMostWaves + 1)) void gated_scan_backward_ker
         for (int v = 0; v < kV; ++v) {
             gate[i][v].set(zi[v]);
             const float a = gate[i][v].decay();
+            if (kMode != 2) grows |= fabsf(a) > 1.0f;
             if (last) {
                 d[i][v] += leaves[v];
                 G[v] = a * d[i][v];
@@ -550,7 +594,8 @@ __global__ __launch_bounds__(64 * (kMostWaves + 1)) void gated_scan_backward_ker
         }
     }
     float g[kV];  // the gradient that comes in from behind
-    join_runs<kV, true, kPacked>(p, shared, wave, lane, A, G, kPacked && at.last != 0, g);
+    const bool serial = join_runs<kMode, kV, true, kPacked>(p, shared, wave, lane, A, G, kPacked && at.last != 0,
+                                                            __any(grows) && (!kPacked || at.inside), g);
 #pragma unroll
     for (int i = kTokens - 1; i >= 0; --i) {
         if (i >= count || !live || (kPacked && !(at.inside >> i & 1))) continue;
@@ -572,6 +617,7 @@ __global__ __launch_bounds__(64 * (kMostWaves + 1)) void gated_scan_backward_ker
         store_channels<kG, kV>(p.dgate, b, t0 + i, c, dgate);
         if (kPacked && first) store_state<kV>(p.dstate_in, at.of(i), p.C, c, g);
     }
+    if (__builtin_expect(serial, 0)) hand_on<kV, true>(p, shared, wave, lane, g);
     if (kPacked && live) pass_on<kV>(p, p.dstate_out, p.dstate_in, k, wave, c);
 }
 

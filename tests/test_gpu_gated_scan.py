@@ -495,3 +495,106 @@ def test_the_sizes_of_a_batch_of_prompts(leet, backward):
     dx, dz = leet.leet_attn_gated_scan_backward(dh, None, z, h, mode=mode, state_in=s, dstate_out=ds, dstate_in=din)
     to_x, to_z, to_s = forms.scan_backward(part(dh), part(z), part(x), part(h), mode, part(s), part(ds))
     assert forms.close(part(dx), to_x, BF16) and forms.close(part(dz), to_z, BF16) and forms.close(part(din), to_s, F32)
+
+
+def _growing(B, N, C, dtype, gdt, mode, seed):
+    """x, gate and entering state with decays above 1 in magnitude; by the channel's number modulo 5: zeros under decays of
+    4; a state of 1 that decays of 4 and inputs of -3 leave as it is (mode 0: 4 is exact); decays that grow and shrink by
+    turns; one single decay of -8 (mode 1: 8) among ordinary ones; ordinary ones alone."""
+    x, z, s = _normal((B, N, C), F32, seed), _gate((B, N, C), F32, mode, seed + 1), _normal((B, C), F32, seed + 2, 3.0)
+    log = torch.where(torch.arange(N, device="cuda") % 200 < 100, 0.25, -0.25).expand(B, N)
+    of = [torch.arange(C)[i::5] for i in range(5)]
+    for i in (0, 1):
+        z[..., of[i]] = 4.0 if mode == 0 else 1.25
+    x[..., of[0]], s[..., of[0]] = 0.0, 0.0
+    x[..., of[1]], s[..., of[1]] = (-3.0, 1.0) if mode == 0 else (0.0, 0.0)
+    z[..., of[2]] = (log.exp() if mode == 0 else log)[..., None]
+    z[:, N // 2, of[3]] = -8.0 if mode == 0 else 2.0
+    return x.to(dtype), z.to(gdt), s, of
+
+
+@pytest.mark.parametrize("types", [(BF16, BF16), (BF16, F32), (F32, F32)])
+@pytest.mark.parametrize("mode", [0, 1])
+@pytest.mark.parametrize("B, N, C", [(1, 1500, 130), (16, 700, 130), (2, 300, 1), (3, 16, 66), (1, 9, 257)])
+def test_decays_above_one(leet, B, N, C, mode, types):
+    """The recurrence is right whatever the decays are.  Products of runs would be infinite, and times a state of zero not a
+    number; and what they leave of a zero state would cancel a small state's share to nothing but rounding."""
+    x, z, s, of = _growing(B, N, C, *types, mode, 190)
+    left = torch.full((B, C), 9.0, device="cuda")
+    h = leet.leet_attn_gated_scan(x, z, mode=mode, state_in=s, state_out=left)
+    assert bool((h[..., of[0]] == 0).all()) and bool((h[..., of[1]] == (1 - mode)).all())
+    rest = torch.cat(of[2:]).sort().values.cuda()
+    part = lambda t: _f64(t[..., rest])  # noqa: E731
+    want, last = forms.scan(part(z), part(x), mode, part(s))
+    assert forms.close(part(h), want, types[0]) and forms.close(part(left), last, F32)
+
+    # the way back: zeros, and a gradient of 1 that 4 (1 - 0.75) leaves as it is
+    dh, ds = _normal((B, N, C), types[0], 193), _normal((B, C), F32, 194)
+    dh[..., of[0]], ds[..., of[0]] = 0.0, 0.0
+    dh[..., of[1]], ds[..., of[1]] = (-0.75, 1.0) if mode == 0 else (0.0, 0.0)
+    din = torch.full((B, C), 9.0, device="cuda")
+    dx, dz = leet.leet_attn_gated_scan_backward(dh, None, z, h, mode=mode, state_in=s, dstate_out=ds, dstate_in=din)
+    assert bool((dx[..., of[0]] == 0).all()) and bool((dz[..., of[0]] == 0).all()) and bool((din[..., of[0]] == 0).all())
+    assert bool((dx[..., of[1]] == 0.25 * (1 - mode)).all()) and bool((din[..., of[1]] == 1 - mode).all())
+    assert bool((dz[..., of[1]] == 0.25 * (1 - mode)).all())
+    to_x, to_z, to_s = forms.scan_backward(part(dh), part(z), part(x), part(h), mode, part(s), part(ds))
+    assert forms.close(part(dx), to_x, types[0]) and forms.close(part(dz), to_z, types[1]) and forms.close(part(din), to_s, F32)
+
+    again = torch.empty_like(left)
+    assert torch.equal(h, leet.leet_attn_gated_scan(x, z, mode=mode, state_in=s, state_out=again)) and torch.equal(left, again)
+    two = leet.leet_attn_gated_scan_backward(dh, None, z, h, mode=mode, state_in=s, dstate_out=ds, dstate_in=din.clone())
+    assert torch.equal(two[0], dx) and torch.equal(two[1], dz)
+
+
+@pytest.mark.parametrize("mode", [0, 1])
+@pytest.mark.parametrize("lengths", [[700, 0, 1, 799], [3] * 200, [240, 1, 0, 111, 112, 16], [1500] + [5] * 20])
+def test_decays_above_one_in_packed_sequences(leet, lengths, mode):
+    off, C = _offsets(lengths), 130
+    S, N = len(lengths), int(off[-1])
+    x, z, _, of = _growing(1, N + 50, C, BF16, F32, mode, 200)
+    s = _normal((S, C), F32, 201, 3.0)
+    s[:, of[0]], s[:, of[1]] = 0.0, float(1 - mode)
+    x[:, N:], z[:, N:] = float("nan"), 1e30     # behind the last sequence
+    left, out = torch.full((S, C), 9.0, device="cuda"), torch.full_like(x, 7.0)
+    leet.leet_attn_gated_scan(x, z, mode=mode, out=out, state_in=s, state_out=left, offsets=off.cuda())
+    dh, ds = _normal((1, N + 50, C), BF16, 202), _normal((S, C), F32, 203)
+    dh[..., of[0]], ds[..., of[0]] = 0.0, 0.0
+    dh[..., of[1]], ds[..., of[1]] = (-0.75, 1.0) if mode == 0 else (0.0, 0.0)
+    din, dx, dz = torch.full((S, C), 9.0, device="cuda"), torch.full_like(x, 7.0), torch.full_like(z, 7.0)
+    leet.leet_attn_gated_scan_backward(dh, None, z, out, mode=mode, dx=dx, dgate=dz, state_in=s, dstate_out=ds, dstate_in=din,
+                                       offsets=off.cuda())
+    assert all(bool((t[:, N:] == 7).all()) for t in (out, dx, dz))
+    for t, want in ((out[:, :N], 1.0), (left, 1.0), (dx[:, :N], 0.25), (dz[:, :N], 0.25), (din, 1.0)):
+        assert bool((t[..., of[0]] == 0).all()) and bool((t[..., of[1]] == want * (1 - mode)).all())
+    rest = torch.cat(of[2:]).sort().values.cuda()
+    for j in range(S):
+        at, part = slice(int(off[j]), int(off[j + 1])), lambda t: _f64(t[..., rest])  # noqa: E731
+        want, last = forms.scan(part(z[:, at]), part(x[:, at]), mode, part(s[j:j + 1]))
+        assert forms.close(part(out[:, at]), want, BF16) and forms.close(part(left[j:j + 1]), last, F32)
+        to_x, to_z, to_s = forms.scan_backward(part(dh[:, at]), part(z[:, at]), part(x[:, at]), part(out[:, at]), mode,
+                                               part(s[j:j + 1]), part(ds[j:j + 1]))
+        assert forms.close(part(dx[:, at]), to_x, BF16) and forms.close(part(dz[:, at]), to_z, F32)
+        assert forms.close(part(din[j:j + 1]), to_s, F32)
+
+
+@pytest.mark.parametrize("packed", [False, True])
+def test_one_tile_with_decays_above_one_among_many(leet, packed):
+    """A long chain whose runs are joined, but for single tiles that wait for the state before them."""
+    N, C, mode = 9000, 320, 0
+    x, z, s = _normal((1, N, C), F32, 210), _gate((1, N, C), F32, mode, 211), _normal((3 if packed else 1, C), F32, 212, 3.0)
+    for t, c in ((0, 5), (1, 200), (4000, 319), (4100, 0), (4101, 0), (8999, 130)):
+        z[0, t, c] = 1.5
+    off = _offsets([4050, 0, 4950]).cuda() if packed else None
+    dh, ds = _normal((1, N, C), F32, 213), _normal(s.shape, F32, 214)
+    left, din = torch.empty_like(s), torch.empty_like(s)
+    h = leet.leet_attn_gated_scan(x, z, mode=mode, state_in=s, state_out=left, offsets=off)
+    dx, dz = leet.leet_attn_gated_scan_backward(dh, None, z, h, mode=mode, state_in=s, dstate_out=ds, dstate_in=din, offsets=off)
+    for lo, hi, j in ((0, 4050, 0), (4050, 9000, 2)) if packed else ((0, N, 0),):
+        at = slice(lo, hi)
+        want, last = forms.scan(_f64(z[:, at]), _f64(x[:, at]), mode, _f64(s[j:j + 1]))
+        assert forms.close(h[:, at], want) and forms.close(left[j:j + 1], last)
+        to_x, to_z, to_s = forms.scan_backward(_f64(dh[:, at]), _f64(z[:, at]), _f64(x[:, at]), _f64(h[:, at]), mode,
+                                               _f64(s[j:j + 1]), _f64(ds[j:j + 1]))
+        assert forms.close(dx[:, at], to_x) and forms.close(dz[:, at], to_z) and forms.close(din[j:j + 1], to_s)
+    for _ in range(5):
+        assert torch.equal(h, leet.leet_attn_gated_scan(x, z, mode=mode, state_in=s, offsets=off))
