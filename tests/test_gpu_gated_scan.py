@@ -184,6 +184,25 @@ def test_ends_of_the_gates(leet):
         _check(leet, 1, 300, 64, (F32, F32), mode, True, gate=z)
 
 
+def test_gates_are_rounded_once_after_their_exponential(leet):
+    """A moving average's a and 1 - a are e / (1 + e) with e = exp(-|z|), and what that leaves of 1: sum, quotient and
+    difference each the nearest fp32 number.  e is the kernel's own, seen through the other mode with a state of 1."""
+    g = torch.Generator().manual_seed(167)
+    z = torch.cat((torch.randn(1 << 16, generator=g) * 6, torch.linspace(-104, 104, 5001), torch.tensor([0.0, -0.0])))
+    z = z[None].cuda()
+    zeros, ones = torch.zeros_like(z), torch.ones_like(z)
+    step = lambda x, gate, s, mode: leet.leet_attn_gated_scan_step(x, gate, s.clone(), mode=mode).cpu()  # noqa: E731
+    e = step(zeros, -z.abs(), ones, leet.GATE_LOG)
+    small = e / (1 + e)
+    a, rest = step(zeros, z, ones, leet.GATE_SIGMOID), step(ones, z, zeros, leet.GATE_SIGMOID)
+    below = z.cpu() < 0
+    assert torch.equal(a[below], small[below]) and torch.equal(rest[below], (1 - small)[below])
+    assert torch.equal(a[~below], (1 - small)[~below]) and torch.equal(rest[~below], small[~below])
+    # and over whole sequences
+    h = leet.leet_attn_gated_scan(zeros[None], z[None], mode=leet.GATE_SIGMOID, state_in=ones)
+    assert torch.equal(h[0].cpu(), a)
+
+
 @pytest.mark.parametrize("C", [96, 97])
 @pytest.mark.parametrize("packed", [False, True])
 def test_states_in_place(leet, packed, C):
