@@ -354,8 +354,9 @@ typedef enum {
  * Position rotation: pair i of the first `rot` elements of a head row at position p is turned by
  * theta = p freq[i] and multiplied by `scale`,
  *     y1 = scale (x1 cos theta - x2 sin theta),   y2 = scale (x2 cos theta + x1 sin theta);
- * the elements from `rot` on are passed on.  Angles are formed and reduced in fp64, so positions
- * may be as far out as fp64 counts.
+ * the elements from `rot` on are passed on.  Angles, cosines and sines are formed in fp64, these times
+ * the scale rounded to fp32 once.  An angle is off by some 2^-52 of itself, half a step of fp32 at 2^27
+ * radians; positions farther out are turned by less and less certain angles.
  *   freq       [rot/2] double, DEVICE memory: radians a position
  *   rot        even, 2 <= rot <= d
  *   positions  NULL: token n is at pos0 + n; else 64-bit integers, token n of sequence b at

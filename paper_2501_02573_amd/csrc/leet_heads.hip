@@ -13,8 +13,7 @@
 //   layout the pieces are rot / 2 apart, so both elements of every pair are in one lane; with the interleaved layout a
 //   pair is within a piece.  The sums over a row are then DPP adds over L lanes.
 // * A wave holds 64 / L tokens and walks over some heads of them, the next head's rows under way, so the cosines and sines,
-//   which depend on the token only, are formed once a wave: in fp64 up to the reduced angle (a product, two roundings), in
-//   fp32 from there.
+//   which depend on the token only, are formed once a wave, in fp64.
 // * Rows whose halves cannot be cut into pieces of four take the same kernel with pieces of one element (kV = 1), two pieces
 //   a lane and round (rot 34 of d 128: 73, 90 and 143 us where rot 128 takes 49, 51 and 78).
 #include "leet_heads.hpp"
@@ -82,21 +81,22 @@ struct RowLane {
     }
 };
 
-// Sine and cosine of x in [-pi/4, pi/4] by their power series; what is left out is under 2^-28 of the sine and 2^-32.
-__device__ __forceinline__ void sine_cosine(float x, float* s, float* c) {
-    const float y = x * x;
-    *s = x * fmaf(y, fmaf(y, fmaf(y, fmaf(y, 1.0f / 362880, -1.0f / 5040), 1.0f / 120), -1.0f / 6), 1.0f);
-    *c = fmaf(y, fmaf(y, fmaf(y, fmaf(y, fmaf(y, -1.0f / 3628800, 1.0f / 40320), -1.0f / 720), 1.0f / 24), -0.5f), 1.0f);
+// Sine and cosine of x in [-pi/4, pi/4] by their power series; what is left out is under 2^-36 of the sine and 2^-32.
+__device__ __forceinline__ void sine_cosine(double x, double* s, double* c) {
+    const double y = x * x;
+    *s = fma(x * y, fma(y, fma(y, fma(y, fma(y, -1.0 / 39916800, 1.0 / 362880), -1.0 / 5040), 1.0 / 120), -1.0 / 6), x);
+    *c = fma(y, fma(y, fma(y, fma(y, fma(y, -1.0 / 3628800, 1.0 / 40320), -1.0 / 720), 1.0 / 24), -0.5), 1.0);
 }
 
-// Cosines and sines (times the scale) of a lane's pairs at a position.  The angle in quarter turns is a product in fp64;
-// its distance to the nearest whole one goes on in fp32, where it is off by 2^-25 of a quarter turn at most, so a cosine
-// is off by little more than its own rounding however far out the position is.
+// Cosines and sines (times the scale) of a lane's pairs at a position, in fp64 and rounded once.  The angle in quarter turns
+// is off by some 2^-52 of itself (two products): as much as the series leave out at 2^20 radians, half a step of fp32 at 2^27.
+// us with series in fp32 (up to a step off) | in fp64: B4 N4096 H16+16 d128 bf16 rotation, norm, backward 48.8 50.8 76.6 |
+// 49.1 50.9 77.3, B3 N1777 H32+8 d64 fp16 11.5 13.0 23.7 | 11.4 13.6 24.1, B2 N4096 H16+4 d256 31.2 35.0 52.5 | 31.7 34.9 55.1.
 template <int kV, int kK, int kLog, bool kInter>
 __device__ __forceinline__ void angles(const RowLane<kV, kK, kLog, kInter>& row, const HeadsParams& p, double position,
                                        float (*cs)[kV], float (*sn)[kV]) {
     const double quarter_position = position * (2.0 / 3.14159265358979323846);
-    const float sin_scale = p.transposed ? -p.scale : p.scale;
+    const int turned_back = p.transposed ? 2 : 0;
 #pragma unroll
     for (int k = 0; k < kK; ++k)
 #pragma unroll
@@ -106,13 +106,14 @@ __device__ __forceinline__ void angles(const RowLane<kV, kK, kLog, kInter>& row,
             const int pair = !kInter ? row.first[k] + j : in_b ? row.second[k] / 2 + j - kV / 2 : row.first[k] / 2 + j;
             const double quarters = quarter_position * p.freq[in ? pair : 0];
             const double whole = rint(quarters);
-            float s, c;
-            sine_cosine((float)(quarters - whole) * 1.57079632679489661923f, &s, &c);
+            double s64, c64;
+            sine_cosine((quarters - whole) * (3.14159265358979323846 / 2), &s64, &c64);
+            const float s = (float)(s64 * (double)p.scale), c = (float)(c64 * (double)p.scale);
             // of the four quadrants only the last two bits count; a product beyond 2^31 keeps them
             const int quadrant = (int)(long long)whole;
             const float c1 = (quadrant & 1) ? s : c, s1 = (quadrant & 1) ? c : s;
-            cs[k][j] = ((quadrant + 1) & 2 ? -c1 : c1) * p.scale;
-            sn[k][j] = (quadrant & 2 ? -s1 : s1) * sin_scale;
+            cs[k][j] = (quadrant + 1) & 2 ? -c1 : c1;
+            sn[k][j] = (quadrant & 2) != turned_back ? -s1 : s1;
         }
 }
 

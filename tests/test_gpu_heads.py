@@ -87,6 +87,29 @@ def test_rope_far_out_and_before_zero(leet):
     assert forms.close(z, forms.rotate(_f64(x), freq, torch.full((1, 6), -3), 0))
 
 
+@pytest.mark.parametrize("scale", [1.0, 1.2079441, -0.7])
+@pytest.mark.parametrize("layout", [0, 1])
+@pytest.mark.parametrize("d, rot", [(128, 128), (64, 32), (128, 34)])
+def test_cosines_and_sines_are_rounded_once(leet, d, rot, layout, scale):
+    """Pairs (1, 0) come out as their cosine and sine times the scale, each the nearest fp32 number but for what the 64 bits
+    leave out: 2^-32 of the series, and 2^-51 of the angle here and in the form (which adds a rounding of its own)."""
+    N = 4000
+    pos = torch.randint(-70000, 200000, (1, N), generator=torch.Generator().manual_seed(9))
+    freq, x = _freq(rot), torch.zeros((1, 1, N, d), dtype=F32)
+    one, two = (slice(0, rot // 2), slice(rot // 2, rot)) if layout == 0 else (slice(0, rot, 2), slice(1, rot, 2))
+    x[..., one] = 1.0
+    scale = torch.tensor(scale, dtype=F32).double().item()
+    theta = pos.double()[0, :, None] * freq
+    for transposed in (False, True):
+        y = leet.leet_attn_rope(x.cuda(), freq.cuda(), positions=pos.cuda(), layout=layout, scale=scale, transposed=transposed)
+        y, sign = _f64(y)[0, 0], -1.0 if transposed else 1.0
+        for got, want in ((y[:, one], theta.cos() * scale), (y[:, two], sign * theta.sin() * scale)):
+            # half a step at a value is 2^-25 of the power of two above it, at the most
+            half = 2.0 ** -25 * torch.exp2(torch.ceil(torch.log2(want.abs().clamp_min(2.0 ** -100))))
+            off = half + abs(scale) * (2.0 ** -32 + 2.0 ** -50 * theta.abs())
+            assert bool(((got - want).abs() <= off).all())
+
+
 @pytest.mark.parametrize("layout", [0, 1])
 @pytest.mark.parametrize("rot", [16, 20])
 def test_elements_that_are_not_rotated_keep_clear_of_their_neighbours(leet, rot, layout):
