@@ -411,7 +411,8 @@ int leet_attn_rope(const leet_attn_heads *q, const leet_attn_heads *out_q, int H
  *     y = R (w .* x / sqrt(mean(x^2) + eps)).
  *   q_weight, k_weight  [d] of weight_dtype (`dtype` or LEET_F32), or NULL: ones
  *   eps                 >= 0, finite.  A row of zeros with eps = 0 gives NaN, as the formula does
- * The rest as for leet_attn_rope; fp32 inside, rounded once, at the store.
+ * The rest as for leet_attn_rope; fp32 inside, rounded once, at the store.  A row whose squares would leave
+ * fp32's range is multiplied by a power of two for its norm, so any finite row has one.
  */
 int leet_attn_qk_norm_rope(const leet_attn_heads *q, const leet_attn_heads *out_q, int Hq,
                            const leet_attn_heads *k, const leet_attn_heads *out_k, int Hk,

@@ -211,6 +211,30 @@ def test_norm_of_zero_rows_and_large_values(leet):
     assert torch.equal(z, y)
 
 
+@pytest.mark.parametrize("layout", [0, 1])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("d, rot", [(128, 128), (64, 32), (256, 64), (34, 10)])
+def test_norm_of_rows_whose_squares_leave_the_range(leet, d, rot, dtype, layout):
+    """Rows of 2^-100 to 2^120 and more beside ordinary ones: their squares are beyond fp32, their norms are not."""
+    freq, eps = _freq(rot), 1e-37          # below the range's end is weighed against eps = 2^-123
+    q, k = _normal((1, 3, 40, d), F32, 24), _normal((1, 1, 40, d), F32, 25)
+    powers = torch.tensor([0.0, 120.0, 63.0, 90.0, -100.0, -63.0, 55.0, 60.0, -49.0, -55.0]).exp2()
+    q, k = q * powers.repeat(4).cuda()[:, None], k * powers.flip(0).repeat(4).cuda()[:, None]
+    q[0, 0, 11, 0], q[0, 0, 11, 1:] = 3e38, 0.0
+    q, k = q.to(dtype), k.to(dtype)
+    w, pos = _normal((d,), dtype, 26, 0.3, 1.0), torch.arange(40).view(1, 40)
+    y, z = leet.leet_attn_qk_norm_rope(q, k, w, w, freq.cuda(), eps=eps, layout=layout)
+    eps = torch.tensor(eps, dtype=F32).double().item()
+    for x, out in ((q, y), (k, z)):
+        assert forms.close(out, forms.norm_rope(_f64(x), _f64(w), freq, pos, layout, eps=eps))
+    # gradients of inputs go like one over the row's length: those of a row of 2^120 are not below the smallest normal number
+    dy, dz = _normal(q.shape, dtype, 27, 2.0 ** 10), _normal(k.shape, dtype, 28, 2.0 ** 10)
+    dx, dk, dw, dwk = leet.leet_attn_qk_norm_rope_backward(dy, dz, q, k, w, w, freq.cuda(), eps=eps, layout=layout)
+    for x, g, gx, gw in ((q, dy, dx, dw), (k, dz, dk, dwk)):
+        to_x, to_w = forms.norm_rope_backward(_f64(g), _f64(x), _f64(w), freq, pos, layout, eps=eps)
+        assert forms.close(gw, to_w) and forms.close(gx, to_x)
+
+
 def test_weight_gradient_over_many_rows(leet):
     """More rows than one round of workgroups takes: dw of ones' gradient is a sum that is known."""
     B, H, N, d = 2, 16, 5000, 64
