@@ -333,7 +333,10 @@ int leet_attn_query_plan_rd(int B, int H, int N, int r, int dv, int dtype, int s
  * head row, or the channels of a token row, are adjacent), pointers need only their element's
  * alignment, and a workspace, where one is needed, is always the caller's, so that calls on several
  * streams and captured graphs share nothing.  Calls that may overlap in time need one each (the
- * recurrence's workgroups find one another through it).
+ * recurrence's workgroups find one another through it).  Outputs and workspaces that share memory with
+ * one another or with an input, other than in place where a call says so, are LEET_ERR_INVALID_ARG.
+ * (Rows of one buffer may lie between one another.  Where the strides leave more possibilities than the
+ * check looks at, which parts of one buffer at the same strides never do, the call is not refused.)
  * N = 0 is legal everywhere here and writes no rows.
  * ---------------------------------------------------------------------------------------------- */
 
@@ -395,8 +398,7 @@ int leet_attn_rope_frequencies(int rot, double base, int scaling, double factor,
 /*
  * Position rotation of queries and, in the same launch, of keys.
  *   q, k          [B][Hq][N][d], [B][Hk][N][d] of `dtype`; k and out_k may be NULL (Hk is then ignored)
- *   out_q, out_k  of the same shapes and type; each may be its input itself (same data and strides),
- *                 and must not overlap anything else (the same address is LEET_ERR_INVALID_ARG)
+ *   out_q, out_k  of the same shapes and type; each may be its input itself (same data and strides)
  *   transposed    non-zero: the transposed map (angles negated, same scale), which takes gradients of
  *                 the outputs to gradients of the inputs
  * d even, 2 <= d <= 256.  Rounded once, at the store.
@@ -424,8 +426,8 @@ int leet_attn_qk_norm_rope(const leet_attn_heads *q, const leet_attn_heads *out_
  * r = 1/sqrt(mean(x^2) + eps) and n = x r:
  *     dx = r (w .* u - n mean(w .* u .* n)),      dw = sum of u .* n over tokens and heads.
  *   dout_q, dout_k        gradients of the outputs
- *   dq, dk                gradients of the inputs; each may be the gradient it comes from (same data
- *                         and strides), and must not overlap anything else
+ *   dq, dk                gradients of the inputs; each may be the gradient it comes from, or the input
+ *                         (same data and strides)
  *   dq_weight, dk_weight  [d] of weight_dtype, two of them, or NULL: not wanted
  *   workspace             leet_attn_qk_norm_rope_workspace_bytes bytes, 256-byte aligned; may be NULL
  *                         when neither weight's gradient is wanted.  Its contents are scratch
@@ -462,8 +464,7 @@ typedef struct {
 /*
  * Over whole sequences.
  *   x, out     [B][N][C] of `dtype`;  gate  [B][N][C] of gate_dtype (`dtype` or LEET_F32)
- *   out        h of every token, rounded once, at the store (the recurrence itself runs in fp32);
- *              must not overlap an input
+ *   out        h of every token, rounded once, at the store (the recurrence itself runs in fp32)
  *   state_in   [S][C] float or NULL (zeros): h before each sequence's first token
  *   state_out  [S][C] float or NULL; receives h after each sequence's last token; may be state_in
  *   offsets    NULL: every batch entry is one sequence of N tokens, S = B (`sequences` is ignored).
@@ -492,7 +493,7 @@ int leet_attn_gated_scan(const leet_attn_rows *x, const leet_attn_rows *gate, co
  *     dgate = D h_{t-1} | g h_{t-1} | D (h_{t-1} - x) a (1 - a)      by mode,
  *     dstate_in = g of the first token.
  *   x            read by LEET_GATE_SIGMOID only; may be NULL otherwise
- *   h, dh, dx    [B][N][C] of `dtype`;  dgate  of gate_dtype; the outputs must not overlap an input
+ *   h, dh, dx    [B][N][C] of `dtype`;  dgate  of gate_dtype
  *   state_in     what the forward call was given (NULL: zeros)
  *   dstate_out   [S][C] float or NULL;  dstate_in  [S][C] float or NULL; may be dstate_out
  * The rest as for leet_attn_gated_scan.
@@ -507,7 +508,7 @@ size_t leet_attn_gated_scan_workspace_bytes(int B, int N, int C, int backward);
 /*
  * One token of every sequence: state <- a state + b, out = state (rounded).
  *   x, gate, out  [B][C], row b at data + b*batch (`token` is ignored);  state  [B][C] float, in place
- *   out may be x, or a gate of its type (same data and stride), and must not overlap anything else
+ *   out may be x, or a gate of its type (same data and stride)
  */
 int leet_attn_gated_scan_step(const leet_attn_rows *x, const leet_attn_rows *gate, const leet_attn_rows *out,
                               float *state, int B, int C, int dtype, int gate_dtype, int mode, void *stream);

@@ -5,8 +5,12 @@
 #include "leet_gated_scan.hpp"
 #include "leet_heads.hpp"
 #include "leet_host.hpp"
+#include "leet_overlap.hpp"
 
 namespace {
+
+using leet::Dim;
+using leet::Span;
 
 // A launch has fewer than 2^32 threads.
 constexpr long long kMaxThreads = 1LL << 32;
@@ -17,10 +21,6 @@ int elem_of(int dtype) { return dtype == LEET_F32 ? 0 : dtype == LEET_BF16 ? 1 :
 bool dtype_ok(int dtype) { return dtype == LEET_F32 || dtype == LEET_BF16 || dtype == LEET_F16; }
 size_t size_of(int dtype) { return dtype == LEET_F32 ? 4 : 2; }
 bool aligned(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
-
-struct Dim {
-    long long size, stride;
-};
 
 // Whether rows of `width` adjacent elements at these strides cannot overlap (checked from the smallest stride up, which
 // every layout of a dense tensor and of a part of one passes).
@@ -41,6 +41,12 @@ bool rows_apart(long long width, Dim* dims, int n) {
     return true;
 }
 
+bool shares_any(const Span& out, std::initializer_list<const Span*> others) {
+    for (const Span* o : others)
+        if (overlap(out, *o)) return true;
+    return false;
+}
+
 // ---- heads ----
 
 // Rows read and written beyond this are streamed past the last-level cache (256 MiB, 0.6 of it: where the prefill's inputs
@@ -55,11 +61,11 @@ bool heads_ok(const leet_attn_heads* t, int B, int H, int N, int d, size_t size,
     return !written || rows_apart(d, dims, 3);
 }
 
-// Whether an output at an input's address is that input, stride for stride.
-bool same_place_or_none(const leet_attn_heads* out, const leet_attn_heads* in, int B, int H, int N) {
-    return out->data != in->data || ((B == 1 || out->batch == in->batch) && (H == 1 || out->head == in->head) &&
-                                     (N == 1 || out->token == in->token));
+Span span_of(const leet_attn_heads* t, int B, int H, int N, int d, long long size) {
+    return t ? Span(t->data, size, d, {{B, t->batch}, {H, t->head}, {N, t->token}}) : Span();
 }
+// Whether an output is its input, stride for stride, or apart from it.
+bool in_place_or_apart(const Span& out, const Span& in) { return out == in || !overlap(out, in); }
 
 struct HeadsCall {
     const leet_attn_heads *in, *grad, *out;
@@ -69,8 +75,9 @@ struct HeadsCall {
 };
 
 // The arguments that the three operators on heads share.  LEET_OK with p->tokens = 0: nothing to do.
+// workspace: of the backward pass.
 int heads_params(const HeadsCall& q, const HeadsCall& k, const leet_attn_rotation* rotation, bool keys, bool backward,
-                 int weight_dtype, float eps, int B, int N, int d, int dtype, leet::HeadsParams* p) {
+                 int weight_dtype, float eps, const void* workspace, int B, int N, int d, int dtype, leet::HeadsParams* p) {
     if (!rotation || B <= 0 || N < 0 || q.H <= 0 || (keys && k.H <= 0)) return LEET_ERR_INVALID_ARG;
     if (!dtype_ok(dtype) || (weight_dtype != LEET_F32 && weight_dtype != dtype)) return LEET_ERR_UNSUPPORTED;
     if (d < 2 || d > 256 || d % 2 != 0) return LEET_ERR_UNSUPPORTED;
@@ -89,9 +96,7 @@ int heads_params(const HeadsCall& q, const HeadsCall& k, const leet_attn_rotatio
         if (c == &k && !keys) continue;
         if (!heads_ok(c->in, B, c->H, N, d, size, false) ||
             !heads_ok(c->out, B, c->H, N, d, size, true) ||
-            (backward && !heads_ok(c->grad, B, c->H, N, d, size, false)) ||
-            !same_place_or_none(c->out, c->in, B, c->H, N) ||
-            (backward && !same_place_or_none(c->out, c->grad, B, c->H, N)))
+            (backward && !heads_ok(c->grad, B, c->H, N, d, size, false)))
             return LEET_ERR_INVALID_ARG;
         if (!aligned(c->weight, weight_size) || !aligned(c->weight_grad, weight_size)) return LEET_ERR_INVALID_ARG;
         leet::HeadRows& r = c == &q ? p->q : p->k;
@@ -107,11 +112,6 @@ int heads_params(const HeadsCall& q, const HeadsCall& k, const leet_attn_rotatio
         r.weight_grad = c->weight_grad;
         r.H = c->H;
     }
-    // the outputs are two, and neither is the other's input
-    if (keys && (q.out->data == k.out->data || q.out->data == k.in->data || k.out->data == q.in->data ||
-                 (backward && (q.out->data == k.grad->data || k.out->data == q.grad->data))))
-        return LEET_ERR_INVALID_ARG;
-    if (q.weight_grad && q.weight_grad == k.weight_grad) return LEET_ERR_INVALID_ARG;
     p->freq = rotation->freq;
     p->positions = rotation->positions;
     p->positions_batch = rotation->positions_batch;
@@ -125,6 +125,29 @@ int heads_params(const HeadsCall& q, const HeadsCall& k, const leet_attn_rotatio
     leet::plan_heads(p, backward);
     // a wave takes 64 lanes of tokens of at least one lane each, for one unit
     if ((long long)p->tokens * p->units * 64 >= kMaxThreads) return LEET_ERR_TOO_LARGE;
+    // an output may be what it is made from; everything else that is written lies apart from the rest
+    const long long isz = (long long)size, wsz = (long long)weight_size;
+    const Span q_in = span_of(q.in, B, q.H, N, d, isz), q_out = span_of(q.out, B, q.H, N, d, isz);
+    const Span k_in = span_of(k.in, B, k.H, N, d, isz), k_out = span_of(k.out, B, k.H, N, d, isz);
+    const Span q_grad = span_of(q.grad, B, q.H, N, d, isz), k_grad = span_of(k.grad, B, k.H, N, d, isz);
+    const Span q_weight(q.weight, wsz, d), k_weight(k.weight, wsz, d), freq(rotation->freq, 8, rotation->rot / 2);
+    const Span positions(rotation->positions, 8, N, {{B, rotation->positions_batch}});
+    if (!in_place_or_apart(q_out, q_in) || !in_place_or_apart(q_out, q_grad) || !in_place_or_apart(k_out, k_in) ||
+        !in_place_or_apart(k_out, k_grad) ||
+        shares_any(q_out, {&k_out, &k_in, &k_grad, &q_weight, &k_weight, &freq, &positions}) ||
+        shares_any(k_out, {&q_in, &q_grad, &q_weight, &k_weight, &freq, &positions}))
+        return LEET_ERR_INVALID_ARG;
+    if (backward) {
+        const Span q_sum(q.weight_grad, wsz, d), k_sum(k.weight_grad, wsz, d);
+        // written when all else has been read
+        if (shares_any(q_sum, {&k_sum, &q_out, &k_out}) || shares_any(k_sum, {&q_out, &k_out})) return LEET_ERR_INVALID_ARG;
+        if (q.weight_grad || k.weight_grad) {
+            const Span scratch(workspace, sizeof(float), (long long)p->groups * p->units * d);
+            if (shares_any(scratch, {&q_out, &k_out, &q_in, &k_in, &q_grad, &k_grad, &q_weight, &k_weight, &freq, &positions,
+                                     &q_sum, &k_sum}))
+                return LEET_ERR_INVALID_ARG;
+        }
+    }
     int dev = 0;
     return leet::current_device(&dev);
 }
@@ -138,6 +161,10 @@ bool rows_ok(const leet_attn_rows* t, int B, int N, int C, size_t size, bool wri
     Dim dims[2] = {{B, t->batch}, {N, t->token}};
     return !written || rows_apart(C, dims, 2);
 }
+Span span_of(const leet_attn_rows* t, int B, int N, int C, long long size) {
+    return t ? Span(t->data, size, C, {{B, t->batch}, {N, t->token}}) : Span();
+}
+Span states_of(const float* s, int S, int C) { return Span(s, 4, (long long)S * C); }
 // Whether rows can be taken four channels at a time.
 bool by_four(const leet_attn_rows* t, int B, size_t size) {
     return aligned(t->data, 4 * size) && (B <= 1 || t->batch % 4 == 0);
@@ -202,7 +229,7 @@ int leet_attn_rope(const leet_attn_heads *q, const leet_attn_heads *out_q, int H
     if (!k != !out_k) return LEET_ERR_INVALID_ARG;
     leet::HeadsParams p;
     const int status = heads_params({q, nullptr, out_q, Hq, nullptr, nullptr}, {k, nullptr, out_k, Hk, nullptr, nullptr},
-                                    rotation, k != nullptr, false, dtype, 0.0f, B, N, d, dtype, &p);
+                                    rotation, k != nullptr, false, dtype, 0.0f, nullptr, B, N, d, dtype, &p);
     if (status != LEET_OK || p.tokens == 0) return status;
     p.transposed = transposed != 0;
     return done(leet::launch_heads(p, elem_of(dtype), rotation->layout, false, static_cast<hipStream_t>(stream)));
@@ -214,7 +241,7 @@ int leet_attn_qk_norm_rope(const leet_attn_heads *q, const leet_attn_heads *out_
                            const leet_attn_rotation *rotation, int B, int N, int d, int dtype, void *stream) {
     leet::HeadsParams p;
     const int status = heads_params({q, nullptr, out_q, Hq, q_weight, nullptr}, {k, nullptr, out_k, Hk, k_weight, nullptr},
-                                    rotation, true, false, weight_dtype, eps, B, N, d, dtype, &p);
+                                    rotation, true, false, weight_dtype, eps, nullptr, B, N, d, dtype, &p);
     if (status != LEET_OK || p.tokens == 0) return status;
     return done(leet::launch_heads(p, elem_of(dtype), rotation->layout, true, static_cast<hipStream_t>(stream)));
 }
@@ -250,7 +277,7 @@ int leet_attn_qk_norm_rope_backward(const leet_attn_heads *dout_q, const leet_at
                                     int B, int N, int d, int dtype, void *stream) {
     leet::HeadsParams p;
     const int status = heads_params({q, dout_q, dq, Hq, q_weight, dq_weight}, {k, dout_k, dk, Hk, k_weight, dk_weight},
-                                    rotation, true, true, weight_dtype, eps, B, N, d, dtype, &p);
+                                    rotation, true, true, weight_dtype, eps, workspace, B, N, d, dtype, &p);
     if (status != LEET_OK) return status;
     const bool sums = dq_weight || dk_weight;
     if (p.tokens == 0) {
@@ -294,13 +321,23 @@ int leet_attn_gated_scan(const leet_attn_rows *x, const leet_attn_rows *gate, co
     if (N > 0) {
         if (!rows_ok(x, B, N, C, size_of(dtype), false) ||
             !rows_ok(gate, B, N, C, size_of(gate_dtype), false) ||
-            !rows_ok(out, B, N, C, size_of(dtype), true) || out->data == x->data || out->data == gate->data)
+            !rows_ok(out, B, N, C, size_of(dtype), true))
             return LEET_ERR_INVALID_ARG;
         p.x = rows_in(x);
         p.gate = rows_in(gate);
         p.out = rows_out(out);
     }
     if (!aligned(state_in, 4) || !aligned(state_out, 4)) return LEET_ERR_INVALID_ARG;
+    {
+        const long long size = (long long)size_of(dtype);
+        const Span rows_x = span_of(x, B, N, C, size), rows_gate = span_of(gate, B, N, C, (long long)size_of(gate_dtype));
+        const Span to = span_of(out, B, N, C, size), in = states_of(state_in, S, C), left = states_of(state_out, S, C);
+        const Span places(offsets, 4, S + 1LL), scratch(workspace, 1, (long long)leet_attn_gated_scan_workspace_bytes(B, N, C, 0));
+        if (shares_any(to, {&rows_x, &rows_gate, &in, &left, &places, &scratch}) ||
+            shares_any(left, {&rows_x, &rows_gate, &places, &scratch}) || (state_out != state_in && overlap(left, in)) ||
+            shares_any(scratch, {&rows_x, &rows_gate, &in, &places}))
+            return LEET_ERR_INVALID_ARG;
+    }
     if (S == 0 || (N == 0 && (!state_out || state_out == state_in))) return LEET_OK;
     p.state_in = state_in;
     p.state_out = state_out;
@@ -333,10 +370,6 @@ int leet_attn_gated_scan_backward(const leet_attn_rows *dh, const leet_attn_rows
             if (!rows_ok(x, B, N, C, size, false)) return LEET_ERR_INVALID_ARG;
             p.x = rows_in(x);
         }
-        for (const leet_attn_rows* o : {dx, dgate})
-            if (o->data == dh->data || o->data == gate->data || o->data == h->data || (p.x.data && o->data == x->data))
-                return LEET_ERR_INVALID_ARG;
-        if (dx->data == dgate->data) return LEET_ERR_INVALID_ARG;
         p.dh = rows_in(dh);
         p.gate = rows_in(gate);
         p.h = rows_in(h);
@@ -344,7 +377,19 @@ int leet_attn_gated_scan_backward(const leet_attn_rows *dh, const leet_attn_rows
         p.dgate = rows_out(dgate);
     }
     if (!aligned(state_in, 4) || !aligned(dstate_out, 4) || !aligned(dstate_in, 4)) return LEET_ERR_INVALID_ARG;
-    if (dstate_in && dstate_in == state_in) return LEET_ERR_INVALID_ARG;
+    {
+        const long long size = (long long)size_of(dtype), gate_size = (long long)size_of(gate_dtype);
+        const Span rows_dh = span_of(dh, B, N, C, size), rows_gate = span_of(gate, B, N, C, gate_size);
+        const Span rows_h = span_of(h, B, N, C, size), rows_x = p.x.data ? span_of(x, B, N, C, size) : Span();
+        const Span to_x = span_of(dx, B, N, C, size), to_gate = span_of(dgate, B, N, C, gate_size);
+        const Span in = states_of(state_in, S, C), behind = states_of(dstate_out, S, C), before = states_of(dstate_in, S, C);
+        const Span places(offsets, 4, S + 1LL), scratch(workspace, 1, (long long)leet_attn_gated_scan_workspace_bytes(B, N, C, 1));
+        for (const Span* o : {&to_x, &to_gate, &before, &scratch})
+            if (shares_any(*o, {&rows_dh, &rows_gate, &rows_h, &rows_x, &in, &places})) return LEET_ERR_INVALID_ARG;
+        if (shares_any(to_x, {&to_gate, &before, &behind, &scratch}) || shares_any(to_gate, {&before, &behind, &scratch}) ||
+            shares_any(scratch, {&before, &behind}) || (dstate_in != dstate_out && overlap(before, behind)))
+            return LEET_ERR_INVALID_ARG;
+    }
     if (S == 0 || (N == 0 && (!dstate_in || dstate_in == dstate_out))) return LEET_OK;
     p.state_in = state_in;
     p.dstate_out = dstate_out;
@@ -370,8 +415,10 @@ int leet_attn_gated_scan_step(const leet_attn_rows *x, const leet_attn_rows *gat
         !rows_ok(out, B, 1, C, size_of(dtype), true))
         return LEET_ERR_INVALID_ARG;
     // in place only element for element
-    if ((out->data == x->data && B > 1 && out->batch != x->batch) ||
-        (out->data == gate->data && (gate_dtype != dtype || (B > 1 && out->batch != gate->batch))) || out->data == state)
+    const Span rows_x = span_of(x, B, 1, C, (long long)size_of(dtype)), to = span_of(out, B, 1, C, (long long)size_of(dtype));
+    const Span rows_gate = span_of(gate, B, 1, C, (long long)size_of(gate_dtype)), rows_state = states_of(state, B, C);
+    if (!in_place_or_apart(to, rows_x) || !in_place_or_apart(to, rows_gate) ||
+        shares_any(rows_state, {&rows_x, &rows_gate, &to}))
         return LEET_ERR_INVALID_ARG;
     p.vector = C % 4 == 0 && aligned(state, 16) && by_four(x, B, size_of(dtype)) && by_four(gate, B, size_of(gate_dtype)) &&
                        by_four(out, B, size_of(dtype)) ? 4 : 1;
