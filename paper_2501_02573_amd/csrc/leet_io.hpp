@@ -48,53 +48,29 @@ struct Io {
         __device__ __forceinline__ void store(char* p) const { __builtin_nontemporal_store(word, reinterpret_cast<Anywhere*>(p)); }
     };
 
-    // V adjacent elements at p (aligned to all of them, to 16 bytes at most)
+    // One or four adjacent elements at p (aligned to all of them)
     template <int V>
     static __device__ __forceinline__ void load(const char* p, float* f) {
-        if constexpr (kElem == 0) {
-            if constexpr (V == 1) f[0] = *reinterpret_cast<const float*>(p);
-            else if constexpr (V == 2) {
-                const float2 x = *reinterpret_cast<const float2*>(p);
-                f[0] = x.x; f[1] = x.y;
-            } else {
+        static_assert(V == 1 || V == 4, "one or four elements");
+        if constexpr (kElem == 0 && V == 1) f[0] = *reinterpret_cast<const float*>(p);
+        else if constexpr (kElem == 0) {
+            const f32x4 x = *reinterpret_cast<const f32x4*>(p);
 #pragma unroll
-                for (int e = 0; e < V; e += 4) {
-                    const f32x4 x = *reinterpret_cast<const f32x4*>(p + 4 * e);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) f[e + j] = x[j];
-                }
-            }
-        } else {
-            if constexpr (V == 1) f[0] = lo(*reinterpret_cast<const uint16_t*>(p));
-            else if constexpr (V == 2) {
-                const uint32_t x = *reinterpret_cast<const uint32_t*>(p);
-                f[0] = lo(x); f[1] = hi(x);
-            } else if constexpr (V == 4) {
-                const u32x2 x = *reinterpret_cast<const u32x2*>(p);
-                f[0] = lo(x[0]); f[1] = hi(x[0]); f[2] = lo(x[1]); f[3] = hi(x[1]);
-            } else {
-                const u32x4 x = *reinterpret_cast<const u32x4*>(p);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) { f[2 * j] = lo(x[j]); f[2 * j + 1] = hi(x[j]); }
-            }
+            for (int j = 0; j < 4; ++j) f[j] = x[j];
+        } else if constexpr (V == 1) f[0] = lo(*reinterpret_cast<const uint16_t*>(p));
+        else {
+            const u32x2 x = *reinterpret_cast<const u32x2*>(p);
+            f[0] = lo(x[0]); f[1] = hi(x[0]); f[2] = lo(x[1]); f[3] = hi(x[1]);
         }
     }
 
     template <int V>
     static __device__ __forceinline__ void store(char* p, const float* f) {
-        if constexpr (kElem == 0) {
-            if constexpr (V == 1) *reinterpret_cast<float*>(p) = f[0];
-            else if constexpr (V == 2) *reinterpret_cast<float2*>(p) = float2{f[0], f[1]};
-            else {
-#pragma unroll
-                for (int e = 0; e < V; e += 4) *reinterpret_cast<f32x4*>(p + 4 * e) = f32x4{f[e], f[e + 1], f[e + 2], f[e + 3]};
-            }
-        } else {
-            if constexpr (V == 1) *reinterpret_cast<uint16_t*>(p) = (uint16_t)pack2(f[0], 0.0f);
-            else if constexpr (V == 2) *reinterpret_cast<uint32_t*>(p) = pack2(f[0], f[1]);
-            else if constexpr (V == 4) *reinterpret_cast<u32x2*>(p) = u32x2{pack2(f[0], f[1]), pack2(f[2], f[3])};
-            else *reinterpret_cast<u32x4*>(p) = u32x4{pack2(f[0], f[1]), pack2(f[2], f[3]), pack2(f[4], f[5]), pack2(f[6], f[7])};
-        }
+        static_assert(V == 1 || V == 4, "one or four elements");
+        if constexpr (kElem == 0 && V == 1) *reinterpret_cast<float*>(p) = f[0];
+        else if constexpr (kElem == 0) *reinterpret_cast<f32x4*>(p) = f32x4{f[0], f[1], f[2], f[3]};
+        else if constexpr (V == 1) *reinterpret_cast<uint16_t*>(p) = (uint16_t)pack2(f[0], 0.0f);
+        else *reinterpret_cast<u32x2*>(p) = u32x2{pack2(f[0], f[1]), pack2(f[2], f[3])};
     }
 };
 
