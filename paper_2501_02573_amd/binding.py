@@ -700,6 +700,8 @@ def leet_attn_decode_step_rd(q, k, v, gamma: Optional[torch.Tensor], state, out:
 # Their tensors may have any strides but for the last dimension's, which must be 1, and outputs that the caller does not
 # bring are dense.  A workspace that the caller does not bring comes from torch's allocator, on the current stream: it
 # belongs to this call alone, also while a graph is captured.
+# Like the attention's calls they record nothing for autograd: outputs require no gradient even where inputs do.  Who
+# trains with them puts a call and its _backward (the rotation's: the transposed rotation) into a torch.autograd.Function.
 
 def _on(*tensors: Optional[torch.Tensor]) -> int:
     """Index of the one device of all tensors that are there."""
@@ -825,8 +827,8 @@ def leet_attn_rope(q: torch.Tensor, freq: torch.Tensor, k: Optional[torch.Tensor
     """Position rotation of q [B, Hq, N, d], and of k [B, Hk, N, d] in the same launch.
 
     The first ``2 * len(freq)`` elements of each row are rotated by the token's position (``positions`` or the token's
-    number, plus ``pos0``).  ``transposed`` takes gradients of the outputs to gradients of the inputs.  Returns out_q,
-    or (out_q, out_k); an output may be its input."""
+    number, plus ``pos0``).  ``transposed`` takes gradients of the outputs to gradients of the inputs; autograd sees
+    nothing of the call.  Returns out_q, or (out_q, out_k); an output may be its input."""
     B, Hq, Hk, N, d = _heads_pair(q, k, "leet_attn_rope")
     if out_q is None:
         out_q = _new_dense(q)
@@ -869,7 +871,8 @@ def leet_attn_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, q_weight: Optional[
                            scale: float = 1.0, out_q: Optional[torch.Tensor] = None,
                            out_k: Optional[torch.Tensor] = None):
     """Norm of every head of q [B, Hq, N, d] and k [B, Hk, N, d], times its weight [d], then the rotation of
-    ``leet_attn_rope``, in one pass.  Returns (out_q, out_k): dense [B, H, N, d], as the prefill reads them, unless given."""
+    ``leet_attn_rope``, in one pass.  Returns (out_q, out_k): dense [B, H, N, d], as the prefill reads them, unless given;
+    autograd sees nothing of it (``leet_attn_qk_norm_rope_backward``)."""
     B, Hq, Hk, N, d = _heads_pair(q, k, "leet_attn_qk_norm_rope")
     weight_dtype = _weights(q, q_weight, k_weight, d)
     if out_q is None:
@@ -898,7 +901,8 @@ def leet_attn_qk_norm_rope_backward(dout_q: torch.Tensor, dout_k: torch.Tensor, 
                                     dq_weight: Optional[torch.Tensor] = None, dk_weight: Optional[torch.Tensor] = None,
                                     workspace: Optional[torch.Tensor] = None):
     """Gradients of ``leet_attn_qk_norm_rope``: (dx_q, dx_k, dq_weight, dk_weight) from those of its outputs and its
-    inputs.  A weight that is None has the gradient None."""
+    inputs.  A weight that is None has the gradient None.  The attention here has no backward pass: where its q and k
+    are what was normed, their gradients come from the caller's own."""
     B, Hq, Hk, N, d = _heads_pair(q, k, "leet_attn_qk_norm_rope_backward")
     weight_dtype = _weights(q, q_weight, k_weight, d)
     grads = []
@@ -968,7 +972,8 @@ def leet_attn_gated_scan(x: torch.Tensor, gate: torch.Tensor, mode: int = GATE_L
     """Gated linear recurrence ``h_t = a_t h_{t-1} + b_t`` in every channel of x, gate [B, N, C]; returns h in x's type.
 
     ``mode``: what the gate is (GATE_DECAY a itself, GATE_LOG its logarithm, GATE_SIGMOID its logit with b = (1 - a) x).
-    States are float32 [B, C]; with ``offsets`` (int32 [S + 1], B = 1: packed sequences) [S, C]."""
+    States are float32 [B, C]; with ``offsets`` (int32 [S + 1], B = 1: packed sequences) [S, C].  Autograd sees nothing
+    of it (``leet_attn_gated_scan_backward``)."""
     S = _scan_sequences(x.shape, offsets)
     B, N, C = x.shape
     _sizes("leet_attn_gated_scan", B, N, C, S)

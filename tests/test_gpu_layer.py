@@ -87,3 +87,82 @@ def test_training_step_in_a_graph_beside_an_eager_one():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(eager, kept))
+
+
+def test_gradients_by_a_function_of_the_callers():
+    """The calls record nothing for autograd; wrapped, each with its way back, they give the gradients of the 64-bit formula."""
+    from paper_2501_02573_amd import binding as leet
+    B, H, N, d = 2, 2, 75, 64
+    g = torch.Generator().manual_seed(3)
+    freq, pos = leet.rope_frequencies(d)[0], torch.arange(N).expand(B, N)
+    on = freq.cuda()
+
+    class Rope(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, q):
+            return leet.leet_attn_rope(q, on)
+
+        @staticmethod
+        def backward(ctx, dy):
+            return leet.leet_attn_rope(dy.contiguous(), on, transposed=True)
+
+    class NormRope(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, q, k, wq, wk):
+            ctx.save_for_backward(q, k, wq, wk)
+            return leet.leet_attn_qk_norm_rope(q, k, wq, wk, on)
+
+        @staticmethod
+        def backward(ctx, dq, dk):
+            return leet.leet_attn_qk_norm_rope_backward(dq.contiguous(), dk.contiguous(), *ctx.saved_tensors, on)
+
+    class Scan(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, gate):
+            h = leet.leet_attn_gated_scan(x, gate, mode=leet.GATE_SIGMOID)
+            ctx.save_for_backward(x, gate, h)
+            return h
+
+        @staticmethod
+        def backward(ctx, dh):
+            return leet.leet_attn_gated_scan_backward(dh.contiguous(), *ctx.saved_tensors, mode=leet.GATE_SIGMOID)
+
+    q, k, gate, weigh = (torch.randn((B, H, N, d), generator=g) for _ in range(4))
+    wq, wk = 1 + 0.2 * torch.randn((2, d), generator=g)
+    gate = gate.view(B, N, H * d)
+    leaves = [t.clone().cuda().requires_grad_() for t in (q, k, wq, wk, gate)]
+    assert not any(t.requires_grad for t in leet.leet_attn_qk_norm_rope(*leaves[:4], on))
+    assert not leet.leet_attn_gated_scan(leaves[4], leaves[4]).requires_grad and not leet.leet_attn_rope(leaves[0], on).requires_grad
+
+    def loss(q, k, wq, wk, gate, weigh, norm_rope, rope, scan):
+        y, z = norm_rope(q, k, wq, wk)
+        x = (y * z + rope(q)).transpose(1, 2).reshape(B, N, H * d)
+        return (scan(x, gate).view(B, N, H, d).transpose(1, 2) * weigh).sum()
+
+    got = torch.autograd.grad(loss(*leaves, weigh.cuda(), NormRope.apply, Rope.apply, Scan.apply), leaves)
+
+    def scan64(x, gate):
+        h, out = torch.zeros(B, H * d, dtype=torch.float64), []
+        a = torch.sigmoid(gate)
+        for t in range(N):
+            h = a[:, t] * h + (1 - a[:, t]) * x[:, t]
+            out.append(h)
+        return torch.stack(out, 1)
+
+    def norm64(q, k, wq, wk):
+        def one(x, w):
+            u = x / (x.square().mean(-1, keepdim=True) + 1e-6).sqrt() * w
+            return turn64(u)
+        return one(q, wq), one(k, wk)
+
+    def turn64(u):
+        theta = pos.double()[:, None, :, None] * freq
+        a, b = u.chunk(2, -1)
+        return torch.cat((a * theta.cos() - b * theta.sin(), b * theta.cos() + a * theta.sin()), -1)
+
+    plain = [t.double().requires_grad_() for t in (q, k, wq, wk, gate)]
+    want = torch.autograd.grad(loss(*plain, weigh.double(), norm64, turn64, scan64), plain)
+    for a, b in zip(got, want):
+        # some forty fp32 roundings of 2^-24 on the way to each value, of numbers up to a hundred times the gradient's largest
+        # (the weights' are sums over 300 rows): 2^-24 40 100 < 2.4e-4 of it
+        assert float((a.double().cpu() - b).abs().max() / b.abs().max()) < 2.4e-4
