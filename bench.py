@@ -40,9 +40,11 @@ timed region; ``no_settle`` is the headline figure without it.
 from __future__ import annotations
 
 import argparse
+import hashlib
 import json
 import math
 import os
+import re
 import sys
 import time
 
@@ -176,15 +178,30 @@ def kernel_times(binding, q, k, v, gamma, out, reps, segments):
     return [a / reps for a in acc]
 
 
-def load_traffic(binding, workload, kernel):
+# What decides how many bytes an attention launch moves: its kernels, and the planner that launches them.
+TRAFFIC_SOURCES = ("leet_api.hip", "leet_common.hpp", "leet_fwd_16bit.hip", "leet_fwd_16bit_coop.hip", "leet_fwd_f32.hip",
+                   "leet_fwd_f32_split.hip", "leet_scan_decode.hip", "leet_elementwise.hip")
+
+
+def traffic_key():
+    """Digest of these sources without comments, white space and the version number."""
+    h = hashlib.sha256()
+    for name in TRAFFIC_SOURCES:
+        with open(os.path.join(ROOT, "paper_2501_02573_amd", "csrc", name)) as f:
+            text = re.sub(r"//[^\n]*|/\*.*?\*/", "", f.read(), flags=re.S)
+        h.update(re.sub(r'"\d+\.\d+\.\d+"|\s', "", text).encode())
+    return h.hexdigest()[:16]
+
+
+def load_traffic(workload, kernel):
     """HBM bytes per launch of a kernel from the committed profiler summary -- measured by
-    rocprofv3 PMC runs, not in this run -- or None when that summary was taken from another
-    version of the library than the one loaded now."""
+    rocprofv3 PMC runs, not in this run -- or None when that summary was taken from other
+    kernels than the sources have now."""
     path = os.path.join(ROOT, "profiles", "hbm_traffic.json")
     try:
         with open(path) as f:
             rec = json.load(f)
-        if rec.get("_library_version") != binding.version():
+        if rec.get("_kernels") != traffic_key():
             return None
         ent = rec.get(f"{workload}/{kernel}")
         return None if ent is None else ent.get("hbm_bytes_per_launch")
@@ -312,8 +329,8 @@ def main():
             "peak": HBM_PEAK_GBS,
             "unit": "GB/s",
             "frac": hbm_frac,
-            "traffic": load_traffic(binding, cfg.name, kernel_ran),
-            "traffic_source": "profiles/hbm_traffic.json (rocprofv3 FETCH_SIZE and WRITE_SIZE runs of this library version; null if stale)",
+            "traffic": load_traffic(cfg.name, kernel_ran),
+            "traffic_source": "profiles/hbm_traffic.json (rocprofv3 FETCH_SIZE and WRITE_SIZE runs of these kernels; null if stale)",
             "algorithmic_bytes_per_launch": nbytes,
             "avg_launch_ms": walk_ms,
             "timed_by": ("HIP events around the timed steps (one kernel per step)" if single_kernel else
@@ -377,7 +394,7 @@ def extra_legs(torch, binding, W, dev, cfg3, tokens3, use_graph):
         "hbm_frac_whole_step": b4 / (ms4 * 1e-3) / 1e9 / HBM_PEAK_GBS,
         "kernel_ms": {"segment_state_prepass": kms4[0], "segment_scan": kms4[1], "chunk_walk": kms4[2]},
         "walk_hbm_frac": b4 / (kms4[2] * 1e-3) / 1e9 / HBM_PEAK_GBS,
-        "traffic": {name: load_traffic(binding, cfg4.name, name) for name in ("prepass", "scan", "walk")},
+        "traffic": {name: load_traffic(cfg4.name, name) for name in ("prepass", "scan", "walk")},
         "note": "805 MB of inputs: every step streams from HBM; the step moves the inputs once for the walk and "
                 "k, v of 7/8 of the tokens a second time for the segment-state pre-pass",
     }
@@ -411,7 +428,7 @@ def extra_legs(torch, binding, W, dev, cfg3, tokens3, use_graph):
         "roofline": {"kernel": "decode_kernel<128,128,bf16>", "bound": "hbm",
                      "achieved": b5 / (us5 * 1e-6) / 1e9, "peak": HBM_PEAK_GBS, "unit": "GB/s",
                      "frac": b5 / (us5 * 1e-6) / 1e9 / HBM_PEAK_GBS,
-                     "traffic": load_traffic(binding, c5.name, "decode"),
+                     "traffic": load_traffic(c5.name, "decode"),
                      "algorithmic_bytes_per_launch": b5,
                      "note": "256 back-to-back steps on one 128 MiB state"},
         "by_store_policy": {name: decode_entry(us) for name, us in resident.items()},
