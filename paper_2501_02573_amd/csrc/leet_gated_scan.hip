@@ -13,12 +13,12 @@
 // registers and forms its run's (A, H); the waves of a workgroup lie behind one another in time and exchange their runs
 // through LDS; each then knows the state before its first token and goes over its registers once more.  So inputs are
 // read once and outputs written once, which is what bounds it where there are many channels (a bf16 forward pass moves 6
-// bytes a token and channel for some ten operations): N32768 C4096 with fp32 decays 197 us, 5.4 TB/s, where a copy of
-// as many bytes runs at 5.1; B4 N4096 C2048 bf16 51 us, 3.9 TB/s, of which some 5 us are the looks back, 1 the tickets
-// and 2 the clearing of the workspace before it (measured by leaving parts out).  Tried and slower: workgroups that stay
-// and load the next tile during the look back (61 and 227 us: a tile's run is published only when the tile before it is
-// done); a copy of both passes without branches for waves whose tokens are all there (51 us, but backward 105 instead of
-// 92: registers).
+// bytes a token and channel for some ten operations): N32768 C4096 with fp32 decays 205 us, 5.2 TB/s, where a copy of
+// as many bytes runs at 5.1; B4 N4096 C2048 bf16 52 us, 3.9 TB/s.  Without the looks back that is 5 us less, without the
+// tickets 1, without the kernel that clears the workspace 2 (parts left out; a trace, which keeps kernels apart, has 5.3 for
+// that kernel and 48.8 for the scan).  Tried and slower: workgroups that stay and load the next tile during the look back
+// (61 and 227 us: a tile's run is published only when the tile before it is done); a copy of both passes without branches
+// for waves whose tokens are all there (51 us, but backward 105 instead of 92: registers).
 //
 // That holds for decays of at most 1 in magnitude.  Larger ones (none of a moving average's are) can take a product, and
 // what it leaves of a zero state, out of fp32's range where the state itself is small, or cancel all but their rounding:
@@ -198,7 +198,8 @@ struct Board {
     }
 
     // A window of what tiles k, k - 1, .. have published.  What is looked at in vain costs memory bandwidth: two, four and
-    // eight tiles at a time, B4 N4096 C2048 52, 54 and 55 us.
+    // eight tiles at a time, B4 N4096 C2048 (64 chains) 52, 54 and 55 us.  That is decided by where many chains look: one
+    // sequence of 20000 tokens, moving average, C128 (one chain) 40 37 57, C512 (4) 44 40 69, C1024 (8) 48 49 82, C2048 70 83 100.
     template <int kV>
     struct Window {
         static constexpr int kTiles = 2;
@@ -696,8 +697,12 @@ static hipError_t launch_scan(const GatedScanParams& p, int elem, int gate_elem,
 // Waves of a workgroup that hold tokens.  A chain advances a tile every 0.3 us, so where there are few chains long tiles
 // count; else that several workgroups fit a compute unit.  us with 7 | 11 | 15 waves, bf16: forward N20000 C1024 (8 chains)
 // 65 47 43, C2048 (16) 80 71 69, B2 N4096 C2048 (32) 31 32 33, B4 (64) 50 58 61, N32768 C4096 (32) 176 200 194; backward
-// C1024 125 86 72, B4 N4096 C2048 79 76 74, N32768 C4096 313 267 253.  Packed sequences are chains of their own (37 of them
-// in N20011 C1001 forward: 54 - 60).
+// C1024 125 86 72, B4 N4096 C2048 79 76 74, N32768 C4096 313 267 253.
+// Packed sequences count as chains of their own, however long they are: their offsets lie on the device.  bf16 moving average,
+// 20011 tokens, 7 | 15 waves: 37 equal sequences forward C128 18 21, C1001 56 61, C2048 92 115, backward C128 21 19, C1001 79
+// 96, C2048 126 165; one long sequence and 36 of ten tokens forward C128 64 43, C1001 75 65, C2048 97 114, backward C128 111 62,
+// C1001 137 97, C2048 162 156.  So it costs a third where nearly all tokens are one sequence's and channels are few (forward),
+// and up to a quarter where sequences are equal and channels many (backward).
 constexpr int kForwardWaves = 7;
 static int waves_of(const GatedScanParams& p, bool backward) {
     const long long chains = (long long)p.B * p.columns * (p.offsets ? p.sequences : 1);

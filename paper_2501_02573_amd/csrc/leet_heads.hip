@@ -322,7 +322,10 @@ __global__ __launch_bounds__(64 * kHeadsWaves) void heads_kernel(HeadsParams p) 
 // Backward.  All waves of a workgroup take the same heads (a unit); workgroup g of a unit takes token groups g, g +
 // groups, ...  The lanes' sums for the weight gradient are joined over the wave's rows, then over the waves, and go to
 // one row of `partial`; heads_weight_kernel adds the rows up in order.
-// Five workgroups a compute unit fit in 102 registers a lane: plan_heads launches so many.
+// plan_heads launches five workgroups a compute unit, which leaves 96 registers a lane.  Rows of 16 bits fit (but for two or
+// three words a lane at width 256, which the kernel leaves in scratch memory), rows of fp32 leave nine to thirteen words
+// there: four workgroups would take 108 registers and nothing there, in as much time (us with five | four: B2 N2047 H8+8 d64 fp32
+// 17.3 16.8, B2 N4096 H16+16 d128 fp32 77.8 75.6, the same in bf16 with N4096 B4 79.7 81.0, d256 H16+4 56.3 58.9).
 template <int kElem, int kV, int kK, int kLog, bool kInter, bool kStream>
 __global__ __launch_bounds__(64 * kHeadsWaves, kBackwardResident) void heads_backward_kernel(HeadsParams p) {
     constexpr int kTokens = 64 >> kLog;
@@ -475,6 +478,10 @@ static int row_log(const HeadsParams& p) { return !p.vector ? 6 : kPieceLog + (p
 // cache 16 (forward B3 N1777 H32+8 d64 with 4, 16, 64: 14.8 13.3 18, B4 N1024 H16+16 d128 15.3 13.7 -) or, backward, where a
 // workgroup ends with a sum over its waves, 4 (B2 N2047 H8+8 d64 fp32 with 4, 16, 32: 14.8 18.4 20.7, B4 N1024 H16+16 d128
 // 24.3 23.7 23.4).
+// Elsewhere, us with 4 | 16 | 64: forward from the cache B1 N2048 H32+8 d128 bf16 14.9 11.9 20, B2 N1500 H24+24 d80 16.3 15.1
+// 19.6; from memory with 16 | 64: B1 N16384 H32+8 d128 66.5 63.7, B2 N4096 H16+16 d128 fp32 48.7 51.6, B16 N2048 H12+12 d64 fp16
+// 49.9 49.9.  Backward, where the rule is less good, from the cache with 4 | 16: the first two 23.9 19.9 and 28.3 24.5; from
+// memory with 16 | 64: the last three 104 99, 79.1 77.9, 76.7 92.3.
 void plan_heads(HeadsParams* p, bool backward) {
     const long tokens = 64 >> row_log(*p);
     const long groups = (p->tokens + tokens - 1) / tokens;  // waves that one head a wave needs
