@@ -476,9 +476,10 @@ typedef struct {
  *   workspace  leet_attn_gated_scan_workspace_bytes bytes, 256-byte aligned (NULL when that is 0); scratch
  * Decays may have any values.  Tokens are combined in tiles of up to 240 tokens and 128 channels by the
  * products of their decays, formed in fp32: of the state that enters a tile nothing is left where that
- * product is under 2^-149.  A tile that holds a decay above 1 in magnitude is taken token by token from the
- * state before it instead, and the tiles behind it wait: the recurrence as it stands, at 5 to 30 times the
- * time where every tile does (the longer the sequences and the fewer the channels, the slower).  A non-finite value makes the later values of its
+ * product is under 2^-149.  A tile in which decays above 1 in magnitude multiply to more than 16 within some
+ * sixteen tokens is taken token by token from the state before it instead, and the tiles behind it wait: the
+ * recurrence as it stands, at 5 to 30 times the time where every tile does (the longer the sequences and the
+ * fewer the channels, the slower).  A non-finite value makes the later values of its
  * channel and sequence non-finite and no others (once such a state has decayed to nothing it is NaN).
  */
 int leet_attn_gated_scan(const leet_attn_rows *x, const leet_attn_rows *gate, const leet_attn_rows *out,

@@ -20,12 +20,13 @@
 // (61 and 227 us: a tile's run is published only when the tile before it is done); a copy of both passes without branches
 // for waves whose tokens are all there (51 us, but backward 105 instead of 92: registers).
 //
-// That holds for decays of at most 1 in magnitude.  Larger ones (none of a moving average's are) can take a product, and
-// what it leaves of a zero state, out of fp32's range where the state itself is small, or cancel all but their rounding:
-// zeros with decays of 4 would be infinity times zero from token 64 on.  So a tile that holds one is no run: its tokens are
-// taken one after the other from the state before it, and the tiles behind it wait for that: some 8 us a tile of 112 tokens
-// (every decay above 1: B4 N4096 C2048 forward 305 us, N32768 C4096 2447; one token in a thousand: 78 and 374).  Watching for
-// them costs other calls 1 to 2 % (B4 N4096 C2048 52 -> 53 us, N32768 C4096 200 -> 205).
+// That holds while decays do not grow.  Ones above 1 in magnitude (none of a moving average's are) can take a product, and
+// what it leaves of a zero state, out of fp32's range where the state itself is small: zeros with decays of 4 would be infinity
+// times zero from token 64 on.  So where the decays above 1 that a wave holds multiply to more than kMostGrowth in any channel
+// the tile is no run: its tokens are taken one after the other from the state before it, and the tiles behind it wait for that:
+// some 8 us a tile of 112 tokens (decays of 4 everywhere: B4 N4096 C2048 forward 305 us, N32768 C4096 2447; one token in a
+// thousand of 20: 78 and 374).  Watching for them costs other calls 1 to 2 % (B4 N4096 C2048 52 -> 53 us, N32768 C4096 200 ->
+// 205).
 //
 // Packed sequences: where a sequence begins, the run so far is cut off.  That is decided by the offsets alone, so it
 // is the same for all channels and no arithmetic carries anything over (zero times an infinity would).
@@ -40,6 +41,10 @@ namespace leet {
 // better where sequences are very long and worse elsewhere (16 | 24 tokens: N32768 C4096 178 157, B32 N512 C4096 82 97,
 // N1000 C1024 12 14; of a moving average 186 187, 89 105, 16 20).
 constexpr int kForwardTokens = 16, kBackwardTokens = 8, kMostWaves = 15;
+
+// Of the tokens of a wave.  Fifteen waves' products then stay under 2^60, and rounding is multiplied by no more than the
+// recurrence itself multiplies it by.
+constexpr float kMostGrowth = 16.0f;
 
 // A gate as it is kept between its two uses, in one register: the decay a itself, or for the moving average the smaller of
 // a and 1 - a with the sign of the logit.  The larger one is what that leaves of 1, so both are as accurate as fp32 has
@@ -294,9 +299,9 @@ template <int kV>
 struct Shared {
     float A[kMostWaves][64 * kV], H[kMostWaves][64 * kV];  // the waves' runs
     int cut[kMostWaves];    // a sequence begins (backward: ends) in the run: what came before does not reach behind it
-    int grows[kMostWaves];  // a decay above 1 in magnitude in the run
+    int grows[kMostWaves];  // by more than kMostGrowth
     float carry[64 * kV];
-    int serial;  // one of the runs has such a decay: the waves go on one after the other
+    int serial;  // one of the runs does: the waves go on one after the other
     unsigned ticket;
 };
 
@@ -486,7 +491,7 @@ __global__ __launch_bounds__(64 * (kMostWaves + 1), kX != 0 && kG != 0 && !kPack
     // three workgroups a compute unit instead of two)
     float h[kPacked ? kTokens : 1][kV];
     float A[kV], H[kV];
-    bool grows = false;  // a decay above 1 in magnitude
+    float growth = 1.0f;  // product of the decays above 1, the larger of the channels'
 #pragma unroll
     for (int v = 0; v < kV; ++v) { A[v] = 1.0f; H[v] = 0.0f; }
 #pragma unroll
@@ -499,15 +504,16 @@ __global__ __launch_bounds__(64 * (kMostWaves + 1), kX != 0 && kG != 0 && !kPack
         float zi[kV], xi[kV];
         z[i].get(zi);
         x[i].get(xi);
+        float largest = 1.0f;
 #pragma unroll
         for (int v = 0; v < kV; ++v) {
             g[i][v].set(zi[v]);
-            // one channel's exponential and quotient after the other's: interleaved they take 67 registers instead of 63,
-            // three workgroups a unit instead of four (B4 N4096 C2048 bf16 61 us instead of 59)
-            if (kMode == 2 && v + 1 < kV) asm volatile("" : "+v"(g[i][v].g), "+v"(zi[v + 1]));
+            // one channel's exponential and quotient after the other's: interleaved they take 65 to 67 registers instead of
+            // 63, three workgroups a unit instead of four (B4 N4096 C2048 bf16 sigmoid 61 us instead of 59)
+            if (kMode != 0 && v + 1 < kV) asm volatile("" : "+v"(g[i][v].g), "+v"(zi[v + 1]));
             const float a = g[i][v].decay();
             float b = g[i][v].input(xi[v]);
-            if (kMode != 2) grows |= fabsf(a) > 1.0f;
+            largest = fmaxf(largest, fabsf(a));
             if (first) {
                 // the only place where the state is read: as soon as this run is known state_out, which may be the
                 // same memory, may be written
@@ -519,10 +525,11 @@ __global__ __launch_bounds__(64 * (kMostWaves + 1), kX != 0 && kG != 0 && !kPack
             }
             if (kPacked) h[i][v] = b;
         }
+        growth *= largest;
     }
     float state[kV];
     const bool serial = join_runs<kMode, kV, false, kPacked>(p, shared, wave, lane, A, H, kPacked && at.first != 0,
-                                                             __any(grows) && (!kPacked || at.inside), state);
+                                                             kMode != 2 && __any(growth > kMostGrowth) && (!kPacked || at.inside), state);
 #pragma unroll
     for (int i = 0; i < kTokens; ++i) {
         if (i >= count) continue;
@@ -575,7 +582,7 @@ __global__ __launch_bounds__(64 * (kMostWaves + 1)) void gated_scan_backward_ker
     const Places<kTokens> at = kPacked ? Places<kTokens>(p.offsets, p.sequences, t0, p.N, lane) : Places<kTokens>{};
     Gate<kMode> gate[kTokens][kV];
     float d[kTokens][kV], A[kV], G[kV];
-    bool grows = false;  // a decay above 1 in magnitude
+    float growth = 1.0f;  // product of the decays above 1, the larger of the channels'
 #pragma unroll
     for (int v = 0; v < kV; ++v) { A[v] = 1.0f; G[v] = 0.0f; }
 #pragma unroll
@@ -588,11 +595,12 @@ __global__ __launch_bounds__(64 * (kMostWaves + 1)) void gated_scan_backward_ker
         float zi[kV];
         z[i].get(zi);
         dh[i].get(d[i]);
+        float largest = 1.0f;
 #pragma unroll
         for (int v = 0; v < kV; ++v) {
             gate[i][v].set(zi[v]);
             const float a = gate[i][v].decay();
-            if (kMode != 2) grows |= fabsf(a) > 1.0f;
+            largest = fmaxf(largest, fabsf(a));
             if (last) {
                 d[i][v] += leaves[v];
                 G[v] = a * d[i][v];
@@ -601,10 +609,11 @@ __global__ __launch_bounds__(64 * (kMostWaves + 1)) void gated_scan_backward_ker
                 A[v] *= a;
             }
         }
+        growth *= largest;
     }
     float g[kV];  // the gradient that comes in from behind
     const bool serial = join_runs<kMode, kV, true, kPacked>(p, shared, wave, lane, A, G, kPacked && at.last != 0,
-                                                            __any(grows) && (!kPacked || at.inside), g);
+                                                            kMode != 2 && __any(growth > kMostGrowth) && (!kPacked || at.inside), g);
 #pragma unroll
     for (int i = kTokens - 1; i >= 0; --i) {
         if (i >= count || !live || (kPacked && !(at.inside >> i & 1))) continue;

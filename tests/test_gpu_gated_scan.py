@@ -519,7 +519,7 @@ def test_the_sizes_of_a_batch_of_prompts(leet, backward):
 def _growing(B, N, C, dtype, gdt, mode, seed):
     """x, gate and entering state with decays above 1 in magnitude; by the channel's number modulo 5: zeros under decays of
     4; a state of 1 that decays of 4 and inputs of -3 leave as it is (mode 0: 4 is exact); decays that grow and shrink by
-    turns; one single decay of -8 (mode 1: 8) among ordinary ones; ordinary ones alone."""
+    turns; one single decay of -20 (mode 1: e^3) among ordinary ones; ordinary ones alone."""
     x, z, s = _normal((B, N, C), F32, seed), _gate((B, N, C), F32, mode, seed + 1), _normal((B, C), F32, seed + 2, 3.0)
     log = torch.where(torch.arange(N, device="cuda") % 200 < 100, 0.25, -0.25).expand(B, N)
     of = [torch.arange(C)[i::5] for i in range(5)]
@@ -528,7 +528,7 @@ def _growing(B, N, C, dtype, gdt, mode, seed):
     x[..., of[0]], s[..., of[0]] = 0.0, 0.0
     x[..., of[1]], s[..., of[1]] = (-3.0, 1.0) if mode == 0 else (0.0, 0.0)
     z[..., of[2]] = (log.exp() if mode == 0 else log)[..., None]
-    z[:, N // 2, of[3]] = -8.0 if mode == 0 else 2.0
+    z[:, N // 2, of[3]] = -20.0 if mode == 0 else 3.0
     return x.to(dtype), z.to(gdt), s, of
 
 
@@ -596,13 +596,14 @@ def test_decays_above_one_in_packed_sequences(leet, lengths, mode):
         assert forms.close(part(din[j:j + 1]), to_s, F32)
 
 
+@pytest.mark.parametrize("above", [1.5, 20.0])
 @pytest.mark.parametrize("packed", [False, True])
-def test_one_tile_with_decays_above_one_among_many(leet, packed):
-    """A long chain whose runs are joined, but for single tiles that wait for the state before them."""
+def test_one_tile_with_decays_above_one_among_many(leet, packed, above):
+    """A long chain whose runs are joined, but for single tiles that wait for the state before them (not for 1.5)."""
     N, C, mode = 9000, 320, 0
     x, z, s = _normal((1, N, C), F32, 210), _gate((1, N, C), F32, mode, 211), _normal((3 if packed else 1, C), F32, 212, 3.0)
     for t, c in ((0, 5), (1, 200), (4000, 319), (4100, 0), (4101, 0), (8999, 130)):
-        z[0, t, c] = 1.5
+        z[0, t, c] = above
     off = _offsets([4050, 0, 4950]).cuda() if packed else None
     dh, ds = _normal((1, N, C), F32, 213), _normal(s.shape, F32, 214)
     left, din = torch.empty_like(s), torch.empty_like(s)
@@ -617,3 +618,14 @@ def test_one_tile_with_decays_above_one_among_many(leet, packed):
         assert forms.close(dx[:, at], to_x) and forms.close(dz[:, at], to_z) and forms.close(din[j:j + 1], to_s)
     for _ in range(5):
         assert torch.equal(h, leet.leet_attn_gated_scan(x, z, mode=mode, state_in=s, offsets=off))
+
+
+@pytest.mark.parametrize("mode", [0, 1])
+@pytest.mark.parametrize("types", [(BF16, F32), (F32, F32)])
+def test_decays_a_little_above_one(leet, mode, types):
+    """Growth that a run's products hold: up to sixteen times over the tokens of a wave, and what is just beyond."""
+    B, N, C = 5, 900, 514
+    rate = torch.linspace(0.0, 0.2, C).expand(B, N, C).clone()   # ln 16 / 16 = 0.173 is the border of sixteen tokens
+    rate *= torch.where(torch.arange(N) % 60 < 30, 1.0, -1.05)[None, :, None]
+    z = (rate.exp() if mode == 0 else rate).to(types[1]).cuda()
+    _check(leet, B, N, C, types, mode, True, gate=z)
