@@ -24,8 +24,8 @@
 // what it leaves of a zero state, out of fp32's range where the state itself is small: zeros with decays of 4 would be infinity
 // times zero from token 64 on.  So where the decays above 1 that a wave holds multiply to more than kMostGrowth in any channel
 // the tile is no run: its tokens are taken one after the other from the state before it, and the tiles behind it wait for that:
-// some 8 us a tile of 112 tokens (decays of 4 everywhere: B4 N4096 C2048 forward 305 us, N32768 C4096 2447; one token in a
-// thousand of 20: 78 and 374).  Watching for them costs other calls 1 to 2 % (B4 N4096 C2048 52 -> 53 us, N32768 C4096 200 ->
+// some 8 us a tile of 112 tokens (every decay beyond that: B4 N4096 C2048 forward 305 us, N32768 C4096 2447; one token in a
+// thousand of 20: 86 and 455).  Watching for them costs other calls 1 to 2 % (B4 N4096 C2048 52 -> 53 us, N32768 C4096 200 ->
 // 205).
 //
 // Packed sequences: where a sequence begins, the run so far is cut off.  That is decided by the offsets alone, so it
