@@ -428,7 +428,8 @@ int leet_attn_qk_norm_rope(const leet_attn_heads *q, const leet_attn_heads *out_
  *   dout_q, dout_k        gradients of the outputs
  *   dq, dk                gradients of the inputs; each may be the gradient it comes from, or the input
  *                         (same data and strides)
- *   dq_weight, dk_weight  [d] of weight_dtype, two of them, or NULL: not wanted
+ *   dq_weight, dk_weight  [d] of weight_dtype, two of them, or NULL: not wanted.  Written when all inputs
+ *                         have been read, so each may be its weight
  *   workspace             leet_attn_qk_norm_rope_workspace_bytes bytes, 256-byte aligned; may be NULL
  *                         when neither weight's gradient is wanted.  Its contents are scratch
  * The sums over tokens and heads are taken in fp32 in a fixed order: no atomics, equal from call to call.

@@ -273,6 +273,17 @@ def test_gradient_in_place(leet):
     assert got[0] is dq and all(torch.equal(a, b) for a, b in zip(want, got))
 
 
+@pytest.mark.parametrize("d, rot", [(128, 64), (34, 10)])
+def test_gradient_over_the_inputs(leet, d, rot):
+    """Gradients of inputs and weights in the place of the inputs and weights, parts of one projection."""
+    q, k = _fused(2, 333, 6, 3, d, BF16, 44)
+    dq, dk = _normal((2, 6, 333, d), BF16, 45), _normal((2, 3, 333, d), BF16, 46)
+    wq, wk = _normal((d,), BF16, 47, 0.3, 1.0), _normal((d,), BF16, 48, 0.3, 1.0)
+    want = leet.leet_attn_qk_norm_rope_backward(dq, dk, q, k, wq, wk, _freq(rot).cuda())
+    got = leet.leet_attn_qk_norm_rope_backward(dq, dk, q, k, wq, wk, _freq(rot).cuda(), dx_q=q, dx_k=k, dq_weight=wq, dk_weight=wk)
+    assert got[0] is q and got[3] is wk and all(torch.equal(a, b) for a, b in zip(want, got))
+
+
 def test_on_another_stream_and_in_a_graph(leet):
     q, k = _fused(2, 300, 4, 4, 128, BF16, 50)
     dq, dk = _normal((2, 4, 300, 128), BF16, 51), _normal((2, 4, 300, 128), BF16, 52)
