@@ -326,6 +326,36 @@ int leet_attn_query_plan(int B, int H, int N, int d, int dtype, int segments, in
 /* The same for rank r and value width dv given separately (shapes as for leet_attn_forward_rd). */
 int leet_attn_query_plan_rd(int B, int H, int N, int r, int dv, int dtype, int segments, int *nseg, int *kernel);
 
+/*
+ * Backward pass of the prefill: gradients of q, k, v and of the entering state from that of the output,
+ *     dq_i = sum over j <= i of gamma^(i-j) (dout_i . v_j) k_j  +  gamma^(i+1) state_in dout_i,
+ *     dk_j = sum over i >= j of gamma^(i-j) (v_j . dout_i) q_i  +  gamma^(N-1-j) dstate_out v_j,
+ *     dv_j = sum over i >= j of gamma^(i-j) (k_j . q_i) dout_i  +  gamma^(N-1-j) k_j dstate_out,
+ *     dstate_in = sum over i of gamma^(i+1) q_i^T dout_i  +  gamma^N dstate_out.
+ * The scores are formed again, nothing of the forward call has to be kept but its inputs.  gamma is a fixed number a head
+ * (as in the paper) and has no gradient.
+ *   dout         [B][H][N][dv] of `dtype`: the gradient of `out`.  A 16-bit call's gradient is taken in 16 bits whatever the
+ *                forward call's out_dtype was
+ *   q, k, v      what the forward call was given
+ *   dq, dk, dv_out  [B][H][N][r], [B][H][N][r], [B][H][N][dv] of `dtype`, rounded once, at the store
+ *   state_in     what the forward call was given ([B][H][r][dv] float or NULL)
+ *   dstate_out   the gradient of its state_out, or NULL: zero
+ *   dstate_in    [B][H][r][dv] float or NULL: not wanted
+ *   workspace    leet_attn_backward_workspace_bytes bytes for the same `segments`, 256-byte aligned (NULL when that is 0);
+ *                always the caller's, so calls on several streams and captured graphs share nothing.  Scratch
+ *   segments     as for leet_attn_forward_ex
+ * Shapes as for leet_attn_forward_rd, `dtype` any leet_dtype, `mask` a leet_mask (gamma may be NULL for LEET_MASK_CAUSAL).
+ * Inside, scores and, as operands of products, states are rounded to the input type, as in the forward pass; states are
+ * carried in fp32, and dstate_in is exact to fp32's products.  In fp16 scores and states beyond 65504 are infinite.
+ * Outputs and workspace that share memory with one another or with an input are LEET_ERR_INVALID_ARG.  N = 0 is legal and
+ * hands the state's gradient on.
+ */
+int leet_attn_backward(const void *dout, const void *q, const void *k, const void *v, const float *gamma,
+                       void *dq, void *dk, void *dv_out, const float *state_in, const float *dstate_out, float *dstate_in,
+                       void *workspace, size_t workspace_bytes, int segments,
+                       int B, int H, int N, int r, int dv, int dtype, int mask, void *stream);
+size_t leet_attn_backward_workspace_bytes(int B, int H, int N, int r, int dv, int dtype, int segments);
+
 /* ------------------------------------------------------------------------------------------------
  * Operators beside the attention: what makes its queries and keys (position rotation, norms of each
  * head), and the element-wise recurrence with a decay of its own for every token and channel.

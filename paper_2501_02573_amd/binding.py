@@ -65,6 +65,8 @@ EXPORTED_SYMBOLS = (
     "leet_attn_gated_scan_backward",
     "leet_attn_gated_scan_workspace_bytes",
     "leet_attn_gated_scan_step",
+    "leet_attn_backward",
+    "leet_attn_backward_workspace_bytes",
     "leet_attn_strerror",
     "leet_attn_version",
 )
@@ -170,6 +172,10 @@ def _load() -> ctypes.CDLL:
     lib.leet_attn_gated_scan_workspace_bytes.restype = sz
     lib.leet_attn_gated_scan_step.argtypes = [rows, rows, rows, vp, i, i, i, i, i, vp]
     lib.leet_attn_gated_scan_step.restype = i
+    lib.leet_attn_backward.argtypes = [vp] * 12 + [sz, i, i, i, i, i, i, i, i, vp]
+    lib.leet_attn_backward.restype = i
+    lib.leet_attn_backward_workspace_bytes.argtypes = [i, i, i, i, i, i, i]
+    lib.leet_attn_backward_workspace_bytes.restype = sz
     lib.leet_attn_strerror.argtypes = [i]
     lib.leet_attn_strerror.restype = ctypes.c_char_p
     lib.leet_attn_version.argtypes = []
@@ -694,6 +700,49 @@ def leet_attn_decode_step_rd(q, k, v, gamma: Optional[torch.Tensor], state, out:
     if st != LEET_OK:
         raise LeetAttnError(st, "leet_attn_decode_step_v3" if store is not None else "leet_attn_decode_step_rd")
     return out
+
+
+# ---------------------------------------------------------------- backward pass of the prefill
+def backward_workspace_bytes(B: int, H: int, N: int, r: int, dv: int, dtype: int, segments: int = 0) -> int:
+    return int(lib.leet_attn_backward_workspace_bytes(B, H, N, r, dv, dtype, segments))
+
+
+def leet_attn_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                       gamma: Optional[torch.Tensor], dq: Optional[torch.Tensor] = None,
+                       dk: Optional[torch.Tensor] = None, dv: Optional[torch.Tensor] = None,
+                       state_in: Optional[torch.Tensor] = None, dstate_out: Optional[torch.Tensor] = None,
+                       dstate_in: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                       segments: int = 0, mask: int = LEET_MASK_DECAY):
+    """Gradients of the prefill: (dq, dk, dv) in the type of q, k, v, and dstate_in (float32 [B, H, r, dv]) where given.
+
+    ``dout``: the gradient of the output, in the type of q, k, v (round the float32 gradient of a float32 output of 16-bit
+    inputs first: the products take it in 16 bits anyhow).  ``state_in`` is what the forward call was given, ``dstate_out``
+    the gradient of its state_out.  ``gamma`` has no gradient.  Autograd sees nothing of the call; a workspace that the
+    caller does not bring comes from torch's allocator and belongs to this call alone."""
+    if dq is None:
+        dq = _new_out(q, q.dtype)
+    if dk is None:
+        dk = _new_out(k, q.dtype)
+    if dv is None:
+        dv = _new_out(v, q.dtype)
+    B, H, N, r, w = _check_rd(q, k, v, gamma, dout, True)
+    for name, t, like in (("dout", dout, v), ("dq", dq, q), ("dk", dk, k), ("dv", dv, v)):
+        if t.dtype != q.dtype:
+            raise TypeError(f"{name} must have the type of q, k, v")
+        if t.shape != like.shape:
+            raise ValueError(f"{name} must have the shape {list(like.shape)}")
+    _check_states_rd(B, H, r, w, state_in=state_in, dstate_out=dstate_out, dstate_in=dstate_in)
+    dev = _check_dev(q, k, v, gamma, dout, dq, dk, dv, state_in, dstate_out, dstate_in, workspace)
+    code = _dtype_code(q)
+    _sizes("leet_attn_backward", B, H, N, r, w)
+    need = backward_workspace_bytes(B, H, N, r, w, code, segments) if workspace is None else 0
+    ws, ws_bytes, keep = _scratch(need, workspace, dev.index)
+    st = _call(lib.leet_attn_backward, dev, _ptr(dout), _ptr(q), _ptr(k), _ptr(v), _ptr(gamma), _ptr(dq), _ptr(dk),
+               _ptr(dv), _ptr(state_in), _ptr(dstate_out), _ptr(dstate_in), ws, ws_bytes, int(segments), B, H, N, r, w,
+               code, int(mask))
+    if st != LEET_OK:
+        raise LeetAttnError(st, "leet_attn_backward")
+    return dq, dk, dv
 
 
 # ---- operators beside the attention -------------------------------------------------------------------------------

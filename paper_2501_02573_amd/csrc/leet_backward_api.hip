@@ -1,0 +1,137 @@
+// C ABI of the attention's backward pass: argument checks, segments, launches.  Nothing here touches tensor data.
+#include "../../include/leet_attn.h"
+#include "leet_backward.hpp"
+#include "leet_common.hpp"
+#include "leet_host.hpp"
+#include "leet_overlap.hpp"
+
+namespace leet {
+hipError_t launch_state_pass(const float* state_in, float* state_out, int BH, int D, int DV, hipStream_t stream);
+hipError_t launch_seg_scan(float* seg_state, const float* state_in, float* state_copy, const float* gamma, int BH, int H,
+                           int nseg, int seg_tokens, int step, int D, int DV, hipStream_t stream);
+}  // namespace leet
+
+namespace {
+
+using leet::kChunk;
+using leet::Span;
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+bool shape_ok(int r, int dv, int dtype) {
+    if (dtype != LEET_F32 && dtype != LEET_BF16 && dtype != LEET_F16) return false;
+    return (r == dv && (r == 64 || r == 128)) || (r == 128 && dv == 256 && dtype != LEET_F32);
+}
+
+struct Plan {
+    int nseg, seg_chunks;
+    size_t ws_bytes;  // states of both directions at the boundaries of segments
+};
+
+bool make_plan(long BH, int N, int r, int dv, int dtype, int segments, Plan* plan) {
+    const int nchunks = (N + kChunk - 1) / kChunk;
+    long want = segments;
+    if (segments == 0) {
+        want = (512 + 3 * BH - 1) / (3 * BH);
+        const long cap = nchunks / 4;
+        if (want > cap) want = cap;
+    }
+    if (want < 1) want = 1;
+    if (want > nchunks) want = nchunks;
+    plan->seg_chunks = (int)((nchunks + want - 1) / want);
+    plan->nseg = (nchunks + plan->seg_chunks - 1) / plan->seg_chunks;
+    plan->ws_bytes = (size_t)2 * BH * (plan->nseg - 1) * r * dv * sizeof(float);
+    // workgroups of up to 512 threads, three a segment; fewer than 2^32 threads a launch
+    return BH * plan->nseg < 1L << 21;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t leet_attn_backward_workspace_bytes(int B, int H, int N, int r, int dv, int dtype, int segments) {
+    Plan plan;
+    if (B <= 0 || H <= 0 || N <= 0 || segments < 0 || !shape_ok(r, dv, dtype) || (long)B * H >= 1L << 21 || N > 1 << 30 ||
+        !make_plan((long)B * H, N, r, dv, dtype, segments, &plan))
+        return 0;
+    return plan.ws_bytes;
+}
+
+int leet_attn_backward(const void *dout, const void *q, const void *k, const void *v, const float *gamma,
+                       void *dq, void *dk, void *dv_out, const float *state_in, const float *dstate_out, float *dstate_in,
+                       void *workspace, size_t workspace_bytes, int segments,
+                       int B, int H, int N, int r, int dv, int dtype, int mask, void *stream) {
+    if (mask != LEET_MASK_DECAY && mask != LEET_MASK_CAUSAL) return LEET_ERR_INVALID_ARG;
+    if (B <= 0 || H <= 0 || N < 0 || r <= 0 || dv <= 0 || segments < 0) return LEET_ERR_INVALID_ARG;
+    if (mask == LEET_MASK_CAUSAL) gamma = nullptr;
+    if ((N > 0 && (!dout || !q || !k || !v || !dq || !dk || !dv_out)) || (!gamma && mask == LEET_MASK_DECAY))
+        return LEET_ERR_INVALID_ARG;
+    if (!shape_ok(r, dv, dtype)) return LEET_ERR_UNSUPPORTED;
+    for (const void* t : {dout, q, k, v, (const void*)dq, (const void*)dk, (const void*)dv_out, (const void*)state_in,
+                          (const void*)dstate_out, (const void*)dstate_in})
+        if (!aligned16(t)) return LEET_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(gamma) & 3u) || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return LEET_ERR_INVALID_ARG;
+    const long BH = (long)B * H;
+    if (BH >= 1L << 21 || N > 1 << 30) return LEET_ERR_TOO_LARGE;
+    Plan plan = {1, 0, 0};
+    if (N > 0 && !make_plan(BH, N, r, dv, dtype, segments, &plan)) return LEET_ERR_TOO_LARGE;
+    if (plan.ws_bytes && (!workspace || workspace_bytes < plan.ws_bytes)) return LEET_ERR_INVALID_ARG;
+
+    const long long isz = dtype == LEET_F32 ? 4 : 2, rows = (long long)BH * N, states = (long long)BH * r * dv;
+    const Span outs[] = {Span(dq, isz, rows * r), Span(dk, isz, rows * r), Span(dv_out, isz, rows * dv), Span(dstate_in, 4, states),
+                         Span(plan.ws_bytes ? workspace : nullptr, 1, (long long)plan.ws_bytes)};
+    const Span ins[] = {Span(dout, isz, rows * dv), Span(q, isz, rows * r), Span(k, isz, rows * r), Span(v, isz, rows * dv),
+                        Span(gamma, 4, H), Span(state_in, 4, states), Span(dstate_out, 4, states)};
+    for (const Span& out : outs) {
+        for (const Span& in : ins)
+            if (overlap(out, in)) return LEET_ERR_INVALID_ARG;
+        for (const Span& other : outs)
+            if (&other != &out && overlap(out, other)) return LEET_ERR_INVALID_ARG;
+    }
+
+    int dev = 0;
+    const int status = leet::current_device(&dev);
+    if (status != LEET_OK) return status;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (N == 0) {
+        // the state is handed on as it is, and so is its gradient
+        const hipError_t e = leet::launch_state_pass(dstate_out, dstate_in, (int)BH, r, dv, s);
+        return e == hipSuccess ? LEET_OK : LEET_ERR_LAUNCH;
+    }
+
+    float* slots = static_cast<float*>(workspace);
+    float* slots_back = slots + plan.ws_bytes / 2 / sizeof(float);
+    leet::BwdParams p = {};
+    p.gamma = gamma;
+    p.BH = (int)BH; p.H = H; p.N = N;
+    p.nseg = plan.nseg; p.seg_chunks = plan.seg_chunks;
+    // dq: the state transposed, [dv][r], in the order of the tokens; dk: the gradient of the state transposed, reversed; dv:
+    // that gradient, [r][dv].  Slots hold [dv][r].
+    const leet::BwdRole of_q = {dout, v, k, dq, state_in, nullptr, slots, 1, dv, r, 1, 0};
+    const leet::BwdRole of_k = {v, dout, q, dk, dstate_out, nullptr, slots_back, 1, dv, r, 1, 1};
+    const leet::BwdRole of_v = {k, q, dout, dv_out, dstate_out, dstate_in, slots_back, dv, 1, 1, r, 1};
+
+    const bool f32 = dtype == LEET_F32, f16 = dtype == LEET_F16, fine = dstate_in != nullptr;
+    hipError_t e = hipSuccess;
+    p.role[0] = of_q;
+    p.role[1] = of_k;
+    p.roles = 2;
+    if (plan.nseg > 1) {
+        e = f32 ? leet::launch_bwd_f32_states(p, r, s) : leet::launch_bwd_16bit_states(p, dv, r, f16, fine, s);
+        if (e == hipSuccess)
+            e = leet::launch_seg_scan(slots, nullptr, nullptr, gamma, 2 * (int)BH, H, plan.nseg, plan.seg_chunks * kChunk, 1, dv, r, s);
+    }
+    if (e == hipSuccess && r == dv) {
+        p.role[2] = of_v;
+        p.roles = 3;
+        e = f32 ? leet::launch_bwd_f32_walk(p, r, s) : leet::launch_bwd_16bit_walk(p, r, r, f16, fine, s);
+    } else if (e == hipSuccess) {
+        e = leet::launch_bwd_16bit_walk(p, dv, r, f16, fine, s);
+        p.role[0] = of_v;
+        p.roles = 1;
+        if (e == hipSuccess) e = leet::launch_bwd_16bit_walk(p, r, dv, f16, fine, s);
+    }
+    return e == hipSuccess ? LEET_OK : LEET_ERR_LAUNCH;
+}
+
+}  // extern "C"

@@ -1,0 +1,384 @@
+// Backward pass of the decayed causal linear attention for 16-bit inputs, bf16 or fp16 (gfx950,
+// v_mfma_f32_32x32x16_{bf16,f16}, fp32 accumulate).
+//
+// With M[i][j] = gamma^(i-j) for i >= j (Section 2.2, Eq. "BCMV"; the paper has no backward pass) and dO the gradient of O:
+//
+//     dQ = ((dO V^T) .* M) K + (state)      dK = ((V dO^T) .* M^T) Q + (state)      dV = ((K Q^T) .* M^T) dO + (state)
+//
+// Each is the attention itself over other operands, out = ((X Y^T) .* M) Z: dQ in the order of the tokens with
+// (X, Y, Z) = (dO, V, K), dK and dV in the reversed order, where M^T is M, with (V, dO, Q) and (K, Q, dO).  So one
+// kernel walks the 64-token chunks of a segment in the role's order with the state S = sum of Y^T Z in MFMA accumulators,
+// and the scores are formed again, never stored:
+//
+//     O_t     = ((X_t Y_t^T) .* D) Z_t + Lam (X_t S_t)       D[i][j] = gamma^(i-j), i >= j
+//     S_{t+1} = gamma^L S_t + (Gam Y_t)^T Z_t
+//
+// In the order of the tokens S is the transposed state before a chunk: Lam = gamma^(i+1), Gam = gamma^(L-1-j).  Reversed, S
+// is the gradient of the state that the chunk's last token leaves: Lam = gamma^i, Gam = gamma^(L-j).
+#include "leet_backward.hpp"
+#include "leet_common.hpp"
+
+namespace leet {
+namespace bwd {
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+template <int D, int DV>
+struct Smem16 {
+    static constexpr int RS = D + 8;                      // row strides (elements): 16-byte reads of 32 rows spread over the banks
+    static constexpr int RSZ = DV + (DV > 128 ? 32 : 16);  // read through ds_read_b64_tr_b16 only; holds the output scratch
+    uint16_t x[kChunk * RS];
+    uint16_t y[kChunk * RS];
+    uint16_t z[kChunk * RSZ];
+    u32x4 pfrag[3][2][64];   // masked score tiles as B operands: [tile][register half][lane]
+    float pw[kChunk + 4];    // gamma^n, n = 0..64
+    float gw[kChunk];        // Gam
+};
+
+__device__ __forceinline__ u32x4 frag16(const uint16_t* p) { return *reinterpret_cast<const u32x4*>(p); }
+
+// ds_read_b64_tr_b16: within each group of 16 lanes, lane i receives element i%4 of the 8-byte rows addressed by lanes
+// i/4, 4+i/4, 8+i/4, 12+i/4 of the group.
+__device__ __forceinline__ u32x2 lds_tr(const uint16_t* p) {
+    s16x4 r = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+        (__attribute__((address_space(3))) s16x4*)(const_cast<uint16_t*>(p)));
+    return __builtin_bit_cast(u32x2, r);
+}
+__device__ __forceinline__ u32x4 join(u32x2 a, u32x2 b) { return u32x4{a.x, a.y, b.x, b.y}; }
+
+// registers 8h .. 8h+7 of an accumulator tile -> 16-bit operand
+template <typename E>
+__device__ __forceinline__ u32x4 pack_half(const f32x16& acc, int h) {
+    u32x4 r;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) r[e] = E::pack2(acc[8 * h + 2 * e], acc[8 * h + 2 * e + 1]);
+    return r;
+}
+
+// Eight 16-bit values times eight fp32 weights as kTerms 16-bit values that add up to the product.  What is left for the next
+// term is taken from the packed word itself: the compiler may form the fp16 of a product in two ways, once from the product
+// rounded to fp32 and once not, and the two differ now and then by a step.
+template <typename E, int kTerms>
+__device__ __forceinline__ void scaled(u32x4 x, f32x4 w0, f32x4 w1, u32x4 (&out)[kTerms]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        float a = E::lo(x[e]) * ((e < 2) ? w0[2 * e] : w1[2 * e - 4]);
+        float b = E::hi(x[e]) * ((e < 2) ? w0[2 * e + 1] : w1[2 * e - 3]);
+#pragma unroll
+        for (int t = 0; t < kTerms; ++t) {
+            uint32_t word = E::pack2(a, b);
+            if (t + 1 < kTerms) asm("" : "+v"(word));
+            out[t][e] = word;
+            a -= E::lo(word);
+            b -= E::hi(word);
+        }
+    }
+}
+
+// Score tiles in production order: tile 0 = (jt 0, it 0), tile 1 = (jt 1, it 1), tile 2 = (jt 0, it 1).
+__device__ __forceinline__ constexpr int tile_jt(int n) { return n == 1 ? 1 : 0; }
+__device__ __forceinline__ constexpr int tile_it(int n) { return n == 0 ? 0 : 1; }
+
+// kOut = true: outputs and state.  kOut = false: state only, of every segment but the last, started from zero.
+template <int D, int DV, bool kOut, typename E, bool kDecay, int kTerms>
+__global__ __launch_bounds__(DV * 2, D > 128 || DV > 128 ? 1 : 2) void walk16_kernel(BwdParams p) {
+    constexpr int NT = DV * 2;   // threads: one wave per 32 columns of z and out
+    constexpr int NW = DV / 32;  // waves
+    constexpr int DT = D / 32;   // 32-row tiles of the state
+    constexpr int PR = D / 8, PRZ = DV / 8;  // 16-byte pieces per row
+    constexpr int XP = kChunk * PR / NT, ZP = kChunk * PRZ / NT;  // pieces per thread per chunk
+    constexpr int RS = Smem16<D, DV>::RS, RSZ = Smem16<D, DV>::RSZ;
+    static_assert(kChunk * RSZ * 2 >= NW * 32 * 20 * 4, "the z tile must hold the output scratch");
+    __shared__ __attribute__((aligned(16))) Smem16<D, DV> sm;
+
+    const int tid = threadIdx.x;
+    const int w = tid >> 6, l = tid & 63, ln = l & 31, g = l >> 5;
+    // workgroups go to the eight XCDs in turn: the roles of a unit share an XCD's L2
+    const int nseg = kOut ? p.nseg : p.nseg - 1;
+    const int slot = blockIdx.x >> 3, which = slot % p.roles, unit = (slot / p.roles) * 8 + (blockIdx.x & 7);
+    if (unit >= p.BH * nseg) return;
+    const BwdRole& role = p.role[which];
+    const bool rev = role.reversed != 0;
+    const int bh = unit / nseg;
+    const int seg = rev ? nseg - 1 - unit % nseg : unit % nseg;
+    const int h = bh % p.H;
+
+    const int tok_begin = seg * p.seg_chunks * kChunk;
+    const int tok_end = (seg == p.nseg - 1) ? p.N : tok_begin + p.seg_chunks * kChunk;
+    const int nchunks = (tok_end - tok_begin + kChunk - 1) / kChunk;
+
+    // token t of the walk is row t, or N - 1 - t, of the tensors
+    const size_t first = (size_t)bh * p.N + (rev ? p.N - 1 : 0);
+    const ptrdiff_t row = rev ? -D : D, row_z = rev ? -DV : DV;
+    const uint16_t* xb = static_cast<const uint16_t*>(role.x) + first * D;
+    const uint16_t* yb = static_cast<const uint16_t*>(role.y) + first * D;
+    const uint16_t* zb = static_cast<const uint16_t*>(role.z) + first * DV;
+    uint16_t* ob = static_cast<uint16_t*>(role.out) + first * DV;
+
+    if (kDecay) {  // fp64 -> fp32 once per workgroup
+        const double gd = (double)p.gamma[h];
+        for (int n = tid; n <= kChunk; n += NT) {
+            const float v = (float)pow_int(gd, n);
+            sm.pw[n] = v;
+            const int j = kChunk - 1 + (rev ? 1 : 0) - n;
+            if (j >= 0 && j < kChunk) sm.gw[j] = v;
+        }
+    }
+
+    // state slice: S[t][r] = S[dk = 32t + pi(m(r, g))][c = 32w + ln]
+    f32x16 S[DT];
+    const int c_own = 32 * w + ln;
+    auto dk_of = [&](int t, int r) {
+        // m = 8(r/4) + 4g + r%4 ; pi swaps the 4- and 8-bits: dk = 16(r/8) + 8g + 4((r/4)&1) + r%4
+        return 32 * t + 16 * (r >> 3) + 8 * g + 4 * ((r >> 2) & 1) + (r & 3);
+    };
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) S[t][r] = 0.0f;
+    if (kOut && seg > 0) {
+        const float* src = role.slots + ((size_t)bh * (p.nseg - 1) + seg - 1) * D * DV + (size_t)c_own * role.slot_col;
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) S[t][r] = src[dk_of(t, r) * role.slot_row];
+    }
+    if (kOut && role.enter) {
+        const float* src = role.enter + (size_t)bh * D * DV + (size_t)c_own * role.enter_col;
+        const float left = kDecay ? (float)pow_int((double)p.gamma[h], tok_begin) : 1.0f;
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) S[t][r] += left * src[dk_of(t, r) * role.enter_row];
+    }
+
+    // per-lane LDS bases; every fragment address below is one of these plus a constant
+    const int s16 = l & 15, half = (l >> 4) & 1;
+    const uint16_t* x_row = &sm.x[ln * RS + 8 * g];   // + 32*it*RS + 16*s
+    const uint16_t* y_row = &sm.y[ln * RS + 8 * g];   // + 32*jt*RS + 16*s
+    // transposing reads: lane supplies row 4g + s16/4 (+ 8*rd + 16*f) and four consecutive columns
+    const uint16_t* z_tr = &sm.z[(4 * g + (s16 >> 2)) * RSZ + 32 * w + 16 * half + 4 * (s16 & 3)];
+    const uint16_t* y_tr = &sm.y[(4 * g + (s16 >> 2)) * RS + 16 * half + 8 * (s16 & 1) + 4 * ((s16 >> 1) & 1)];
+
+    __syncthreads();  // tables visible
+
+    // Decay weights of the score tiles this wave produces.  wgt[0]: a tile on the diagonal (i - j = ln - jr, zero above the
+    // diagonal); wgt[1]: the tile below it (i - j = 32 + ln - jr).  With four waves each wave needs one set.
+    constexpr bool kBothSets = NW < 3;
+    f32x16 wgt[kBothSets ? 2 : 1];
+    const int later = rev ? 0 : 1;
+    float lam_full[2];  // Lam of a full chunk
+    if (kOut) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int n = ln - (8 * (r >> 2) + 4 * g + (r & 3));
+            const float diag = (n >= 0) ? (kDecay ? sm.pw[max(n, 0)] : 1.0f) : 0.0f;
+            const float below = kDecay ? sm.pw[32 + n] : 1.0f;
+            if (kBothSets) {
+                wgt[0][r] = diag;
+                wgt[kBothSets ? 1 : 0][r] = below;
+            } else {
+                wgt[0][r] = (w == 2) ? below : diag;
+            }
+        }
+        lam_full[0] = kDecay ? sm.pw[ln + later] : 1.0f;
+        lam_full[1] = kDecay ? sm.pw[32 + ln + later] : 1.0f;
+    }
+
+    u32x4 rx[XP], ry[XP], rz[ZP];
+    auto prefetch = [&](int tok0) {
+        const int shift = max(0, tok0 + kChunk - tok_end);  // rows [0, shift) of the tile stay zero
+        const u32x4 zero = {0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int r = 0; r < XP; ++r) {
+            const int piece = r * NT + tid, j = piece / PR, cc = piece % PR;
+            const bool ok = j >= shift;
+            const ptrdiff_t off = (tok0 - shift + j) * row + cc * 8;
+            if (kOut) rx[r] = ok ? *reinterpret_cast<const u32x4*>(xb + off) : zero;
+            ry[r] = ok ? *reinterpret_cast<const u32x4*>(yb + off) : zero;
+        }
+#pragma unroll
+        for (int r = 0; r < ZP; ++r) {
+            const int piece = r * NT + tid, j = piece / PRZ, cc = piece % PRZ;
+            const ptrdiff_t off = (tok0 - shift + j) * row_z + cc * 8;
+            rz[r] = j >= shift ? *reinterpret_cast<const u32x4*>(zb + off) : zero;
+        }
+    };
+
+    prefetch(tok_begin);
+
+    for (int t = 0; t < nchunks; ++t) {
+        const int tok0 = tok_begin + t * kChunk;
+        const int Lc = min(kChunk, tok_end - tok0);
+        const int shift = kChunk - Lc;  // a ragged last chunk is right-aligned in the tile, rows above are zero
+
+        if (t > 0) __syncthreads();  // everyone is done reading the previous chunk's tiles and score fragments
+#pragma unroll
+        for (int r = 0; r < XP; ++r) {
+            const int piece = r * NT + tid, j = piece / PR, cc = piece % PR;
+            if (kOut) *reinterpret_cast<u32x4*>(&sm.x[j * RS + cc * 8]) = rx[r];
+            *reinterpret_cast<u32x4*>(&sm.y[j * RS + cc * 8]) = ry[r];
+        }
+#pragma unroll
+        for (int r = 0; r < ZP; ++r) {
+            const int piece = r * NT + tid, j = piece / PRZ, cc = piece % PRZ;
+            *reinterpret_cast<u32x4*>(&sm.z[j * RSZ + cc * 8]) = rz[r];
+        }
+        __syncthreads();
+        if (t + 1 < nchunks) prefetch(tok0 + kChunk);  // in flight during the MFMA work below
+
+        f32x16 o[2];
+        if (kOut) {
+            // P^T = Y X^T, masked, for the score tiles this wave produces
+#pragma unroll
+            for (int n = 0; n < 3; ++n) {
+                if (n % NW != w) continue;
+                f32x16 acc;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[r] = 0.0f;
+#pragma unroll
+                for (int s = 0; s < D / 16; ++s)
+                    acc = E::mfma32(frag16(y_row + 32 * tile_jt(n) * RS + 16 * s),
+                                    frag16(x_row + 32 * tile_it(n) * RS + 16 * s), acc);
+                if (kDecay || n != 2) {  // without decay the tile below the diagonal needs no weights
+                    const f32x16& wt = wgt[(kBothSets && n == 2) ? 1 : 0];
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) acc[r] *= wt[r];
+                }
+                sm.pfrag[n][0][l] = pack_half<E>(acc, 0);
+                sm.pfrag[n][1][l] = pack_half<E>(acc, 1);
+            }
+
+            // O^T = S^T X^T, rows of O scaled by Lam
+            float lam[2] = {lam_full[0], lam_full[1]};
+            if (kDecay && shift) {
+                lam[0] = sm.pw[max(ln + later - shift, 0)];
+                lam[1] = sm.pw[max(32 + ln + later - shift, 0)];
+            }
+#pragma unroll
+            for (int it = 0; it < 2; ++it)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[it][r] = 0.0f;
+#pragma unroll
+            for (int s = 0; s < D / 16; ++s) {
+                const u32x4 sa = pack_half<E>(S[s >> 1], s & 1);
+#pragma unroll
+                for (int it = 0; it < 2; ++it) o[it] = E::mfma32(sa, frag16(x_row + 32 * it * RS + 16 * s), o[it]);
+            }
+            if (kDecay) {
+#pragma unroll
+                for (int it = 0; it < 2; ++it)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) o[it][r] *= lam[it];
+            }
+        }
+
+        // z fragments: zf[f], f = 2*jt + hh, holds tokens 16f + {4g..4g+3, 8+4g..8+4g+3} of column c_own
+        u32x4 zf[4];
+#pragma unroll
+        for (int f = 0; f < 4; ++f) zf[f] = join(lds_tr(z_tr + (16 * f) * RSZ), lds_tr(z_tr + (16 * f + 8) * RSZ));
+
+        if (kOut) {
+            __syncthreads();  // score fragments visible; the z tile is dead: its fragments are in registers
+            // O^T += Z^T P^T over the tiles (jt <= it)
+#pragma unroll
+            for (int n = 0; n < 3; ++n)
+#pragma unroll
+                for (int hh = 0; hh < 2; ++hh)
+                    o[tile_it(n)] = E::mfma32(zf[2 * tile_jt(n) + hh], sm.pfrag[n][hh][l], o[tile_it(n)]);
+
+            // O^T: lane = token 32it + ln, registers 4q..4q+3 = columns 32w + 8q + 4g + (0..3).  Through a wave-private LDS
+            // tile so that a store covers whole 64-byte row pieces: lane -> (row l/4, 16 bytes l%4).
+            uint32_t* scr = reinterpret_cast<uint32_t*>(sm.z) + w * (32 * 20);
+#pragma unroll
+            for (int it = 0; it < 2; ++it) {
+#pragma unroll
+                for (int qd = 0; qd < 4; ++qd) {
+                    const u32x2 val = {E::pack2(o[it][4 * qd], o[it][4 * qd + 1]), E::pack2(o[it][4 * qd + 2], o[it][4 * qd + 3])};
+                    *reinterpret_cast<u32x2*>(scr + ln * 20 + 4 * qd + 2 * g) = val;
+                }
+                u32x4 val[2];
+#pragma unroll
+                for (int m = 0; m < 2; ++m) val[m] = *reinterpret_cast<const u32x4*>(scr + (16 * m + (l >> 2)) * 20 + 4 * (l & 3));
+#pragma unroll
+                for (int m = 0; m < 2; ++m) {
+                    const int i = 32 * it + 16 * m + (l >> 2);
+                    if (i >= shift)
+                        __builtin_nontemporal_store(val[m], reinterpret_cast<u32x4*>(ob + (tok0 - shift + i) * row_z + 32 * w + 8 * (l & 3)));
+                }
+            }
+        }
+
+        // S = gamma^L S + Y^T (Gam Z)
+        if (kDecay) {
+            const float gl = sm.pw[Lc];
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) S[dt][r] *= gl;
+        }
+#pragma unroll
+        for (int f = 0; f < 4; ++f) {
+            u32x4 zs[kTerms];
+            if (kDecay)
+                scaled<E, kTerms>(zf[f], *reinterpret_cast<const f32x4*>(&sm.gw[16 * f + 4 * g]),
+                                  *reinterpret_cast<const f32x4*>(&sm.gw[16 * f + 8 + 4 * g]), zs);
+            else zs[0] = zf[f];
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) {
+                const u32x4 a = join(lds_tr(y_tr + (16 * f) * RS + 32 * dt), lds_tr(y_tr + (16 * f + 8) * RS + 32 * dt));
+#pragma unroll
+                for (int u = 0; u < (kDecay ? kTerms : 1); ++u) S[dt] = E::mfma32(a, zs[u], S[dt]);
+            }
+        }
+    }
+
+    // hand the state on
+    float* dst = nullptr;
+    if (!kOut) dst = role.slots + ((size_t)bh * (p.nseg - 1) + seg) * D * DV;
+    else if (seg == p.nseg - 1 && role.leave) dst = role.leave + (size_t)bh * D * DV;
+    if (dst) {
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) dst[dk_of(t, r) * DV + c_own] = S[t][r];
+    }
+}
+
+template <int D, int DV, bool kOut, typename E, bool kDecay>
+static void launch_terms(const BwdParams& p, bool fine, hipStream_t stream) {
+    const int units = p.BH * (kOut ? p.nseg : p.nseg - 1);
+    const dim3 grid((units + 7) / 8 * 8 * p.roles), block(DV * 2);
+    if (kDecay && fine) hipLaunchKernelGGL((walk16_kernel<D, DV, kOut, E, kDecay, 3>), grid, block, 0, stream, p);
+    else hipLaunchKernelGGL((walk16_kernel<D, DV, kOut, E, kDecay, 1>), grid, block, 0, stream, p);
+}
+
+template <int D, int DV, bool kOut>
+static void launch_elem(const BwdParams& p, bool f16, bool fine, hipStream_t stream) {
+    if (f16 && p.gamma) launch_terms<D, DV, kOut, ElemF16, true>(p, fine, stream);
+    else if (f16) launch_terms<D, DV, kOut, ElemF16, false>(p, fine, stream);
+    else if (p.gamma) launch_terms<D, DV, kOut, ElemBf16, true>(p, fine, stream);
+    else launch_terms<D, DV, kOut, ElemBf16, false>(p, fine, stream);
+}
+
+// (D, DV) is one of (64, 64), (128, 128), (256, 128), (128, 256); the host has checked it
+template <bool kOut>
+static hipError_t launch_width(const BwdParams& p, int D, int DV, bool f16, bool fine, hipStream_t stream) {
+    if (D == 64) launch_elem<64, 64, kOut>(p, f16, fine, stream);
+    else if (D == 256) launch_elem<256, 128, kOut>(p, f16, fine, stream);
+    else if (DV == 128) launch_elem<128, 128, kOut>(p, f16, fine, stream);
+    else if (kOut) launch_elem<128, 256, true>(p, f16, fine, stream);
+    return hipGetLastError();
+}
+
+}  // namespace bwd
+
+hipError_t launch_bwd_16bit_states(const BwdParams& p, int D, int DV, bool f16, bool fine, hipStream_t stream) {
+    return bwd::launch_width<false>(p, D, DV, f16, fine, stream);
+}
+
+hipError_t launch_bwd_16bit_walk(const BwdParams& p, int D, int DV, bool f16, bool fine, hipStream_t stream) {
+    return bwd::launch_width<true>(p, D, DV, f16, fine, stream);
+}
+
+}  // namespace leet
