@@ -545,6 +545,75 @@ size_t leet_attn_gated_scan_workspace_bytes(int B, int N, int C, int backward);
 int leet_attn_gated_scan_step(const leet_attn_rows *x, const leet_attn_rows *gate, const leet_attn_rows *out,
                               float *state, int B, int C, int dtype, int gate_dtype, int mode, void *stream);
 
+/*
+ * Root-mean-square norm of rows, the residual stream's addition in the same pass:
+ *     s = x + residual,     out = w .* s / sqrt(mean(s^2) + eps),     residual_out = s.
+ *   x, out        [B][N][C] of `dtype`
+ *   residual, residual_out  [B][N][C] of residual_dtype (`dtype` or LEET_F32); residual NULL: s = x, and residual_out must be
+ *                 NULL; residual_out NULL: not wanted
+ *   weight        [C] of weight_dtype (`dtype` or LEET_F32), or NULL: ones
+ *   eps           >= 0, finite.  A row of zeros with eps = 0 gives NaN, as the formula does
+ * The norm is that of the sum before it is rounded to residual_dtype.  fp32 inside, rounded once, at the store; a row whose
+ * squares would leave fp32's range is multiplied by a power of two for its norm.  out may be x or residual, residual_out
+ * residual or x (same data, strides and type).  C <= 16384 (LEET_ERR_TOO_LARGE).
+ */
+int leet_attn_add_rms_norm(const leet_attn_rows *x, const leet_attn_rows *residual, const leet_attn_rows *out,
+                           const leet_attn_rows *residual_out, const void *weight, int weight_dtype, float eps,
+                           int B, int N, int C, int dtype, int residual_dtype, void *stream);
+
+/*
+ * The same with an output in 8 bits (e4m3: four bits of exponent, three of mantissa, largest value 448) and scales:
+ *     scale = max(largest |y|, 2^-100) / 448,     out = e4m3(y / scale),     y = out scale.
+ *   out      [B][N][C] bytes (strides in bytes)
+ *   scales   [B][N][C / group] float, dense; one for `group` neighbouring channels: 32, 64 or 128, which must divide C, or 0:
+ *            one a row, scales [B][N]
+ * Where y is not a finite number the row's or group's scale or values are not either.
+ */
+int leet_attn_add_rms_norm_q8(const leet_attn_rows *x, const leet_attn_rows *residual, const leet_attn_rows *out,
+                              float *scales, int group, const leet_attn_rows *residual_out, const void *weight,
+                              int weight_dtype, float eps, int B, int N, int C, int dtype, int residual_dtype, void *stream);
+
+/*
+ * Backward pass of leet_attn_add_rms_norm.  With r = 1/sqrt(mean(h^2) + eps) and n = h r:
+ *     g = r (w .* dout - n mean(w .* dout .* n)) + dresidual,     dweight = sum of dout .* n over the rows;
+ * g is the gradient of the sum, so of x and of the residual both.
+ *   dout       [B][N][C] of `dtype`: the gradient of out
+ *   h          [B][N][C] of residual_dtype: the forward call's residual_out (x where there was no residual)
+ *   dresidual  [B][N][C] of residual_dtype: the gradient of residual_out, or NULL: zero
+ *   dx, dh     g in `dtype`, g in residual_dtype; either may be NULL.  Each may be dout, h or dresidual (same data, strides and type)
+ *   dweight    [C] of weight_dtype, or NULL: not wanted.  Written when all inputs have been read, so it may be the weight
+ *   workspace  leet_attn_add_rms_norm_workspace_bytes bytes, 256-byte aligned; may be NULL without dweight.  Scratch
+ * The sums over rows are taken in fp32 in a fixed order: no atomics, equal from call to call.
+ */
+int leet_attn_add_rms_norm_backward(const leet_attn_rows *dout, const leet_attn_rows *h, const leet_attn_rows *dresidual,
+                                    const leet_attn_rows *dx, const leet_attn_rows *dh, const void *weight, void *dweight,
+                                    int weight_dtype, float eps, void *workspace, size_t workspace_bytes,
+                                    int B, int N, int C, int dtype, int residual_dtype, void *stream);
+size_t leet_attn_add_rms_norm_workspace_bytes(int B, int N, int C);
+
+/* One of a model's gradients: `count` adjacent values of `dtype`, DEVICE memory, and where the clipped ones go (may be data). */
+typedef struct {
+    const void *data;
+    void *out;
+    long long count;
+    int dtype;
+} leet_attn_gradient;
+
+/*
+ * The norm over all gradients of a model, and the gradients clipped to it:
+ *     norm = sqrt(sum of all squares),     out = data min(1, limit / norm).
+ *   grads      HOST memory, read before the call returns; `count` of them, of any types and sizes (0 values are legal)
+ *   limit      >= 0; INFINITY: the norm alone, `out` is ignored
+ *   norm       one float, DEVICE memory, or NULL: not wanted
+ *   workspace  leet_attn_clip_gradients_workspace_bytes bytes, 256-byte aligned; scratch
+ * Squares are added in fp64 in a fixed order, so the norm neither overflows (but as a float) nor changes from call to call.  A
+ * norm that is not finite clips nothing: `out` then holds the gradients as they are.  Where nothing is clipped gradients in
+ * place are not written.
+ */
+int leet_attn_clip_gradients(const leet_attn_gradient *grads, int count, float limit, float *norm, void *workspace,
+                             size_t workspace_bytes, void *stream);
+size_t leet_attn_clip_gradients_workspace_bytes(void);
+
 /* Static, never-NULL description of a leet_status value. */
 const char *leet_attn_strerror(int status);
 

@@ -65,6 +65,12 @@ EXPORTED_SYMBOLS = (
     "leet_attn_gated_scan_backward",
     "leet_attn_gated_scan_workspace_bytes",
     "leet_attn_gated_scan_step",
+    "leet_attn_add_rms_norm",
+    "leet_attn_add_rms_norm_q8",
+    "leet_attn_add_rms_norm_backward",
+    "leet_attn_add_rms_norm_workspace_bytes",
+    "leet_attn_clip_gradients",
+    "leet_attn_clip_gradients_workspace_bytes",
     "leet_attn_backward",
     "leet_attn_backward_workspace_bytes",
     "leet_attn_strerror",
@@ -82,6 +88,7 @@ class LeetAttnError(RuntimeError):
 # A call passes the bytes where the library takes a pointer to the structure.
 _pack_heads = struct.Struct("@P3q").pack      # leet_attn_heads: data, batch, head, token
 _pack_rows = struct.Struct("@P2q").pack       # leet_attn_rows: data, batch, token
+_gradient = struct.Struct("@PPqi4x")          # leet_attn_gradient: data, out, count, dtype
 _pack_rotation = struct.Struct("@PiiPqqf4x").pack  # leet_attn_rotation
 
 
@@ -172,6 +179,19 @@ def _load() -> ctypes.CDLL:
     lib.leet_attn_gated_scan_workspace_bytes.restype = sz
     lib.leet_attn_gated_scan_step.argtypes = [rows, rows, rows, vp, i, i, i, i, i, vp]
     lib.leet_attn_gated_scan_step.restype = i
+    lib.leet_attn_add_rms_norm.argtypes = [rows, rows, rows, rows, vp, i, ctypes.c_float, i, i, i, i, i, vp]
+    lib.leet_attn_add_rms_norm.restype = i
+    lib.leet_attn_add_rms_norm_q8.argtypes = [rows, rows, rows, vp, i, rows, vp, i, ctypes.c_float, i, i, i, i, i, vp]
+    lib.leet_attn_add_rms_norm_q8.restype = i
+    lib.leet_attn_add_rms_norm_backward.argtypes = [rows, rows, rows, rows, rows, vp, vp, i, ctypes.c_float, vp, sz,
+                                                    i, i, i, i, i, vp]
+    lib.leet_attn_add_rms_norm_backward.restype = i
+    lib.leet_attn_add_rms_norm_workspace_bytes.argtypes = [i, i, i]
+    lib.leet_attn_add_rms_norm_workspace_bytes.restype = sz
+    lib.leet_attn_clip_gradients.argtypes = [vp, i, ctypes.c_float, vp, vp, sz, vp]
+    lib.leet_attn_clip_gradients.restype = i
+    lib.leet_attn_clip_gradients_workspace_bytes.argtypes = []
+    lib.leet_attn_clip_gradients_workspace_bytes.restype = sz
     lib.leet_attn_backward.argtypes = [vp] * 12 + [sz, i, i, i, i, i, i, i, i, vp]
     lib.leet_attn_backward.restype = i
     lib.leet_attn_backward_workspace_bytes.argtypes = [i, i, i, i, i, i, i]
@@ -1091,3 +1111,175 @@ def leet_attn_gated_scan_step(x: torch.Tensor, gate: torch.Tensor, state: torch.
     if st != LEET_OK:
         raise LeetAttnError(st, "leet_attn_gated_scan_step")
     return out
+
+
+def _norm_rows(x: torch.Tensor, where: str):
+    """B, N, C of rows [B, N, C] or [B, C]."""
+    if x.dim() not in (2, 3):
+        raise ValueError("rows must be [B, N, C] or [B, C]")
+    B, N, C = x.shape if x.dim() == 3 else (x.shape[0], 1, x.shape[1])
+    _sizes(where, B, N, C)
+    return B, N, C
+
+
+def _stream_code(t: torch.Tensor, like: torch.dtype, name: str) -> int:
+    if t.dtype != like and t.dtype != torch.float32:
+        raise TypeError(f"{name} must have the type of the rows or be float32")
+    return _dtype_code(t)
+
+
+def _norm_weight(weight: Optional[torch.Tensor], dtype: torch.dtype, C: int) -> int:
+    """dtype code of the weight."""
+    if weight is None:
+        return LEET_F32
+    if tuple(weight.shape) != (C,) or not weight.is_contiguous():
+        raise ValueError("weight must be contiguous [C]")
+    return _stream_code(weight, dtype, "weight")
+
+
+def _norm_sum(x, residual, residual_out):
+    """(residual_out, dtype code of the stream) of a forward call."""
+    if residual is None:
+        if residual_out is not None:
+            raise ValueError("residual_out without residual")
+        return None, _dtype_code(x)
+    code = _stream_code(residual, x.dtype, "residual")
+    return (_new_dense(residual) if residual_out is None else residual_out), code
+
+
+def leet_attn_add_rms_norm(x: torch.Tensor, residual: Optional[torch.Tensor] = None,
+                           weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                           out: Optional[torch.Tensor] = None, residual_out: Optional[torch.Tensor] = None):
+    """Root-mean-square norm of the rows of ``x + residual`` ([B, N, C] or [B, C]), times the weight [C]; returns
+    (out, residual_out), the second the sum itself in the residual's type (None without a residual).
+
+    The residual has the type of x or is float32.  ``out`` may be x or residual, ``residual_out`` residual or x.  Autograd
+    sees nothing of it (``leet_attn_add_rms_norm_backward``)."""
+    B, N, C = _norm_rows(x, "leet_attn_add_rms_norm")
+    weight_code = _norm_weight(weight, x.dtype, C)
+    residual_out, code = _norm_sum(x, residual, residual_out)
+    if out is None:
+        out = _new_dense(x)
+    dev = _on(x, residual, weight, out, residual_out)
+    shape, t = x.shape, x.dtype
+    vr = vs = None
+    if residual is not None:
+        vr = _rows_view(residual, "residual", shape, residual.dtype)
+        vs = _rows_view(residual_out, "residual_out", shape, residual.dtype)
+    st = _call_on(dev, lib.leet_attn_add_rms_norm, _rows_view(x, "x", shape, t), vr, _rows_view(out, "out", shape, t), vs,
+                  _ptr(weight), weight_code, eps, B, N, C, _dtype_code(x), code)
+    if st != LEET_OK:
+        raise LeetAttnError(st, "leet_attn_add_rms_norm")
+    return out, residual_out
+
+
+def leet_attn_add_rms_norm_q8(x: torch.Tensor, residual: Optional[torch.Tensor] = None,
+                              weight: Optional[torch.Tensor] = None, eps: float = 1e-6, group: int = 0,
+                              out: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None,
+                              residual_out: Optional[torch.Tensor] = None):
+    """``leet_attn_add_rms_norm`` with the normed rows in 8 bits: returns (out, scales, residual_out), out in
+    torch.float8_e4m3fn and scales in float32, one for ``group`` (32, 64 or 128) neighbouring channels, [B, N, C / group],
+    or, with group 0, one a row, [B, N, 1]: the rows are ``out.float() * scales`` group by group."""
+    B, N, C = _norm_rows(x, "leet_attn_add_rms_norm_q8")
+    weight_code = _norm_weight(weight, x.dtype, C)
+    residual_out, code = _norm_sum(x, residual, residual_out)
+    if group < 0 or (group and C % group):
+        raise ValueError("group must divide C")
+    shape, t = x.shape, x.dtype
+    if out is None:
+        out = torch.empty(shape, dtype=torch.float8_e4m3fn, device=x.device)
+    scale_shape = shape[:-1] + (C // group if group else 1,)
+    if scales is None:
+        scales = torch.empty(scale_shape, dtype=torch.float32, device=x.device)
+    elif scales.shape != scale_shape or scales.dtype != torch.float32 or not scales.is_contiguous():
+        raise ValueError(f"scales must be contiguous float32 {list(scale_shape)}")
+    dev = _on(x, residual, weight, out, scales, residual_out)
+    vr = vs = None
+    if residual is not None:
+        vr = _rows_view(residual, "residual", shape, residual.dtype)
+        vs = _rows_view(residual_out, "residual_out", shape, residual.dtype)
+    st = _call_on(dev, lib.leet_attn_add_rms_norm_q8, _rows_view(x, "x", shape, t), vr,
+                  _rows_view(out, "out", shape, torch.float8_e4m3fn), _ptr(scales), int(group), vs, _ptr(weight),
+                  weight_code, eps, B, N, C, _dtype_code(x), code)
+    if st != LEET_OK:
+        raise LeetAttnError(st, "leet_attn_add_rms_norm_q8")
+    return out, scales, residual_out
+
+
+def add_rms_norm_workspace_bytes(B: int, N: int, C: int) -> int:
+    return int(lib.leet_attn_add_rms_norm_workspace_bytes(B, N, C))
+
+
+def leet_attn_add_rms_norm_backward(dout: torch.Tensor, h: torch.Tensor, weight: Optional[torch.Tensor] = None,
+                                    eps: float = 1e-6, dresidual: Optional[torch.Tensor] = None,
+                                    dx: Optional[torch.Tensor] = None, dh: Optional[torch.Tensor] = None,
+                                    dweight: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """Gradients of ``leet_attn_add_rms_norm``: (dx, dh, dweight) from that of its output and from ``h``, its residual_out
+    (x where there was no residual); ``dresidual`` is the gradient of residual_out, in h's type (None: zero).
+
+    dx and dh are the gradient of the sum, so of x and of the residual both, in dout's type and in h's; where these are one
+    type dh is dx.  dweight is None without a weight."""
+    B, N, C = _norm_rows(dout, "leet_attn_add_rms_norm_backward")
+    weight_code = _norm_weight(weight, dout.dtype, C)
+    code = _stream_code(h, dout.dtype, "h")
+    if weight is None:
+        if dweight is not None:
+            raise ValueError("dweight without a weight")
+    elif dweight is None:
+        dweight = _new_dense(weight)
+    elif dweight.dtype != weight.dtype or dweight.shape != weight.shape or not dweight.is_contiguous():
+        raise ValueError("dweight must be contiguous [C] of the weight's type")
+    if dx is None:
+        dx = _new_dense(dout)
+    one = h.dtype == dout.dtype
+    if one and dh is not None and dh is not dx:
+        raise ValueError("where h has dout's type dh is dx")
+    if not one and dh is None:
+        dh = _new_dense(h)
+    dev = _on(dout, h, weight, dresidual, dx, dh, dweight, workspace)
+    need = add_rms_norm_workspace_bytes(B, N, C) if workspace is None and dweight is not None else 0
+    ws, ws_bytes, keep = _scratch(need, workspace, dev)
+    shape, t, s = dout.shape, dout.dtype, h.dtype
+    st = _call_on(dev, lib.leet_attn_add_rms_norm_backward, _rows_view(dout, "dout", shape, t), _rows_view(h, "h", shape, s),
+                  None if dresidual is None else _rows_view(dresidual, "dresidual", shape, s),
+                  _rows_view(dx, "dx", shape, t), None if one else _rows_view(dh, "dh", shape, s), _ptr(weight),
+                  _ptr(dweight), weight_code, eps, ws, ws_bytes, B, N, C, _dtype_code(dout), code)
+    if st != LEET_OK:
+        raise LeetAttnError(st, "leet_attn_add_rms_norm_backward")
+    return dx, dx if one else dh, dweight
+
+
+def clip_gradients_workspace_bytes() -> int:
+    return int(lib.leet_attn_clip_gradients_workspace_bytes())
+
+
+def leet_attn_clip_gradients(grads, limit: Optional[float] = None, outs=None, norm: Optional[torch.Tensor] = None,
+                             workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Norm over all tensors of ``grads`` together, and the tensors times min(1, limit / norm): in place, or into ``outs``
+    (tensors of the same sizes and types).  Returns the norm, float32 [1] on their device; without a ``limit`` that is all.
+
+    All tensors must be dense (any order of dimensions, an output the same one).  A norm that is not finite clips nothing."""
+    grads = list(grads)
+    if not grads:
+        raise ValueError("no gradients")
+    targets = grads if outs is None else list(outs)
+    if len(targets) != len(grads):
+        raise ValueError("outs must be as many as grads")
+    dev = _on(*grads, *targets, norm, workspace)
+    packed = bytearray(_gradient.size * len(grads))
+    for n, (g, o) in enumerate(zip(grads, targets)):
+        if o is not g and (o.dtype != g.dtype or o.shape != g.shape or o.stride() != g.stride()):
+            raise ValueError("outs must have the shapes, strides and types of grads")
+        if not g.is_contiguous() and not torch.ops.aten.is_non_overlapping_and_dense(g):
+            raise ValueError("gradients must be dense")
+        _gradient.pack_into(packed, n * _gradient.size, g.data_ptr(), o.data_ptr(), g.numel(), _dtype_code(g))
+    if norm is None:
+        norm = torch.empty(1, dtype=torch.float32, device=torch.device("cuda", dev))
+    elif norm.dtype != torch.float32 or norm.numel() != 1:
+        raise ValueError("norm must be one float32")
+    ws, ws_bytes, keep = _scratch(clip_gradients_workspace_bytes() if workspace is None else 0, workspace, dev)
+    st = _call_on(dev, lib.leet_attn_clip_gradients, bytes(packed), len(grads), float("inf") if limit is None else limit,
+                  _ptr(norm), ws, ws_bytes)
+    if st != LEET_OK:
+        raise LeetAttnError(st, "leet_attn_clip_gradients")
+    return norm

@@ -18,6 +18,7 @@
 //   a lane and round (rot 34 of d 128: 73, 90 and 143 us where rot 128 takes 49, 51 and 78).
 #include "leet_heads.hpp"
 #include "leet_io.hpp"
+#include "leet_reduce.hpp"
 
 namespace leet {
 
@@ -27,22 +28,6 @@ constexpr int kPiece = 4, kPieceLog = 3;  // a row of 64 elements has 2^kPieceLo
 constexpr int kHeadsWaves = 4;  // waves of a workgroup
 constexpr int kBackwardResident = 5;  // workgroups of the backward kernel on a compute unit
 constexpr int kComputeUnits = 256;
-
-// Sum over the 2^kLog neighbouring lanes that hold a row; every one of them gets it, with the same bits.
-template <int kCtrl>
-__device__ __forceinline__ float dpp(float x) {
-    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), kCtrl, 0xf, 0xf, true));
-}
-template <int kLog>
-__device__ __forceinline__ float row_sum(float v) {
-    if constexpr (kLog >= 1) v += dpp<0xB1>(v);   // quad_perm 1 0 3 2
-    if constexpr (kLog >= 2) v += dpp<0x4E>(v);   // quad_perm 2 3 0 1
-    if constexpr (kLog >= 3) v += dpp<0x141>(v);  // row_half_mirror: the quads of eight lanes swap
-    if constexpr (kLog >= 4) v += dpp<0x140>(v);  // row_mirror: the halves of sixteen lanes swap
-    if constexpr (kLog >= 5) v += __shfl_xor(v, 16, 64);
-    if constexpr (kLog >= 6) v += __shfl_xor(v, 32, 64);
-    return v;
-}
 
 // What a lane holds of a row: kK chunks of two pieces of kV elements, chunk k = elements first(k) .. + kV-1 and second(k)
 // .. + kV-1.  The lanes' first pieces lie beside one another, and so do their second ones: an access of a wave is whole

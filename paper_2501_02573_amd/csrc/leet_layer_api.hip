@@ -1,10 +1,15 @@
 // C ABI of the operators beside the attention: argument checks and launches.  Nothing here touches tensor data.
 #include <math.h>
 
+#include <algorithm>
+#include <new>
+
 #include "../../include/leet_attn.h"
+#include "leet_clip.hpp"
 #include "leet_gated_scan.hpp"
 #include "leet_heads.hpp"
 #include "leet_host.hpp"
+#include "leet_norm.hpp"
 #include "leet_overlap.hpp"
 
 namespace {
@@ -190,6 +195,91 @@ int scan_sizes_ok(const int* offsets, int sequences, const void* workspace, size
     if (need && (!workspace || workspace_bytes < need || !aligned(workspace, 256))) return LEET_ERR_INVALID_ARG;
     *S = offsets ? sequences : B;
     return LEET_OK;
+}
+
+// ---- norms of a residual stream ----
+
+// Sizes, types and the weight of the three calls.  LEET_OK with p->rows = 0: no rows.
+int norm_sizes(int B, int N, int C, int dtype, int stream_dtype, int weight_dtype, const void* weight, float eps,
+               leet::NormParams* p) {
+    if (B <= 0 || N < 0 || C <= 0 || !isfinite(eps) || eps < 0.0f) return LEET_ERR_INVALID_ARG;
+    if (!dtype_ok(dtype) || (stream_dtype != dtype && stream_dtype != LEET_F32) ||
+        (weight_dtype != dtype && weight_dtype != LEET_F32))
+        return LEET_ERR_UNSUPPORTED;
+    if (!aligned(weight, size_of(weight_dtype))) return LEET_ERR_INVALID_ARG;
+    if (C > leet::kNormChannels || (long long)B * N >= 1LL << 31) return LEET_ERR_TOO_LARGE;
+    // a workgroup of up to 1024 threads a row
+    if ((long long)B * N * (C <= 512 ? 64 : C <= 1024 ? 128 : C <= 2048 ? 256 : C <= 4096 ? 512 : 1024) >= kMaxThreads)
+        return LEET_ERR_TOO_LARGE;
+    *p = leet::NormParams{};
+    p->weight = weight;
+    p->weight_f32 = weight_dtype == LEET_F32;
+    p->eps = eps;
+    p->C = C;
+    p->N = N;
+    p->rows = B * N;
+    return LEET_OK;
+}
+
+leet::RowsIn rows_in_or_none(const leet_attn_rows* t) { return t ? rows_in(t) : leet::RowsIn{nullptr, 0, 0}; }
+leet::RowsOut rows_out_or_none(const leet_attn_rows* t) { return t ? rows_out(t) : leet::RowsOut{nullptr, 0, 0}; }
+
+// out_size: bytes of an output element (1: 8 bits with scales)
+int norm_forward(const leet_attn_rows* x, const leet_attn_rows* residual, const leet_attn_rows* out, int out_size,
+                 float* scales, int group, const leet_attn_rows* residual_out, const void* weight, int weight_dtype, float eps,
+                 int B, int N, int C, int dtype, int residual_dtype, void* stream) {
+    leet::NormParams p;
+    const int status = norm_sizes(B, N, C, dtype, residual_dtype, weight_dtype, weight, eps, &p);
+    if (status != LEET_OK) return status;
+    const bool q8 = out_size == 1;
+    if (q8 && group != 0 && group != 32 && group != 64 && group != 128) return LEET_ERR_UNSUPPORTED;
+    if (q8 && ((group && C % group != 0) || !aligned(scales, 4))) return LEET_ERR_INVALID_ARG;
+    if (!residual && residual_out) return LEET_ERR_INVALID_ARG;
+    if (p.rows == 0) return LEET_OK;
+    const size_t size = size_of(dtype), residual_size = size_of(residual_dtype);
+    if (!rows_ok(x, B, N, C, size, false) || !rows_ok(out, B, N, C, q8 ? 1 : size, true) || (q8 && !scales) ||
+        (residual && !rows_ok(residual, B, N, C, residual_size, false)) ||
+        (residual_out && !rows_ok(residual_out, B, N, C, residual_size, true)))
+        return LEET_ERR_INVALID_ARG;
+    const Span from = span_of(x, B, N, C, size), with = span_of(residual, B, N, C, residual_size);
+    const Span to = span_of(out, B, N, C, out_size), sum = span_of(residual_out, B, N, C, residual_size);
+    const Span weights(weight, size_of(weight_dtype), C);
+    const Span scale(q8 ? scales : nullptr, 4, (long long)p.rows * (group ? C / group : 1));
+    // what is written may be what it is made from, element for element; everything else lies apart
+    if (!in_place_or_apart(to, from) || !in_place_or_apart(to, with) || !in_place_or_apart(sum, from) ||
+        !in_place_or_apart(sum, with) || shares_any(to, {&sum, &weights, &scale}) || shares_any(sum, {&weights, &scale}) ||
+        shares_any(scale, {&from, &with, &weights}))
+        return LEET_ERR_INVALID_ARG;
+    int dev = 0;
+    const int found = leet::current_device(&dev);
+    if (found != LEET_OK) return found;
+    p.x = rows_in(x);
+    p.stream = rows_in_or_none(residual);
+    p.out = rows_out(out);
+    p.sum = rows_out_or_none(residual_out);
+    p.scales = scales;
+    p.group = group;
+    p.far = (size_t)p.rows * C * (size + out_size + (residual ? residual_size : 0) + (residual_out ? residual_size : 0)) > kStreamBytes;
+    return done(leet::launch_norm(p, elem_of(dtype), elem_of(residual_dtype), q8, static_cast<hipStream_t>(stream)));
+}
+
+// ---- clipping ----
+
+struct Extent {
+    uintptr_t first, last;
+    bool written;
+};
+
+// Whether something that is written shares memory with anything else.
+bool extents_clash(Extent* e, size_t n) {
+    std::sort(e, e + n, [](const Extent& a, const Extent& b) { return a.first < b.first; });
+    uintptr_t any = 0, written = 0;  // where those before end
+    for (size_t i = 0; i < n; ++i) {
+        if (e[i].first < written || (e[i].written && e[i].first < any)) return true;
+        any = std::max(any, e[i].last);
+        if (e[i].written) written = std::max(written, e[i].last);
+    }
+    return false;
 }
 
 }  // namespace
@@ -431,6 +521,160 @@ int leet_attn_gated_scan_step(const leet_attn_rows *x, const leet_attn_rows *gat
     status = leet::current_device(&dev);
     if (status != LEET_OK) return status;
     return done(leet::launch_gated_step(p, elem_of(dtype), elem_of(gate_dtype), mode, static_cast<hipStream_t>(stream)));
+}
+
+int leet_attn_add_rms_norm(const leet_attn_rows *x, const leet_attn_rows *residual, const leet_attn_rows *out,
+                           const leet_attn_rows *residual_out, const void *weight, int weight_dtype, float eps,
+                           int B, int N, int C, int dtype, int residual_dtype, void *stream) {
+    const int out_size = dtype_ok(dtype) ? (int)size_of(dtype) : 2;
+    return norm_forward(x, residual, out, out_size, nullptr, 0, residual_out, weight, weight_dtype, eps, B, N, C, dtype,
+                        residual_dtype, stream);
+}
+
+int leet_attn_add_rms_norm_q8(const leet_attn_rows *x, const leet_attn_rows *residual, const leet_attn_rows *out,
+                              float *scales, int group, const leet_attn_rows *residual_out, const void *weight,
+                              int weight_dtype, float eps, int B, int N, int C, int dtype, int residual_dtype, void *stream) {
+    return norm_forward(x, residual, out, 1, scales, group, residual_out, weight, weight_dtype, eps, B, N, C, dtype,
+                        residual_dtype, stream);
+}
+
+size_t leet_attn_add_rms_norm_workspace_bytes(int B, int N, int C) {
+    if (B <= 0 || N <= 0 || C <= 0 || C > leet::kNormChannels || (long long)B * N >= 1LL << 31) return 0;
+    return (size_t)leet::norm_groups(B * N, C) * C * sizeof(float);
+}
+
+int leet_attn_add_rms_norm_backward(const leet_attn_rows *dout, const leet_attn_rows *h, const leet_attn_rows *dresidual,
+                                    const leet_attn_rows *dx, const leet_attn_rows *dh, const void *weight, void *dweight,
+                                    int weight_dtype, float eps, void *workspace, size_t workspace_bytes,
+                                    int B, int N, int C, int dtype, int residual_dtype, void *stream) {
+    leet::NormParams p;
+    const int status = norm_sizes(B, N, C, dtype, residual_dtype, weight_dtype, weight, eps, &p);
+    if (status != LEET_OK) return status;
+    const size_t size = size_of(dtype), residual_size = size_of(residual_dtype), weight_size = size_of(weight_dtype);
+    if (!aligned(dweight, weight_size)) return LEET_ERR_INVALID_ARG;
+    p.groups = p.rows ? leet::norm_groups(p.rows, C) : 0;
+    p.weight_grad = dweight;
+    const size_t need = dweight ? (size_t)p.groups * C * sizeof(float) : 0;
+    if (p.rows) {
+        if (!rows_ok(dout, B, N, C, size, false) || !rows_ok(h, B, N, C, residual_size, false) || (!dx && !dh) ||
+            (dresidual && !rows_ok(dresidual, B, N, C, residual_size, false)) ||
+            (dx && !rows_ok(dx, B, N, C, size, true)) || (dh && !rows_ok(dh, B, N, C, residual_size, true)))
+            return LEET_ERR_INVALID_ARG;
+        if (need && (!workspace || !aligned(workspace, 256) || workspace_bytes < need)) return LEET_ERR_INVALID_ARG;
+        const Span dy = span_of(dout, B, N, C, size), sum = span_of(h, B, N, C, residual_size);
+        const Span along = span_of(dresidual, B, N, C, residual_size);
+        const Span to = span_of(dx, B, N, C, size), to_sum = span_of(dh, B, N, C, residual_size);
+        const Span weights(weight, weight_size, C), dweights(dweight, weight_size, C);
+        const Span scratch(need ? workspace : nullptr, 1, (long long)need);
+        for (const Span* out : {&to, &to_sum})
+            if (!in_place_or_apart(*out, dy) || !in_place_or_apart(*out, sum) || !in_place_or_apart(*out, along) ||
+                shares_any(*out, {&weights, &dweights, &scratch}))
+                return LEET_ERR_INVALID_ARG;
+        if (overlap(to, to_sum) || shares_any(scratch, {&dy, &sum, &along, &weights, &dweights})) return LEET_ERR_INVALID_ARG;
+    }
+    if (p.rows == 0 && !dweight) return LEET_OK;
+    int dev = 0;
+    const int found = leet::current_device(&dev);
+    if (found != LEET_OK) return found;
+    hipError_t e = hipSuccess;
+    if (p.rows) {
+        p.x = rows_in(dout);
+        p.stream = rows_in(h);
+        p.grad = rows_in_or_none(dresidual);
+        p.out = rows_out_or_none(dx);
+        p.sum = rows_out_or_none(dh);
+        p.partial = need ? static_cast<float*>(workspace) : nullptr;
+        p.far = (size_t)p.rows * C * (size + residual_size * (dresidual ? 2 : 1) + (dx ? size : 0) + (dh ? residual_size : 0)) > kStreamBytes;
+        e = leet::launch_norm_backward(p, elem_of(dtype), elem_of(residual_dtype), static_cast<hipStream_t>(stream));
+    }
+    if (e == hipSuccess && dweight) e = leet::launch_norm_weight(p, elem_of(dtype), static_cast<hipStream_t>(stream));
+    return done(e);
+}
+
+size_t leet_attn_clip_gradients_workspace_bytes(void) { return leet::kClipParts * sizeof(double); }
+
+int leet_attn_clip_gradients(const leet_attn_gradient *grads, int count, float limit, float *norm, void *workspace,
+                             size_t workspace_bytes, void *stream) {
+    if (count < 0 || (count && !grads) || !(limit >= 0.0f) || !aligned(norm, 4)) return LEET_ERR_INVALID_ARG;
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < leet_attn_clip_gradients_workspace_bytes())
+        return LEET_ERR_INVALID_ARG;
+    if (count > 1 << 20) return LEET_ERR_TOO_LARGE;
+    const bool clips = isfinite(limit);
+    for (int i = 0; i < count; ++i) {
+        const leet_attn_gradient& g = grads[i];
+        if (!dtype_ok(g.dtype)) return LEET_ERR_UNSUPPORTED;
+        if (g.count < 0 || (g.count && (!g.data || (clips && !g.out))) || !aligned(g.data, size_of(g.dtype)) ||
+            !aligned(g.out, size_of(g.dtype)))
+            return LEET_ERR_INVALID_ARG;
+        if (g.count > 1LL << 40) return LEET_ERR_TOO_LARGE;
+    }
+    // an output is its own gradient or lies apart from everything else
+    Extent few[2 * leet::kClipTensors + 2], *extents = few;
+    if (count > leet::kClipTensors && !(extents = new (std::nothrow) Extent[2 * (size_t)count + 2])) return LEET_ERR_LAUNCH;
+    size_t n = 0;
+    auto add = [&](const void* at, size_t bytes, bool written) {
+        const uintptr_t a = reinterpret_cast<uintptr_t>(at);
+        if (at && bytes) extents[n++] = {a, a + bytes, written};
+    };
+    for (int i = 0; i < count; ++i) {
+        const size_t bytes = (size_t)grads[i].count * size_of(grads[i].dtype);
+        if (!clips || grads[i].out != grads[i].data) add(grads[i].data, bytes, false);
+        if (clips) add(grads[i].out, bytes, true);
+    }
+    add(norm, 4, true);
+    add(workspace, leet_attn_clip_gradients_workspace_bytes(), true);
+    const bool clash = extents_clash(extents, n);
+    if (extents != few) delete[] extents;
+    if (clash) return LEET_ERR_INVALID_ARG;
+    int dev = 0;
+    const int found = leet::current_device(&dev);
+    if (found != LEET_OK) return found;
+
+    leet::ClipParams p = {};
+    p.parts = static_cast<double*>(workspace);
+    p.limit = limit;
+    hipError_t e = hipSuccess;
+    // the tensors in launches of kClipTensors; `over` is called with each launch's parameters
+    auto launches = [&](auto over) {
+        int i = 0;
+        do {
+            p.tensors = 0;
+            long long tiles = 0;
+            for (; i < count && p.tensors < leet::kClipTensors; ++i) {
+                if (grads[i].count == 0) continue;
+                const long long more = (grads[i].count + leet::kClipTile - 1) / leet::kClipTile;
+                if (tiles + more >= 1LL << 30) break;
+                const int t = p.tensors++;
+                p.data[t] = static_cast<const char*>(grads[i].data);
+                p.out[t] = static_cast<char*>(grads[i].out);
+                p.count[t] = grads[i].count;
+                p.elem[t] = (unsigned char)elem_of(grads[i].dtype);
+                p.first[t] = (int)tiles;
+                tiles += more;
+            }
+            p.first[p.tensors] = (int)tiles;
+            e = over();
+        } while (e == hipSuccess && i < count);
+    };
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    launches([&] {
+        const hipError_t launched = leet::launch_clip_squares(p, s);
+        p.add = 1;
+        return launched;
+    });
+    if (e != hipSuccess) return LEET_ERR_LAUNCH;
+    p.norm = norm;
+    if (clips) {
+        launches([&] {
+            const hipError_t launched = leet::launch_clip(p, s);
+            p.norm = nullptr;
+            return launched;
+        });
+    } else if (norm) {
+        p.tensors = p.first[0] = 0;
+        e = leet::launch_clip(p, s);
+    }
+    return done(e);
 }
 
 }  // extern "C"

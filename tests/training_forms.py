@@ -10,6 +10,12 @@ scores and of what the state gives; with all factors taken absolutely (W) its er
   (D + 140 + 20 chunks) u W; also of dstate_in, whose summands are formed to 2^-24 whatever the type.
 
 Where operands of fp16 fall under its normal range a rounding is 2^-25 instead: every operand of a product may be off by that.
+
+Norms of rows, u as above: a row's sum of squares, or of products, of up to 50 additions one after the other (sixteen
+elements of a thread, six steps of a wave, sixteen waves) 50 u, halved by the root; the sum x + residual u; quotient, root and
+products 5 u: 36 u times the value.  Its gradient: the norm's 36 u on each factor r and n (three of them in the second term), 50 u
+of the mean, 8 u of products: 160 u of the terms taken absolutely, u of the sum with what comes along.  The weight's gradient: 36 u
+of n, at most 64 additions one after the other at the sizes that are tested: 110 u of its summands taken absolutely.
 """
 import torch
 
@@ -72,3 +78,29 @@ def attention_backward(dout, q, k, v, gamma, state=None, dstate=None, dtype=torc
         bounds[2] = bounds[2] + small * (row(dout) + each(k) * (1 + row(q).amax(-1, keepdim=True)))
         bounds[3] = bounds[3] + small * row(q).transpose(-1, -2)
     return tuple(zip(got, bounds))
+
+
+def add_norm(x, residual, w, eps):
+    """((y, bound), (s, bound)) of float64 tensors."""
+    s = x if residual is None else x + residual
+    y = s / (s.square().mean(-1, keepdim=True) + eps).sqrt() * w
+    return (y, 36 * U * y.abs()), (s, U * s.abs())
+
+
+def add_norm_backward(dy, h, w, eps, along=None):
+    """((gradient of the sum, bound), (gradient of the weight, bound))."""
+    r = 1 / (h.square().mean(-1, keepdim=True) + eps).sqrt()
+    n, u = h * r, dy * w
+    g = r * (u - n * (u * n).mean(-1, keepdim=True))
+    bound = 160 * U * r * (u.abs() + n.abs() * (u * n).abs().mean(-1, keepdim=True))
+    if along is not None:
+        g = g + along
+        bound = bound + U * g.abs()
+    rows = tuple(range(dy.dim() - 1))
+    return (g, bound), ((dy * n).sum(rows), 110 * U * (dy * n).abs().sum(rows))
+
+
+def eight_bits(y, scale, bound):
+    """How far a value of 8 bits times its scale may be off y: half a step (2^-4 of the value, the smallest step 2^-9), and y's
+    and the scale's own errors."""
+    return 1.01 * torch.maximum(2.0 ** -4 * y.abs(), 2.0 ** -10 * scale) + 2 * bound + 8 * U * y.abs()
