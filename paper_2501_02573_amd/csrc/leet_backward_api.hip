@@ -1,4 +1,6 @@
 // C ABI of the attention's backward pass: argument checks, segments, launches.  Nothing here touches tensor data.
+#include <math.h>
+
 #include "../../include/leet_attn.h"
 #include "leet_backward.hpp"
 #include "leet_common.hpp"
@@ -25,21 +27,72 @@ bool shape_ok(int r, int dv, int dtype) {
 
 struct Plan {
     int nseg, seg_chunks;
+    bool tiles;       // the kernel that takes a compute unit a segment
     size_t ws_bytes;  // states of both directions at the boundaries of segments
 };
 
+// What a call takes, in microseconds, by its number of segments.  Workgroups go to the eight XCDs in turn, and each has 32
+// compute units for them, which hold two: a chunk takes them alone_us with one and pair_us with two.  A call is its walk and,
+// with segments, the pre-pass over the states and the scan; neither is faster than its memory traffic.  Fitted (4 to 10 % rms) to
+// runs of BH 1..512, N 64..16384 and 1 to 64 segments; the picks are 0.8 % (bf16 128), 2.5 % (bf16 64) and 0.7 % (fp32) slower than
+// the best of each run on average.  Width 256 by fewer runs (BH 32 N 2048: 1 to 8 segments 291 221 168 140 178 153 us).
+struct CostModel {
+    double call_us, segments_us, segment_us;  // fixed: of a call, of having segments, of each of them
+    double alone_us, pair_us, round_us;       // walk: a chunk; what a round of workgroups begins with
+    double state_alone_us, state_pair_us;     // pre-pass: a chunk
+    double bytes_per_us;
+};
+constexpr CostModel kModel16x128 = {3.0, 9.7, 0.335, 2.61, 4.50, 6.6, 1.22, 1.85, 4.56e6};
+constexpr CostModel kModel16x64 = {5.5, 6.0, 0.292, 1.71, 2.23, 0.5, 0.92, 1.19, 5.24e6};
+constexpr CostModel kModel16x256 = {3.0, 9.7, 0.335, 9.0, 15.0, 8.0, 4.0, 8.0, 4.5e6};
+constexpr CostModel kModel32x128 = {3.0, 7.6, 0.377, 11.8, 25.5, 8.7, 5.42, 12.5, 3.5e6};
+constexpr CostModel kModel32x64 = {3.0, 6.0, 0.337, 4.85, 8.1, 3.4, 1.99, 2.60, 4.28e6};
+
+double predicted_us(const CostModel& m, long BH, int N, int r, int dv, int size, int nseg, int seg_chunks) {
+    auto chunk_us = [](long units, double alone, double pair) {  // of all rounds of an XCD's workgroups
+        const long rest = units % 64;
+        return units / 64 * pair + (rest == 0 ? 0.0 : rest <= 32 ? alone : pair);
+    };
+    const int roles = r == dv ? 3 : 2;  // width 256: dv has a launch of its own, counted in alone_us
+    const long units = roles * ((BH * nseg + 7) / 8);
+    // walks read seven tensors' worth (dk's and dv's common ones meet in the cache) and write three
+    const double tensor = (double)BH * N * (r + dv) / 2 * size;
+    double us = m.call_us + fmax(seg_chunks * chunk_us(units, m.alone_us, m.pair_us) + m.round_us * ((units + 63) / 64),
+                                 10 * tensor / m.bytes_per_us);
+    if (nseg > 1)
+        us += m.segments_us + m.segment_us * nseg +
+              fmax(seg_chunks * chunk_us(2 * ((BH * (nseg - 1) + 7) / 8), m.state_alone_us, m.state_pair_us),
+                   4 * tensor * (nseg - 1) / nseg / m.bytes_per_us);
+    return us;
+}
+
 bool make_plan(long BH, int N, int r, int dv, int dtype, int segments, Plan* plan) {
-    const int nchunks = (N + kChunk - 1) / kChunk;
-    long want = segments;
-    if (segments == 0) {
-        want = (512 + 3 * BH - 1) / (3 * BH);
-        const long cap = nchunks / 4;
-        if (want > cap) want = cap;
+    const int nchunks = (N + kChunk - 1) / kChunk, size = dtype == LEET_F32 ? 4 : 2;
+    const CostModel& m = dtype == LEET_F32 ? (r == 64 ? kModel32x64 : kModel32x128)
+                                           : dv == 256 ? kModel16x256 : r == 64 ? kModel16x64 : kModel16x128;
+    double best = 0.0;
+    auto consider = [&](int want) {  // a later candidate has to be 2 % better
+        const int seg_chunks = (nchunks + want - 1) / want, nseg = (nchunks + seg_chunks - 1) / seg_chunks;
+        const double us = predicted_us(m, BH, N, r, dv, size, nseg, seg_chunks);
+        if (best > 0.0 && us >= best * 0.98) return;
+        best = us;
+        plan->nseg = nseg;
+        plan->seg_chunks = seg_chunks;
+    };
+    if (segments > 0) consider(segments < nchunks ? segments : nchunks);
+    else
+        // 16-bit segments have two chunks at least
+        for (int want : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64})
+            if (want == 1 || (dtype == LEET_F32 ? want <= nchunks : 2 * want <= nchunks)) consider(want);
+    // The kernel that takes a compute unit a segment: one segment a sequence, no more workgroups than an XCD has compute units.  A
+    // chunk takes it 2.1 us in a few workgroups, 2.45 in 192.  us, here against the best of the other: BH 4 N 512 22.2 25.8, N 1024
+    // 39.4 29.0; BH 32 N 1024 39.9 44.5, N 2048 75.5 65.0; BH 64 N 4096 160 191, N 16384 653 720; BH 85 N 4096 302 265.
+    plan->tiles = r == 128 && dv == 128 && dtype != LEET_F32 && 3 * ((BH + 7) / 8) <= 32 &&
+                  (segments == 0 ? nchunks * (2.05 + 0.006 * BH) + 5.0 < best : plan->nseg == 1);
+    if (plan->tiles) {
+        plan->nseg = 1;
+        plan->seg_chunks = nchunks;
     }
-    if (want < 1) want = 1;
-    if (want > nchunks) want = nchunks;
-    plan->seg_chunks = (int)((nchunks + want - 1) / want);
-    plan->nseg = (nchunks + plan->seg_chunks - 1) / plan->seg_chunks;
     plan->ws_bytes = (size_t)2 * BH * (plan->nseg - 1) * r * dv * sizeof(float);
     // workgroups of up to 512 threads, three a segment; fewer than 2^32 threads a launch
     return BH * plan->nseg < 1L << 21;
@@ -73,7 +126,7 @@ int leet_attn_backward(const void *dout, const void *q, const void *k, const voi
     if ((reinterpret_cast<uintptr_t>(gamma) & 3u) || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return LEET_ERR_INVALID_ARG;
     const long BH = (long)B * H;
     if (BH >= 1L << 21 || N > 1 << 30) return LEET_ERR_TOO_LARGE;
-    Plan plan = {1, 0, 0};
+    Plan plan = {1, 0, false, 0};
     if (N > 0 && !make_plan(BH, N, r, dv, dtype, segments, &plan)) return LEET_ERR_TOO_LARGE;
     if (plan.ws_bytes && (!workspace || workspace_bytes < plan.ws_bytes)) return LEET_ERR_INVALID_ARG;
 
@@ -124,7 +177,9 @@ int leet_attn_backward(const void *dout, const void *q, const void *k, const voi
     if (e == hipSuccess && r == dv) {
         p.role[2] = of_v;
         p.roles = 3;
-        e = f32 ? leet::launch_bwd_f32_walk(p, r, s) : leet::launch_bwd_16bit_walk(p, r, r, f16, fine, s);
+        e = f32 ? leet::launch_bwd_f32_walk(p, r, s)
+            : plan.tiles ? leet::launch_bwd_16bit_tiles(p, f16, fine, s)
+                         : leet::launch_bwd_16bit_walk(p, r, r, f16, fine, s);
     } else if (e == hipSuccess) {
         e = leet::launch_bwd_16bit_walk(p, dv, r, f16, fine, s);
         p.role[0] = of_v;

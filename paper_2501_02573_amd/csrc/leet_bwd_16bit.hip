@@ -75,6 +75,21 @@ __device__ __forceinline__ void scaled(u32x4 x, f32x4 w0, f32x4 w1, u32x4 (&out)
     }
 }
 
+// The rows of a sequence that hold tokens tok0 .. tok0 + L - 1 of a walk (rows of `width` elements; `seq`: its first row), L = 64
+// or what is left before tok_end, as a buffer: what lies outside it is read as zero and not written, so that loads and stores
+// need no branches, behind which the compiler could no longer count those under way.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t chunk_rows(const void* seq, int width, bool rev, int N, int tok0, int tok_end) {
+    const int L = max(min(kChunk, tok_end - tok0), 0);
+    const uintptr_t addr = reinterpret_cast<uintptr_t>(seq) + (size_t)(rev ? N - tok0 - L : tok0) * (width * 2);
+    // the same in every lane; the compiler is told
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)addr), hi = __builtin_amdgcn_readfirstlane((uint32_t)(addr >> 32));
+    return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(((uintptr_t)hi << 32) | lo), 0,
+                                             __builtin_amdgcn_readfirstlane(L * width * 2), 0x00027000);
+}
+// Where row i of a chunk's tile begins in there.  A ragged chunk is right-aligned in the tile: rows above its first one, `shift`,
+// lie outside.
+__device__ __forceinline__ int row_at(int i, int width, bool rev, int shift) { return (rev ? kChunk - 1 - i : i - shift) * (width * 2); }
+
 // Score tiles in production order: tile 0 = (jt 0, it 0), tile 1 = (jt 1, it 1), tile 2 = (jt 0, it 1).
 __device__ __forceinline__ constexpr int tile_jt(int n) { return n == 1 ? 1 : 0; }
 __device__ __forceinline__ constexpr int tile_it(int n) { return n == 0 ? 0 : 1; }
@@ -345,12 +360,315 @@ __global__ __launch_bounds__(DV * 2, D > 128 || DV > 128 ? 1 : 2) void walk16_ke
     }
 }
 
+// ---- both widths alike: a wave for each 32 x 32 tile of the outputs ----
+//
+// What bounds a walk that has a compute unit to itself is the time that one chunk takes after the other, so here twice as many
+// waves share it, two a SIMD: wave (c, it) forms O^T[32 columns c][32 rows it] and carries the half `it` of the state's rows
+// for its columns.  A chunk has two halves with a barrier behind each:
+//   1  the next chunk's tiles into a second set of buffers; what comes from the state behind the last chunk, S^T X^T; the half
+//      `it` of the columns' z rows times Gam, to LDS as the operands that they will be;
+//   2  the state's update, and the new state to LDS as the 16-bit operand of the next chunk; Z^T P^T and the output; the next
+//      chunk's three score tiles, one each in three waves, to LDS as operands.
+// So what one half needs of another wave is formed early in the half before it, and loads have three chunks' time.
+//
+// A tile's rows are unpadded; 16-byte piece p of row r sits at piece p ^ turn(r).  Reads of one piece of 16 rows (operands
+// along a row) and transposing reads of four rows and four pieces meet every bank once.
+template <int PR>
+__device__ __forceinline__ constexpr int turn(int row) {
+    return PR == 16 ? 4 * (row & 3) + ((row >> 2) & 3) : 4 * ((row >> 1) & 1) + ((row >> 2) & 3);
+}
+
+template <int D>
+struct SmemTiles {
+    uint16_t x[2][kChunk * D], y[2][kChunk * D], z[2][kChunk * D];
+    uint16_t st[D * D];               // S^T[c][dk], turned as the tiles are
+    u32x4 pfrag[2][3][2][64];         // masked score tiles as B operands: [buffer][tile][register half][lane]
+    u32x4 zfrag[D / 32][4][64];       // Gam Z as B operands: [column tile][16 tokens][lane]
+    float pw[kChunk + 4];             // gamma^n, n = 0..64
+    float gw[kChunk];                 // Gam
+};
+
+template <int D, typename E, bool kDecay, int kTerms>
+__global__ __launch_bounds__(D * 4, 2) void tiles16_kernel(BwdParams p) {
+    constexpr int NT = D * 4;         // threads
+    constexpr int CT = D / 32;        // column tiles
+    constexpr int HT = D / 64;        // 32-row tiles of the state that a wave carries
+    constexpr int PR = D / 8;         // 16-byte pieces per row
+    constexpr int LP = kChunk * PR / NT;  // pieces per thread per tensor per chunk (= 2)
+    constexpr int LR = NT / PR;           // rows apart (= 32)
+    __shared__ __attribute__((aligned(16))) SmemTiles<D> sm;
+
+    const int tid = threadIdx.x;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, ln = l & 31, g = l >> 5;
+    const int c = w % CT, it = w / CT;
+    const int slot = blockIdx.x >> 3, which = slot % p.roles, unit = (slot / p.roles) * 8 + (blockIdx.x & 7);
+    if (unit >= p.BH * p.nseg) return;
+    const BwdRole& role = p.role[which];
+    const bool rev = role.reversed != 0;
+    const int bh = unit / p.nseg;
+    const int seg = rev ? p.nseg - 1 - unit % p.nseg : unit % p.nseg;
+    const int h = bh % p.H;
+
+    const int tok_begin = seg * p.seg_chunks * kChunk;
+    const int tok_end = (seg == p.nseg - 1) ? p.N : tok_begin + p.seg_chunks * kChunk;
+    const int nchunks = (tok_end - tok_begin + kChunk - 1) / kChunk;
+
+    // token t of the walk is row t, or N - 1 - t, of the sequence
+    const size_t seq = (size_t)bh * p.N * D;
+    const uint16_t *xb = static_cast<const uint16_t*>(role.x) + seq, *yb = static_cast<const uint16_t*>(role.y) + seq;
+    const uint16_t* zb = static_cast<const uint16_t*>(role.z) + seq;
+    uint16_t* ob = static_cast<uint16_t*>(role.out) + seq;
+
+    // the chunk ahead, in registers
+    struct Ahead {
+        u32x4 x[LP], y[LP], z[LP];
+    } ahead;
+    const int j_own = tid / PR, cc = tid % PR;
+    auto fetch = [&](int t) {  // zeros behind the last chunk
+        const int tok0 = tok_begin + t * kChunk, shift = max(0, tok0 + kChunk - tok_end);
+        const auto xr = chunk_rows(xb, D, rev, p.N, tok0, tok_end), yr = chunk_rows(yb, D, rev, p.N, tok0, tok_end);
+        const auto zr = chunk_rows(zb, D, rev, p.N, tok0, tok_end);
+#pragma unroll
+        for (int r = 0; r < LP; ++r) {
+            const int off = row_at(r * LR + j_own, D, rev, shift) + cc * 16;
+            ahead.x[r] = __builtin_amdgcn_raw_buffer_load_b128(xr, off, 0, 0);
+            ahead.y[r] = __builtin_amdgcn_raw_buffer_load_b128(yr, off, 0, 0);
+            ahead.z[r] = __builtin_amdgcn_raw_buffer_load_b128(zr, off, 0, 0);
+        }
+    };
+    const int to_own = (j_own * PR + (cc ^ turn<PR>(j_own))) * 8;
+    auto put = [&](const Ahead& a, int buf) {
+#pragma unroll
+        for (int r = 0; r < LP; ++r) {
+            *reinterpret_cast<u32x4*>(&sm.x[buf][to_own + r * LR * D]) = a.x[r];
+            *reinterpret_cast<u32x4*>(&sm.y[buf][to_own + r * LR * D]) = a.y[r];
+            *reinterpret_cast<u32x4*>(&sm.z[buf][to_own + r * LR * D]) = a.z[r];
+        }
+    };
+    fetch(0);
+
+    if (kDecay) {  // fp64 -> fp32 once per workgroup
+        const double gd = (double)p.gamma[h];
+        for (int n = tid; n <= kChunk; n += NT) {
+            const float v = (float)pow_int(gd, n);
+            sm.pw[n] = v;
+            const int j = kChunk - 1 + (rev ? 1 : 0) - n;
+            if (j >= 0 && j < kChunk) sm.gw[j] = v;
+        }
+    }
+
+    // state: S[i][r] = S[dk = 32 (HT it + i) + pi(m(r, g))][column 32c + ln]
+    f32x16 S[HT];
+    const int c_own = 32 * c + ln;
+    auto dk_of = [&](int i, int r) { return 32 * (HT * it + i) + 16 * (r >> 3) + 8 * g + 4 * ((r >> 2) & 1) + (r & 3); };
+#pragma unroll
+    for (int i = 0; i < HT; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) S[i][r] = 0.0f;
+    if (seg > 0) {
+        const float* src = role.slots + ((size_t)bh * (p.nseg - 1) + seg - 1) * D * D + (size_t)c_own * role.slot_col;
+#pragma unroll
+        for (int i = 0; i < HT; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) S[i][r] = src[dk_of(i, r) * role.slot_row];
+    }
+    if (role.enter) {
+        const float* src = role.enter + (size_t)bh * D * D + (size_t)c_own * role.enter_col;
+        const float left = kDecay ? (float)pow_int((double)p.gamma[h], tok_begin) : 1.0f;
+#pragma unroll
+        for (int i = 0; i < HT; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) S[i][r] += left * src[dk_of(i, r) * role.enter_row];
+    }
+
+    // Offsets (elements).  Operands along a row: piece 2s + g of row ln; the state's pieces of column ln likewise.
+    int at_row[D / 16];
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) at_row[s] = ln * D + (((2 * s) ^ g ^ turn<PR>(ln)) * 8);
+    // Transposing reads: row 4g + s16/4 (+ 8 rd + 16 f), four columns.  Eight rows on, a row's turn differs by 2.
+    const int s16 = l & 15, half = (l >> 4) & 1, r_tr = 4 * g + (s16 >> 2);
+    int z_tr[2], y_tr[HT][2];
+#pragma unroll
+    for (int rd = 0; rd < 2; ++rd) {
+        const int t = turn<PR>(r_tr + 8 * rd), at = (r_tr + 8 * rd) * D;
+        z_tr[rd] = at + ((4 * c + 2 * half + ((s16 >> 1) & 1)) ^ t) * 8 + 4 * (s16 & 1);
+#pragma unroll
+        for (int i = 0; i < HT; ++i) y_tr[i][rd] = at + ((4 * (HT * it + i) + 2 * half + (s16 & 1)) ^ t) * 8 + 4 * ((s16 >> 1) & 1);
+    }
+    auto gam_of = [&](int f, int more) { return *reinterpret_cast<const f32x4*>(&sm.gw[16 * f + 4 * g + more]); };
+    auto publish = [&]() {
+#pragma unroll
+        for (int i = 0; i < HT; ++i)
+#pragma unroll
+            for (int hh = 0; hh < 2; ++hh) {
+                // eight consecutive dk, piece 2 (2 tile + hh) + g of the column
+                const int s2 = 2 * (2 * (HT * it + i) + hh);
+                *reinterpret_cast<u32x4*>(&sm.st[32 * c * D + ln * D + ((s2 ^ g ^ turn<PR>(ln)) * 8)]) = pack_half<E>(S[i], hh);
+            }
+    };
+    publish();
+    put(ahead, 0);
+    fetch(1);
+    __syncthreads();  // tables and the first chunk visible
+
+    // The score tile that this wave forms, if any: 0 = (jt 0, it 0), 1 = (1, 1), 2 = (0, 1), by waves of its rows on SIMDs of
+    // their own.  Decay weights: on the diagonal i - j = ln - jr (zero above it), below it 32 + ln - jr.
+    const int later = rev ? 0 : 1;
+    constexpr bool kOneEach = CT > 2;
+    const int tile = kOneEach ? (it == 0 ? (c == 0 ? 0 : -1) : c == 1 ? 1 : c == 2 ? 2 : -1) : it == 0 ? (c == 0 ? 0 : -1) : c == 0 ? 1 : 2;
+    f32x16 wgt;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+        const int n = ln - (8 * (r >> 2) + 4 * g + (r & 3)) + (tile == 2 ? 32 : 0);
+        const float gn = kDecay ? sm.pw[max(n, 0)] : 1.0f;
+        wgt[r] = n >= 0 ? gn : 0.0f;
+    }
+    const float lam_full = kDecay ? sm.pw[32 * it + ln + later] : 1.0f;
+
+    u32x4 xf[D / 16];
+    // the rows of x that are the wave's own, and its score tile P^T = Y X^T, masked, of the chunk in buffer buf
+    auto scores = [&](int buf) {
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s) xf[s] = frag16(&sm.x[buf][32 * it * D] + at_row[s]);
+        if (tile < 0) return;
+        const uint16_t* y_row = &sm.y[buf][tile == 1 ? 32 * D : 0];
+        f32x16 acc;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[r] = 0.0f;
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s) acc = E::mfma32(frag16(y_row + at_row[s]), xf[s], acc);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[r] *= wgt[r];
+        sm.pfrag[buf][tile][0][l] = pack_half<E>(acc, 0);
+        sm.pfrag[buf][tile][1][l] = pack_half<E>(acc, 1);
+    };
+    scores(0);
+
+    auto chunk = [&](int t, int buf) {
+        const int tok0 = tok_begin + t * kChunk;
+        const int Lc = min(kChunk, tok_end - tok0);
+        const int shift = kChunk - Lc;  // a ragged last chunk is right-aligned in the tile, rows above are zero
+
+        __syncthreads();  // this chunk's scores and state are there, the last chunk's tiles are done with
+        put(ahead, buf ^ 1);
+        fetch(t + 2);
+
+        // zf[f] holds tokens 16f + {4g..4g+3, 8+4g..8+4g+3} of column c_own; rows of the wave's own half in mine
+        // (to fp32's precision the three terms of all four are formed again in each wave: LDS has no room for them)
+        u32x4 mine[2], other[2];
+        auto z_frag = [&](int f) { return join(lds_tr(&sm.z[buf][16 * f * D] + z_tr[0]), lds_tr(&sm.z[buf][16 * f * D] + z_tr[1])); };
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int f = 2 * it + i;
+            mine[i] = z_frag(f);
+            if constexpr (kTerms == 1) {
+                u32x4 zs[1] = {mine[i]};
+                if (kDecay) scaled<E, 1>(mine[i], gam_of(f, 0), gam_of(f, 8), zs);
+                sm.zfrag[c][f][l] = zs[0];
+            }
+        }
+        if (it == 1)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) other[i] = z_frag(i);
+
+        // O^T = S^T X^T, rows of O scaled by Lam
+        f32x16 o;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[r] = 0.0f;
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s) o = E::mfma32(frag16(&sm.st[32 * c * D] + at_row[s]), xf[s], o);
+        if (kDecay) {
+            const float lam = shift ? sm.pw[max(32 * it + ln + later - shift, 0)] : lam_full;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[r] *= lam;
+        }
+        __syncthreads();  // scaled rows and the next tiles are there, everyone has read the state
+
+        // S = gamma^L S + Y^T (Gam Z)
+        if (kDecay) {
+            const float gl = sm.pw[Lc];
+#pragma unroll
+            for (int i = 0; i < HT; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) S[i][r] *= gl;
+        }
+#pragma unroll
+        for (int f = 0; f < 4; ++f) {
+            u32x4 b[kTerms];
+            if constexpr (kTerms == 1) b[0] = sm.zfrag[c][f][l];
+            else scaled<E, kTerms>(z_frag(f), gam_of(f, 0), gam_of(f, 8), b);
+#pragma unroll
+            for (int i = 0; i < HT; ++i) {
+                const uint16_t* y_at = &sm.y[buf][16 * f * D];
+                const u32x4 a = join(lds_tr(y_at + y_tr[i][0]), lds_tr(y_at + y_tr[i][1]));
+#pragma unroll
+                for (int u = 0; u < kTerms; ++u) S[i] = E::mfma32(a, b[u], S[i]);
+            }
+        }
+        publish();
+
+        // O^T += Z^T P^T
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh) o = E::mfma32(mine[hh], sm.pfrag[buf][it][hh][l], o);
+        if (it == 1)
+#pragma unroll
+            for (int hh = 0; hh < 2; ++hh) o = E::mfma32(other[hh], sm.pfrag[buf][2][hh][l], o);
+
+        // O^T: lane = token 32it + ln, registers 4q..4q+3 = columns 32c + 8q + 4g + (0..3).  Lanes of the two halves swap
+        // words, and a lane has eight neighbouring columns of its row.
+        const auto to = chunk_rows(ob, D, rev, p.N, tok0, tok_end);
+        const int off = row_at(32 * it + ln, D, rev, shift) + (32 * c + 8 * g) * 2;
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            u32x4 val;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const u32x2 both = __builtin_amdgcn_permlane32_swap(E::pack2(o[8 * m + 2 * e], o[8 * m + 2 * e + 1]),
+                                                                    E::pack2(o[8 * m + 4 + 2 * e], o[8 * m + 5 + 2 * e]), false, false);
+                val[e] = both[0];
+                val[2 + e] = both[1];
+            }
+            __builtin_amdgcn_raw_buffer_store_b128(val, to, off + 32 * m, 0, 0);  // the cache joins the pieces of a row
+        }
+        scores(buf ^ 1);
+    };
+    // two at a time without a branch between them: the loads under way are counted at every wait
+    int t = 0;
+    for (; t + 1 < nchunks; t += 2) {
+        chunk(t, 0);
+        chunk(t + 1, 1);
+    }
+    if (t < nchunks) chunk(t, 0);
+
+    if (seg == p.nseg - 1 && role.leave) {
+        float* dst = role.leave + (size_t)bh * D * D;
+#pragma unroll
+        for (int i = 0; i < HT; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) dst[dk_of(i, r) * D + c_own] = S[i][r];
+    }
+}
+
+template <typename E>
+static hipError_t launch_tiles(const BwdParams& p, bool fine, hipStream_t stream) {
+    const dim3 grid((p.BH * p.nseg + 7) / 8 * 8 * p.roles), block(512);
+    if (!p.gamma) hipLaunchKernelGGL((tiles16_kernel<128, E, false, 1>), grid, block, 0, stream, p);
+    else if (fine) hipLaunchKernelGGL((tiles16_kernel<128, E, true, 3>), grid, block, 0, stream, p);
+    else hipLaunchKernelGGL((tiles16_kernel<128, E, true, 1>), grid, block, 0, stream, p);
+    return hipGetLastError();
+}
+
 template <int D, int DV, bool kOut, typename E, bool kDecay>
 static void launch_terms(const BwdParams& p, bool fine, hipStream_t stream) {
     const int units = p.BH * (kOut ? p.nseg : p.nseg - 1);
     const dim3 grid((units + 7) / 8 * 8 * p.roles), block(DV * 2);
-    if (kDecay && fine) hipLaunchKernelGGL((walk16_kernel<D, DV, kOut, E, kDecay, 3>), grid, block, 0, stream, p);
-    else hipLaunchKernelGGL((walk16_kernel<D, DV, kOut, E, kDecay, 1>), grid, block, 0, stream, p);
+    if constexpr (kDecay) {
+        if (fine) {
+            hipLaunchKernelGGL((walk16_kernel<D, DV, kOut, E, kDecay, 3>), grid, block, 0, stream, p);
+            return;
+        }
+    }
+    hipLaunchKernelGGL((walk16_kernel<D, DV, kOut, E, kDecay, 1>), grid, block, 0, stream, p);
 }
 
 template <int D, int DV, bool kOut>
@@ -379,6 +697,10 @@ hipError_t launch_bwd_16bit_states(const BwdParams& p, int D, int DV, bool f16, 
 
 hipError_t launch_bwd_16bit_walk(const BwdParams& p, int D, int DV, bool f16, bool fine, hipStream_t stream) {
     return bwd::launch_width<true>(p, D, DV, f16, fine, stream);
+}
+
+hipError_t launch_bwd_16bit_tiles(const BwdParams& p, bool f16, bool fine, hipStream_t stream) {
+    return f16 ? bwd::launch_tiles<ElemF16>(p, fine, stream) : bwd::launch_tiles<ElemBf16>(p, fine, stream);
 }
 
 }  // namespace leet
