@@ -95,6 +95,8 @@ __device__ __forceinline__ constexpr int tile_jt(int n) { return n == 1 ? 1 : 0;
 __device__ __forceinline__ constexpr int tile_it(int n) { return n == 0 ? 0 : 1; }
 
 // kOut = true: outputs and state.  kOut = false: state only, of every segment but the last, started from zero.
+// kTerms: of Gam Z, whose rounding to one would be as large as the outputs' own (two: the outputs' error falls from 1.65 to 1.4
+// times that of outputs that are rounded alone; a call takes 5 to 15 % longer).  Three give a leaving state to fp32's precision.
 template <int D, int DV, bool kOut, typename E, bool kDecay, int kTerms>
 __global__ __launch_bounds__(DV * 2, D > 128 || DV > 128 ? 1 : 2) void walk16_kernel(BwdParams p) {
     constexpr int NT = DV * 2;   // threads: one wave per 32 columns of z and out
@@ -343,7 +345,7 @@ __global__ __launch_bounds__(DV * 2, D > 128 || DV > 128 ? 1 : 2) void walk16_ke
             for (int dt = 0; dt < DT; ++dt) {
                 const u32x4 a = join(lds_tr(y_tr + (16 * f) * RS + 32 * dt), lds_tr(y_tr + (16 * f + 8) * RS + 32 * dt));
 #pragma unroll
-                for (int u = 0; u < (kDecay ? kTerms : 1); ++u) S[dt] = E::mfma32(a, zs[u], S[dt]);
+                for (int u = 0; u < kTerms; ++u) S[dt] = E::mfma32(a, zs[u], S[dt]);
             }
         }
     }
@@ -554,17 +556,19 @@ __global__ __launch_bounds__(D * 4, 2) void tiles16_kernel(BwdParams p) {
         fetch(t + 2);
 
         // zf[f] holds tokens 16f + {4g..4g+3, 8+4g..8+4g+3} of column c_own; rows of the wave's own half in mine
-        // (to fp32's precision the three terms of all four are formed again in each wave: LDS has no room for them)
+        // The second term goes to the place of this chunk's rows of x, which are in registers.
         u32x4 mine[2], other[2];
+        u32x4* rest = reinterpret_cast<u32x4*>(sm.x[buf]);
         auto z_frag = [&](int f) { return join(lds_tr(&sm.z[buf][16 * f * D] + z_tr[0]), lds_tr(&sm.z[buf][16 * f * D] + z_tr[1])); };
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int f = 2 * it + i;
             mine[i] = z_frag(f);
-            if constexpr (kTerms == 1) {
-                u32x4 zs[1] = {mine[i]};
-                if (kDecay) scaled<E, 1>(mine[i], gam_of(f, 0), gam_of(f, 8), zs);
+            if constexpr (kTerms < 3) {
+                u32x4 zs[kTerms] = {mine[i]};
+                if (kDecay) scaled<E, kTerms>(mine[i], gam_of(f, 0), gam_of(f, 8), zs);
                 sm.zfrag[c][f][l] = zs[0];
+                if (kTerms > 1) rest[(c * 4 + f) * 64 + l] = zs[kTerms - 1];
             }
         }
         if (it == 1)
@@ -595,8 +599,12 @@ __global__ __launch_bounds__(D * 4, 2) void tiles16_kernel(BwdParams p) {
 #pragma unroll
         for (int f = 0; f < 4; ++f) {
             u32x4 b[kTerms];
-            if constexpr (kTerms == 1) b[0] = sm.zfrag[c][f][l];
-            else scaled<E, kTerms>(z_frag(f), gam_of(f, 0), gam_of(f, 8), b);
+            if constexpr (kTerms < 3) {
+                b[0] = sm.zfrag[c][f][l];
+                if (kTerms > 1) b[kTerms - 1] = rest[(c * 4 + f) * 64 + l];
+            } else {  // LDS has no room for the third: each wave forms all four anew
+                scaled<E, kTerms>(z_frag(f), gam_of(f, 0), gam_of(f, 8), b);
+            }
 #pragma unroll
             for (int i = 0; i < HT; ++i) {
                 const uint16_t* y_at = &sm.y[buf][16 * f * D];
@@ -654,7 +662,7 @@ static hipError_t launch_tiles(const BwdParams& p, bool fine, hipStream_t stream
     const dim3 grid((p.BH * p.nseg + 7) / 8 * 8 * p.roles), block(512);
     if (!p.gamma) hipLaunchKernelGGL((tiles16_kernel<128, E, false, 1>), grid, block, 0, stream, p);
     else if (fine) hipLaunchKernelGGL((tiles16_kernel<128, E, true, 3>), grid, block, 0, stream, p);
-    else hipLaunchKernelGGL((tiles16_kernel<128, E, true, 1>), grid, block, 0, stream, p);
+    else hipLaunchKernelGGL((tiles16_kernel<128, E, true, 2>), grid, block, 0, stream, p);
     return hipGetLastError();
 }
 
@@ -662,13 +670,9 @@ template <int D, int DV, bool kOut, typename E, bool kDecay>
 static void launch_terms(const BwdParams& p, bool fine, hipStream_t stream) {
     const int units = p.BH * (kOut ? p.nseg : p.nseg - 1);
     const dim3 grid((units + 7) / 8 * 8 * p.roles), block(DV * 2);
-    if constexpr (kDecay) {
-        if (fine) {
-            hipLaunchKernelGGL((walk16_kernel<D, DV, kOut, E, kDecay, 3>), grid, block, 0, stream, p);
-            return;
-        }
-    }
-    hipLaunchKernelGGL((walk16_kernel<D, DV, kOut, E, kDecay, 1>), grid, block, 0, stream, p);
+    if constexpr (!kDecay) hipLaunchKernelGGL((walk16_kernel<D, DV, kOut, E, false, 1>), grid, block, 0, stream, p);
+    else if (fine) hipLaunchKernelGGL((walk16_kernel<D, DV, kOut, E, true, 3>), grid, block, 0, stream, p);
+    else hipLaunchKernelGGL((walk16_kernel<D, DV, kOut, E, true, 2>), grid, block, 0, stream, p);
 }
 
 template <int D, int DV, bool kOut>
