@@ -31,38 +31,44 @@ struct Plan {
     size_t ws_bytes;  // states of both directions at the boundaries of segments
 };
 
-// What a call takes, in microseconds, by its number of segments.  Workgroups go to the eight XCDs in turn, and each has 32
-// compute units for them, which hold two: a chunk takes them alone_us with one and pair_us with two.  A call is its walk and,
-// with segments, the pre-pass over the states and the scan; neither is faster than its memory traffic.  Fitted (4 to 10 % rms) to
-// runs of BH 1..512, N 64..16384 and 1 to 64 segments; the picks are 0.8 % (bf16 128), 2.5 % (bf16 64) and 0.7 % (fp32) slower than
-// the best of each run on average.  Width 256 by fewer runs (BH 32 N 2048: 1 to 8 segments 291 221 168 140 178 153 us).
+// What a call takes, in microseconds, by its number of segments.  Workgroups go to the eight XCDs in turn, and an XCD holds
+// `resident` of them on 32 compute units: a chunk takes them alone_us while each has a unit to itself, full_us when all are there.
+// A call is its walk and, with segments, the pre-pass over the states and the scan, each the smooth maximum
+// (x^p + y^p)^(1/p) of that and of its memory traffic.  Fitted (3 to 8 % rms) to runs of BH 1..512, N 64..32768 and 1 to 64
+// segments; the picks are 0.4 % (16-bit, 128), 1.2 % (16-bit, 64) and 0.7 % (fp32) slower than the best of each run on average.  Width
+// 256 by fewer runs (BH 32 N 2048, 1 to 8 segments: 291 221 168 140 178 153 us).
 struct CostModel {
     double call_us, segments_us, segment_us;  // fixed: of a call, of having segments, of each of them
-    double alone_us, pair_us, round_us;       // walk: a chunk; what a round of workgroups begins with
-    double state_alone_us, state_pair_us;     // pre-pass: a chunk
-    double bytes_per_us;
+    double alone_us, full_us, round_us;       // walk: a chunk; what a round of workgroups begins with
+    double state_alone_us, state_full_us;     // pre-pass: a chunk
+    double bytes_per_us, p;
+    int resident;
 };
-constexpr CostModel kModel16x128 = {3.0, 9.7, 0.335, 2.61, 4.50, 6.6, 1.22, 1.85, 4.56e6};
-constexpr CostModel kModel16x64 = {5.5, 6.0, 0.292, 1.71, 2.23, 0.5, 0.92, 1.19, 5.24e6};
-constexpr CostModel kModel16x256 = {3.0, 9.7, 0.335, 9.0, 15.0, 8.0, 4.0, 8.0, 4.5e6};
-constexpr CostModel kModel32x128 = {3.0, 7.6, 0.377, 11.8, 25.5, 8.7, 5.42, 12.5, 3.5e6};
-constexpr CostModel kModel32x64 = {3.0, 6.0, 0.337, 4.85, 8.1, 3.4, 1.99, 2.60, 4.28e6};
+constexpr CostModel kModel16x128 = {3.0, 7.9, 0.32, 2.41, 3.82, 9.0, 1.94, 3.08, 4.70e6, 4.0, 64};
+constexpr CostModel kModel16x64 = {7.3, 5.3, 0.323, 2.13, 3.33, 0.1, 1.09, 1.15, 5.39e6, 4.0, 128};
+constexpr CostModel kModel16x256 = {3.0, 9.7, 0.335, 9.0, 22.0, 8.0, 4.0, 8.0, 4.50e6, 20.0, 64};
+constexpr CostModel kModel32x128 = {3.0, 7.6, 0.377, 11.8, 25.5, 8.7, 5.42, 12.5, 3.50e6, 20.0, 64};
+constexpr CostModel kModel32x64 = {3.0, 6.0, 0.337, 4.85, 8.10, 3.4, 1.99, 2.60, 4.28e6, 20.0, 64};
+
+double smooth_max(double a, double b, double p) { return pow(pow(a, p) + pow(b, p), 1.0 / p); }
 
 double predicted_us(const CostModel& m, long BH, int N, int r, int dv, int size, int nseg, int seg_chunks) {
-    auto chunk_us = [](long units, double alone, double pair) {  // of all rounds of an XCD's workgroups
-        const long rest = units % 64;
-        return units / 64 * pair + (rest == 0 ? 0.0 : rest <= 32 ? alone : pair);
+    auto chunk_us = [&](long units, double alone, double full) {  // of all rounds of an XCD's workgroups
+        const long rest = units % m.resident;
+        return units / m.resident * full + (rest == 0 ? 0.0 : rest <= 32 ? alone : m.resident == 64 ? full
+                                                 : alone + (full - alone) * (rest - 32) / (m.resident - 32));
     };
     const int roles = r == dv ? 3 : 2;  // width 256: dv has a launch of its own, counted in alone_us
     const long units = roles * ((BH * nseg + 7) / 8);
     // walks read seven tensors' worth (dk's and dv's common ones meet in the cache) and write three
     const double tensor = (double)BH * N * (r + dv) / 2 * size;
-    double us = m.call_us + fmax(seg_chunks * chunk_us(units, m.alone_us, m.pair_us) + m.round_us * ((units + 63) / 64),
-                                 10 * tensor / m.bytes_per_us);
+    double us = m.call_us + smooth_max(seg_chunks * chunk_us(units, m.alone_us, m.full_us) +
+                                           m.round_us * ((units + m.resident - 1) / m.resident),
+                                       10 * tensor / m.bytes_per_us, m.p);
     if (nseg > 1)
         us += m.segments_us + m.segment_us * nseg +
-              fmax(seg_chunks * chunk_us(2 * ((BH * (nseg - 1) + 7) / 8), m.state_alone_us, m.state_pair_us),
-                   4 * tensor * (nseg - 1) / nseg / m.bytes_per_us);
+              smooth_max(seg_chunks * chunk_us(2 * ((BH * (nseg - 1) + 7) / 8), m.state_alone_us, m.state_full_us),
+                         4 * tensor * (nseg - 1) / nseg / m.bytes_per_us, m.p);
     return us;
 }
 
@@ -85,10 +91,10 @@ bool make_plan(long BH, int N, int r, int dv, int dtype, int segments, Plan* pla
         for (int want : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64})
             if (want == 1 || (dtype == LEET_F32 ? want <= nchunks : 2 * want <= nchunks)) consider(want);
     // The kernel that takes a compute unit a segment: one segment a sequence, no more workgroups than an XCD has compute units.  A
-    // chunk takes it 2.1 us in a few workgroups, 2.45 in 192.  us, here against the best of the other: BH 4 N 512 22.2 25.8, N 1024
-    // 39.4 29.0; BH 32 N 1024 39.9 44.5, N 2048 75.5 65.0; BH 64 N 4096 160 191, N 16384 653 720; BH 85 N 4096 302 265.
+    // chunk takes it 2.3 us in a few workgroups, 2.7 in 192.  us, here against the best of the other: BH 4 N 512 24 26, N 1024 43
+    // 30; BH 32 N 1024 43 46, N 2048 83 68; BH 64 N 4096 177 200, N 16384 715 740; BH 85 N 4096 (a second round) 302 270.
     plan->tiles = r == 128 && dv == 128 && dtype != LEET_F32 && 3 * ((BH + 7) / 8) <= 32 &&
-                  (segments == 0 ? nchunks * (2.05 + 0.006 * BH) + 5.0 < best : plan->nseg == 1);
+                  (segments == 0 ? nchunks * (2.3 + 0.0065 * BH) + 5.0 < best : plan->nseg == 1);
     if (plan->tiles) {
         plan->nseg = 1;
         plan->seg_chunks = nchunks;
