@@ -1265,20 +1265,25 @@ def leet_attn_clip_gradients(grads, limit: Optional[float] = None, outs=None, no
     targets = grads if outs is None else list(outs)
     if len(targets) != len(grads):
         raise ValueError("outs must be as many as grads")
-    dev = _on(*grads, *targets, norm, workspace)
-    packed = bytearray(_gradient.size * len(grads))
-    for n, (g, o) in enumerate(zip(grads, targets)):
-        if o is not g and (o.dtype != g.dtype or o.shape != g.shape or o.stride() != g.stride()):
-            raise ValueError("outs must have the shapes, strides and types of grads")
-        if not g.is_contiguous() and not torch.ops.aten.is_non_overlapping_and_dense(g):
-            raise ValueError("gradients must be dense")
-        _gradient.pack_into(packed, n * _gradient.size, g.data_ptr(), o.data_ptr(), g.numel(), _dtype_code(g))
+    dev = _on(grads[0], norm, workspace)
+    packed, pack = [], _gradient.pack
+    for g, o in zip(grads, targets):  # a microsecond a tensor
+        if g.get_device() != dev or o.get_device() != dev:
+            raise ValueError("all tensors must be GPU tensors on one device")
+        if o is not g and (o.dtype is not g.dtype or o.shape != g.shape):
+            raise ValueError("outs must have the shapes and types of grads")
+        if not (g.is_contiguous() and (o is g or o.is_contiguous())):
+            if not torch.ops.aten.is_non_overlapping_and_dense(g):
+                raise ValueError("gradients must be dense")
+            if o.stride() != g.stride():
+                raise ValueError("outs must have the strides of grads")
+        packed.append(pack(g.data_ptr(), o.data_ptr(), g.numel(), _dtype_code(g)))
     if norm is None:
         norm = torch.empty(1, dtype=torch.float32, device=torch.device("cuda", dev))
     elif norm.dtype != torch.float32 or norm.numel() != 1:
         raise ValueError("norm must be one float32")
     ws, ws_bytes, keep = _scratch(clip_gradients_workspace_bytes() if workspace is None else 0, workspace, dev)
-    st = _call_on(dev, lib.leet_attn_clip_gradients, bytes(packed), len(grads), float("inf") if limit is None else limit,
+    st = _call_on(dev, lib.leet_attn_clip_gradients, b"".join(packed), len(grads), float("inf") if limit is None else limit,
                   _ptr(norm), ws, ws_bytes)
     if st != LEET_OK:
         raise LeetAttnError(st, "leet_attn_clip_gradients")

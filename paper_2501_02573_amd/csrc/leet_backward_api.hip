@@ -104,6 +104,24 @@ bool make_plan(long BH, int N, int r, int dv, int dtype, int segments, Plan* pla
     return BH * plan->nseg < 1L << 21;
 }
 
+// make_plan with the last plan of the calling thread kept: a call asks for it twice, and a program's calls mostly repeat one shape.
+bool call_plan(long BH, int N, int r, int dv, int dtype, int segments, Plan* plan) {
+    struct Kept {
+        long BH = 0;  // 0: nothing kept
+        int N, r, dv, dtype, segments;
+        Plan plan;
+    };
+    static thread_local Kept kept;
+    if (kept.BH != BH || kept.N != N || kept.r != r || kept.dv != dv || kept.dtype != dtype || kept.segments != segments) {
+        kept.BH = 0;
+        if (!make_plan(BH, N, r, dv, dtype, segments, &kept.plan)) return false;
+        kept.BH = BH; kept.N = N; kept.r = r; kept.dv = dv;
+        kept.dtype = dtype; kept.segments = segments;
+    }
+    *plan = kept.plan;
+    return true;
+}
+
 }  // namespace
 
 extern "C" {
@@ -111,7 +129,7 @@ extern "C" {
 size_t leet_attn_backward_workspace_bytes(int B, int H, int N, int r, int dv, int dtype, int segments) {
     Plan plan;
     if (B <= 0 || H <= 0 || N <= 0 || segments < 0 || !shape_ok(r, dv, dtype) || (long)B * H >= 1L << 21 || N > 1 << 30 ||
-        !make_plan((long)B * H, N, r, dv, dtype, segments, &plan))
+        !call_plan((long)B * H, N, r, dv, dtype, segments, &plan))
         return 0;
     return plan.ws_bytes;
 }
@@ -133,7 +151,7 @@ int leet_attn_backward(const void *dout, const void *q, const void *k, const voi
     const long BH = (long)B * H;
     if (BH >= 1L << 21 || N > 1 << 30) return LEET_ERR_TOO_LARGE;
     Plan plan = {1, 0, false, 0};
-    if (N > 0 && !make_plan(BH, N, r, dv, dtype, segments, &plan)) return LEET_ERR_TOO_LARGE;
+    if (N > 0 && !call_plan(BH, N, r, dv, dtype, segments, &plan)) return LEET_ERR_TOO_LARGE;
     if (plan.ws_bytes && (!workspace || workspace_bytes < plan.ws_bytes)) return LEET_ERR_INVALID_ARG;
 
     const long long isz = dtype == LEET_F32 ? 4 : 2, rows = (long long)BH * N, states = (long long)BH * r * dv;

@@ -81,6 +81,12 @@ struct Tile {
             }
         return sum;
     }
+    template <bool kFar>
+    static __device__ __forceinline__ void put(char* p, Word w) {
+        if (kFar) __builtin_nontemporal_store(w, reinterpret_cast<Anywhere*>(p));
+        else *reinterpret_cast<Anywhere*>(p) = w;
+    }
+    template <bool kFar>
     __device__ __forceinline__ void store(char* p, int count, float first, float by) const {
 #pragma unroll
         for (int i = 0; i < kClipPieces; ++i) {
@@ -90,11 +96,11 @@ struct Tile {
             char* to = p + (size_t)at(i) * kBytes;
             if (at(i) + 8 <= count) {
                 if constexpr (kElem == 0) {
-                    *reinterpret_cast<Anywhere*>(to) = __builtin_bit_cast(Word, f32x4{f[0], f[1], f[2], f[3]});
-                    *(reinterpret_cast<Anywhere*>(to) + 1) = __builtin_bit_cast(Word, f32x4{f[4], f[5], f[6], f[7]});
+                    put<kFar>(to, __builtin_bit_cast(Word, f32x4{f[0], f[1], f[2], f[3]}));
+                    put<kFar>(to + 16, __builtin_bit_cast(Word, f32x4{f[4], f[5], f[6], f[7]}));
                 } else {
-                    *reinterpret_cast<Anywhere*>(to) = Word{Io<kElem>::pack2(f[0], f[1]), Io<kElem>::pack2(f[2], f[3]),
-                                                           Io<kElem>::pack2(f[4], f[5]), Io<kElem>::pack2(f[6], f[7])};
+                    put<kFar>(to, Word{Io<kElem>::pack2(f[0], f[1]), Io<kElem>::pack2(f[2], f[3]), Io<kElem>::pack2(f[4], f[5]),
+                                       Io<kElem>::pack2(f[6], f[7])});
                 }
             } else {
 #pragma unroll
@@ -123,11 +129,11 @@ __device__ __forceinline__ double tile_squares(const ClipParams& p, const TileOf
     x.load(p.data[t.tensor] + t.begin * Io<kElem>::kBytes, t.count);
     return x.squares();
 }
-template <int kElem>
+template <int kElem, bool kFar>
 __device__ __forceinline__ void tile_times(const ClipParams& p, const TileOf& t, float first, float by) {
     Tile<kElem> x;
     x.load(p.data[t.tensor] + t.begin * Io<kElem>::kBytes, t.count);
-    x.store(p.out[t.tensor] + t.begin * Io<kElem>::kBytes, t.count, first, by);
+    x.template store<kFar>(p.out[t.tensor] + t.begin * Io<kElem>::kBytes, t.count, first, by);
 }
 
 __global__ __launch_bounds__(kClipThreads) void clip_squares_kernel(ClipParams p) {
@@ -143,6 +149,9 @@ __global__ __launch_bounds__(kClipThreads) void clip_squares_kernel(ClipParams p
     if (threadIdx.x == 0) p.parts[blockIdx.x] = sum + (p.add ? p.parts[blockIdx.x] : 0.0);
 }
 
+// kFar: the tensors exceed the last-level cache, and what is written goes past it.  453 MB of bf16 clipped into buffers of their own:
+// 264 -> 240 us, with tiles of 16384 elements instead of 8192 234.
+template <bool kFar>
 __global__ __launch_bounds__(kClipThreads) void clip_kernel(ClipParams p) {
     __shared__ double sums[kClipThreads / 64];
     double sum = 0.0;
@@ -158,9 +167,9 @@ __global__ __launch_bounds__(kClipThreads) void clip_kernel(ClipParams p) {
         const TileOf t(p, tiles - 1 - turn);
         if (factor == 1.0 && p.out[t.tensor] == p.data[t.tensor]) continue;
         const int elem = p.elem[t.tensor];
-        if (elem == 0) tile_times<0>(p, t, first, by);
-        else if (elem == 1) tile_times<1>(p, t, first, by);
-        else tile_times<2>(p, t, first, by);
+        if (elem == 0) tile_times<0, kFar>(p, t, first, by);
+        else if (elem == 1) tile_times<1, kFar>(p, t, first, by);
+        else tile_times<2, kFar>(p, t, first, by);
     }
 }
 
@@ -171,7 +180,9 @@ hipError_t launch_clip_squares(const ClipParams& p, hipStream_t stream) {
 
 hipError_t launch_clip(const ClipParams& p, hipStream_t stream) {
     const int tiles = p.first[p.tensors];
-    hipLaunchKernelGGL(clip_kernel, dim3(tiles < 1 ? 1 : tiles < 2048 ? tiles : 2048), dim3(kClipThreads), 0, stream, p);
+    const dim3 grid(tiles < 1 ? 1 : tiles < 2048 ? tiles : 2048), block(kClipThreads);
+    if (p.far) hipLaunchKernelGGL((clip_kernel<true>), grid, block, 0, stream, p);
+    else hipLaunchKernelGGL((clip_kernel<false>), grid, block, 0, stream, p);
     return hipGetLastError();
 }
 

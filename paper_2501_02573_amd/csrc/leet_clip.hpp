@@ -6,7 +6,7 @@
 namespace leet {
 
 constexpr int kClipTensors = 64;    // of a launch
-constexpr int kClipTile = 8192;     // elements that a workgroup takes at once
+constexpr int kClipTile = 16384;    // elements that a workgroup takes at once
 constexpr int kClipParts = 1024;    // sums of squares that the tensors are cut into, one a workgroup
 
 struct ClipParams {
@@ -16,6 +16,7 @@ struct ClipParams {
     int first[kClipTensors + 1];    // the tile that a tensor begins with; of the last + 1, all tiles
     unsigned char elem[kClipTensors];  // 0 = fp32, 1 = bf16, 2 = fp16
     int tensors;
+    int far;                        // clip: all tensors together exceed the last-level cache
     int add;                        // squares: to the sums that launches before left
     double* parts;                  // [kClipParts]
     float* norm;                    // clip: where the norm goes, or null

@@ -600,6 +600,7 @@ int leet_attn_clip_gradients(const leet_attn_gradient *grads, int count, float l
         return LEET_ERR_INVALID_ARG;
     if (count > 1 << 20) return LEET_ERR_TOO_LARGE;
     const bool clips = isfinite(limit);
+    size_t moved = 0;
     for (int i = 0; i < count; ++i) {
         const leet_attn_gradient& g = grads[i];
         if (!dtype_ok(g.dtype)) return LEET_ERR_UNSUPPORTED;
@@ -607,6 +608,7 @@ int leet_attn_clip_gradients(const leet_attn_gradient *grads, int count, float l
             !aligned(g.out, size_of(g.dtype)))
             return LEET_ERR_INVALID_ARG;
         if (g.count > 1LL << 40) return LEET_ERR_TOO_LARGE;
+        moved += 2 * (size_t)g.count * size_of(g.dtype);
     }
     // an output is its own gradient or lies apart from everything else
     Extent few[2 * leet::kClipTensors + 2], *extents = few;
@@ -633,6 +635,7 @@ int leet_attn_clip_gradients(const leet_attn_gradient *grads, int count, float l
     leet::ClipParams p = {};
     p.parts = static_cast<double*>(workspace);
     p.limit = limit;
+    p.far = moved > kStreamBytes;
     hipError_t e = hipSuccess;
     // the tensors in launches of kClipTensors; `over` is called with each launch's parameters
     auto launches = [&](auto over) {

@@ -364,9 +364,11 @@ __global__ __launch_bounds__(T * kRowsAtOnce<T>) void norm_backward_kernel(NormP
             if (j < count[k]) to[first[k] + j] = dw[k][j];
 }
 
-// dw = sum of the rows of `partial`.  Workgroup = 16 columns x 64 row groups; each thread adds its rows in order, the groups
+// dw = sum of the rows of `partial`.  Workgroup = 32 columns x 32 row groups; each thread adds its rows in order, the groups
 // are joined in a fixed tree.
-constexpr int kNormColumns = 16, kNormGroups = 64;
+// us of both kernels with 8 columns x 128 groups, 16 x 64, 32 x 32: 16384 rows of 2048 59 57 56, of 4096 104 100 99, 2048 of 1024 15
+// 13.7 12.7, 4096 of 16384 116 110 107 (bf16).
+constexpr int kNormColumns = 32, kNormGroups = 32;
 template <int kElem>
 __global__ __launch_bounds__(kNormColumns * kNormGroups) void norm_weight_kernel(NormParams p) {
     __shared__ float part[kNormGroups][kNormColumns + 1];
@@ -390,7 +392,9 @@ __global__ __launch_bounds__(kNormColumns * kNormGroups) void norm_weight_kernel
 
 int norm_rows_at_once(int C) { return C <= 512 ? 4 : 1; }
 
-// As many workgroups as the device holds at once, so that each ends with one row of sums.
+// About as many workgroups as the device holds at once, each of which ends with one row of sums.  us with half, these and twice as
+// many: 16384 rows of 2048 63 57 65, 4094 of 1001 fp32 - 20.6 23.4, 16384 of 4096 - 100 106 (bf16).  Loading the next row while one
+// is worked on gained nothing (54.8 and 55.5, 99.3 and 99.0).
 int norm_groups(int rows, int C) {
     const int at_once = norm_rows_at_once(C);
     const long need = ((long)rows + at_once - 1) / at_once, most = C <= 2048 ? 1024 : C <= 4096 ? 512 : 256;
