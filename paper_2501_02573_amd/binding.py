@@ -1262,6 +1262,8 @@ def leet_attn_clip_gradients(grads, limit: Optional[float] = None, outs=None, no
     grads = list(grads)
     if not grads:
         raise ValueError("no gradients")
+    if outs is not None and (limit is None or limit == float("inf")):
+        raise ValueError("outs without a limit")
     targets = grads if outs is None else list(outs)
     if len(targets) != len(grads):
         raise ValueError("outs must be as many as grads")

@@ -100,8 +100,9 @@ bool make_plan(long BH, int N, int r, int dv, int dtype, int segments, Plan* pla
         plan->seg_chunks = nchunks;
     }
     plan->ws_bytes = (size_t)2 * BH * (plan->nseg - 1) * r * dv * sizeof(float);
-    // workgroups of up to 512 threads, three a segment; fewer than 2^32 threads a launch
-    return BH * plan->nseg < 1L << 21;
+    // fewer than 2^32 threads a launch: workgroups of up to 512 threads, three a segment; the scan, a thread for four elements of the
+    // states of both directions
+    return BH * plan->nseg < 1L << 21 && (plan->nseg == 1 || 2 * BH * (r * dv / 4) < 1L << 32);
 }
 
 // make_plan with the last plan of the calling thread kept: a call asks for it twice, and a program's calls mostly repeat one shape.

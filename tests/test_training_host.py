@@ -90,6 +90,7 @@ def test_backward_unsupported(leet, bad):
 def test_backward_too_large(leet):
     assert backward(leet, B=1 << 20, H=1 << 10) == leet.LEET_ERR_TOO_LARGE
     assert backward(leet, N=(1 << 30) + 1) == leet.LEET_ERR_TOO_LARGE
+    assert backward(leet, B=1 << 10, H=1 << 9, segments=2, wsb=1 << 62) == leet.LEET_ERR_TOO_LARGE   # the scan's threads
 
 
 def test_backward_outputs_over_other_arguments(leet):
@@ -306,3 +307,6 @@ def test_clip_binding_refuses(leet):
         leet.leet_attn_clip_gradients([x], 1.0)
     with pytest.raises(ValueError):
         leet.leet_attn_clip_gradients([x], 1.0, outs=[])
+    for limit in (None, float("inf")):
+        with pytest.raises(ValueError):   # nothing would be written
+            leet.leet_attn_clip_gradients([x], limit, outs=[x.clone()])
