@@ -15,6 +15,14 @@
 //
 // In the order of the tokens S is the transposed state before a chunk: Lam = gamma^(i+1), Gam = gamma^(L-1-j).  Reversed, S
 // is the gradient of the state that the chunk's last token leaves: Lam = gamma^i, Gam = gamma^(L-j).
+//
+// The three walks read seven tensors' worth (dout three times, v, q and k twice each, less what dK and dV, side by side on an XCD,
+// take from its L2) and write three.  Two kernels: walk16_kernel, many small workgroups, for any number of segments; and
+// tiles16_kernel, one large workgroup a sequence, where there are few sequences.  With segments a pre-pass over the states
+// of both directions (walk16_kernel without outputs) and the scan of their boundaries come first.
+// Near memory's rate where the device is full: B16 H32 N2048 d128 bf16 takes 582 us, its ten tensors at 4.6 TB/s (with one term 530,
+// 5.1).  Few sequences are bound by a chunk's latency, or by segments' pre-pass, which reads four tensors again.  B4 H16 N4096: 174
+// to 179 us, of which its ten tensors are 131 at 5.1 TB/s; with dstate_in wanted and three terms 207.
 #include "leet_backward.hpp"
 #include "leet_common.hpp"
 
@@ -96,7 +104,8 @@ __device__ __forceinline__ constexpr int tile_it(int n) { return n == 0 ? 0 : 1;
 
 // kOut = true: outputs and state.  kOut = false: state only, of every segment but the last, started from zero.
 // kTerms: of Gam Z, whose rounding to one would be as large as the outputs' own (two: the outputs' error falls from 1.65 to 1.4
-// times that of outputs that are rounded alone; a call takes 5 to 15 % longer).  Three give a leaving state to fp32's precision.
+// times that of outputs that are rounded alone; B4 H16 N4096 d128 bf16 155 -> 173 us).  Three give a leaving state to fp32's
+// precision.
 template <int D, int DV, bool kOut, typename E, bool kDecay, int kTerms>
 __global__ __launch_bounds__(DV * 2, D > 128 || DV > 128 ? 1 : 2) void walk16_kernel(BwdParams p) {
     constexpr int NT = DV * 2;   // threads: one wave per 32 columns of z and out
@@ -371,7 +380,13 @@ __global__ __launch_bounds__(DV * 2, D > 128 || DV > 128 ? 1 : 2) void walk16_ke
 //      `it` of the columns' z rows times Gam, to LDS as the operands that they will be;
 //   2  the state's update, and the new state to LDS as the 16-bit operand of the next chunk; Z^T P^T and the output; the next
 //      chunk's three score tiles, one each in three waves, to LDS as operands.
-// So what one half needs of another wave is formed early in the half before it, and loads have three chunks' time.
+// So what one half needs of another wave is formed in the half before it, and loads are under way for a chunk's time.
+//
+// A chunk of a role takes 2.3 us with a few workgroups on the device, the latency of its dependent steps (LDS operands and matrix
+// instructions, two waves a SIMD); with 192, 2.7, where memory shows: B4 H16 N4096 bf16 alone reading 74 us, alone storing 58,
+// both 137, alone computing 150, all 179.  Tried: four waves, three buffers and one barrier a chunk 184 to 205 us; loads two
+// chunks ahead, no change; outputs held back and stored as whole rows through LDS 180.  Stores are cached: 32-byte pieces of
+// rows that go past the cache take 1.8 times as long.
 //
 // A tile's rows are unpadded; 16-byte piece p of row r sits at piece p ^ turn(r).  Reads of one piece of 16 rows (operands
 // along a row) and transposing reads of four rows and four pieces meet every bank once.

@@ -5,7 +5,9 @@
 //     O_t     = ((X_t Y_t^T) .* D) Z_t + Lam (X_t S_t)       D[i][j] = gamma^(i-j), i >= j
 //     S_{t+1} = gamma^L S_t + (Gam Y_t)^T Z_t
 //
-// Bound by the matrix instructions: at width 128 a chunk of a role is 20 MFLOP.  Wave w owns 16 columns of O and S; the ten
+// Bound by the matrix instructions: at width 128 a chunk of a role is 5.5 MFLOP, 9 us of one compute unit's rate, and takes 11.8
+// (76 %): the barriers and the first operands of each product.  B2 H8 N2047 d128 with states: pre-pass, scan and walk 31, 12 and
+// 116 us.  Wave w owns 16 columns of O and S; the ten
 // 16 x 16 score tiles on and below the diagonal are each formed once a workgroup and handed on through LDS.
 //
 // MFMA conventions (16x16x4 fp32): an A (B) operand is one float per lane: lane l holds row (column) l%16 and contraction

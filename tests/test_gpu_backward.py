@@ -217,3 +217,65 @@ def test_gradients_by_a_function_of_the_callers(leet):
     bounds = [b for _, b in forms.attention_backward(*wide(do, q, k, v), gamma.double())]
     for a, w, b in zip(got, want, bounds):
         held("gradient", a, (w, b))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("segments", [0, 1])
+def test_more_sequences_than_compute_units(leet, dtype, segments):
+    check(leet, 9, 10, 130, 128, 128, dtype, decays(10), segments=segments)
+    check(leet, 9, 10, 64, 128, 128, dtype, None, segments=segments, states=False)
+
+
+def test_offsets_beyond_two_to_the_31_in_one_segment(leet):
+    B, H, N, d = 1, 36, 500000, 128   # 2.3e9 elements a tensor
+    g = torch.Generator(device="cuda").manual_seed(2)
+    q, k, v, do = (torch.randn((B, H, N, d), generator=g, device="cuda", dtype=torch.bfloat16).mul_(0.1) for _ in range(4))
+    gamma = decays(H).cuda()
+    got = leet.leet_attn_backward(do, q, k, v, gamma, segments=1)
+    for h in (0, H - 1):
+        alone = leet.leet_attn_backward(*(t[:, h:h + 1].clone() for t in (do, q, k, v)), gamma[h:h + 1].clone(), segments=1)
+        assert all(torch.equal(a[:, h:h + 1], b) for a, b in zip(got, alone))
+
+
+@pytest.mark.parametrize("dtype,d,dv", [(BF16, 128, 128), (F16, 64, 64), (BF16, 128, 256), (F32, 128, 128)])
+def test_calls_repeat_eager_on_streams_and_replayed(leet, dtype, d, dv):
+    """The plan is the library's own; every replay is compared with an eager call on the same inputs."""
+    sets = [on(*inputs(2, 4, 900, d, dv, dtype, True, seed)) for seed in (1, 2)]
+    gamma = decays(4).cuda()
+
+    def call(t):
+        return leet.leet_attn_backward(*t[:4], gamma, state_in=t[4], dstate_out=t[5])
+
+    want = [call(t) for t in sets]
+    torch.cuda.synchronize()
+    got = []
+    for t in sets:
+        with torch.cuda.stream(torch.cuda.Stream()):
+            got.append(call(t))
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for a, b in zip(want, got) for x, y in zip(a, b))
+    graphs, kept = [], []
+    for t in sets:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            kept.append(call(t))
+    for _ in range(3):
+        for t in sets:
+            t[0].mul_(-0.5)
+        eager = [call(t) for t in sets]
+        for gr in graphs:
+            gr.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for a, b in zip(eager, kept) for x, y in zip(a, b))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_a_value_that_is_not_finite_stays_in_its_sequence(leet, dtype):
+    do, q, k, v, _, _ = on(*inputs(1, 3, 150, 128, 128, dtype, False))
+    gamma = decays(3).cuda()
+    want = leet.leet_attn_backward(do, q, k, v, gamma)
+    v[0, 1, 70, 5] = float("nan")
+    got = leet.leet_attn_backward(do, q, k, v, gamma)
+    for a, b in zip(want, got):
+        assert torch.equal(a[:, 0::2], b[:, 0::2])
+    assert bool(got[0][0, 1, 70:].isnan().all()) and bool(got[1][0, 1, 70].isnan().all())

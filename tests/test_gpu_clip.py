@@ -158,3 +158,17 @@ def test_graph_and_streams(leet):
             g.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(p, q) for a, b in zip(eager, kept) for p, q in zip(a, b))
+
+
+@pytest.mark.parametrize("dtypes", [[F32], [BF16], [F16, F32]])
+def test_sizes_about_a_tile(leet, dtypes):
+    check(leet, tensors([16383, 16385, 32767, 32768, 0, 32769, 16384, 49153], dtypes), 0.7)
+    check(leet, tensors([16383], dtypes), 0.7)
+
+
+def test_unaligned_tensors_past_the_cache(leet):
+    n = 70_000_001   # in, out: 280 MB
+    buf, to = torch.ones(n + 2, device="cuda", dtype=BF16), torch.full((n + 2,), 7.0, device="cuda", dtype=BF16)
+    norm = leet.leet_attn_clip_gradients([buf[1:-1]], n ** 0.5 / 4, outs=[to[1:-1]])
+    assert abs(float(norm) / n ** 0.5 - 1) < 4 * U and bool((buf == 1).all())
+    assert bool((to[1:-1] == 0.25).all()) and float(to[0]) == 7.0 and float(to[-1]) == 7.0
