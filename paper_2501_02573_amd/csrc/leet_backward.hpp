@@ -31,7 +31,7 @@ struct BwdParams {
 // D: width of the rows of x and y, DV of z and out.  fine: the leaving states are wanted to fp32's precision.
 hipError_t launch_bwd_16bit_states(const BwdParams& p, int D, int DV, bool f16, bool fine, hipStream_t stream);
 hipError_t launch_bwd_16bit_walk(const BwdParams& p, int D, int DV, bool f16, bool fine, hipStream_t stream);
-// the same for both widths 128, a compute unit a segment
+// the same for both widths 128, a compute unit a sequence
 hipError_t launch_bwd_16bit_tiles(const BwdParams& p, bool f16, bool fine, hipStream_t stream);
 hipError_t launch_bwd_f32_states(const BwdParams& p, int D, hipStream_t stream);
 hipError_t launch_bwd_f32_walk(const BwdParams& p, int D, hipStream_t stream);

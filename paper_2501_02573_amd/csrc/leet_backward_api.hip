@@ -27,7 +27,7 @@ bool shape_ok(int r, int dv, int dtype) {
 
 struct Plan {
     int nseg, seg_chunks;
-    bool tiles;       // the kernel that takes a compute unit a segment
+    bool tiles;       // the kernel that takes a compute unit a sequence
     size_t ws_bytes;  // states of both directions at the boundaries of segments
 };
 
@@ -90,7 +90,7 @@ bool make_plan(long BH, int N, int r, int dv, int dtype, int segments, Plan* pla
         // 16-bit segments have two chunks at least
         for (int want : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64})
             if (want == 1 || (dtype == LEET_F32 ? want <= nchunks : 2 * want <= nchunks)) consider(want);
-    // The kernel that takes a compute unit a segment: one segment a sequence, no more workgroups than an XCD has compute units.  A
+    // The kernel that takes a compute unit a sequence: no more workgroups than an XCD has compute units.  A
     // chunk takes it 2.3 us in a few workgroups, 2.7 in 192.  us, here against the best of the other: BH 4 N 512 24 26, N 1024 43
     // 30; BH 32 N 1024 43 46, N 2048 83 68; BH 64 N 4096 177 200, N 16384 715 740; BH 85 N 4096 (a second round) 302 270.
     plan->tiles = r == 128 && dv == 128 && dtype != LEET_F32 && 3 * ((BH + 7) / 8) <= 32 &&

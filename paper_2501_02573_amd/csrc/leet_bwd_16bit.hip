@@ -84,10 +84,10 @@ __device__ __forceinline__ void scaled(u32x4 x, f32x4 w0, f32x4 w1, u32x4 (&out)
 }
 
 // The rows of a sequence that hold tokens tok0 .. tok0 + L - 1 of a walk (rows of `width` elements; `seq`: its first row), L = 64
-// or what is left before tok_end, as a buffer: what lies outside it is read as zero and not written, so that loads and stores
+// or what is left of its N, as a buffer: what lies outside it is read as zero and not written, so that loads and stores
 // need no branches, behind which the compiler could no longer count those under way.
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t chunk_rows(const void* seq, int width, bool rev, int N, int tok0, int tok_end) {
-    const int L = max(min(kChunk, tok_end - tok0), 0);
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t chunk_rows(const void* seq, int width, bool rev, int N, int tok0) {
+    const int L = max(min(kChunk, N - tok0), 0);
     const uintptr_t addr = reinterpret_cast<uintptr_t>(seq) + (size_t)(rev ? N - tok0 - L : tok0) * (width * 2);
     // the same in every lane; the compiler is told
     const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)addr), hi = __builtin_amdgcn_readfirstlane((uint32_t)(addr >> 32));
@@ -419,19 +419,13 @@ __global__ __launch_bounds__(D * 4, 2) void tiles16_kernel(BwdParams p) {
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, ln = l & 31, g = l >> 5;
     const int c = w % CT, it = w / CT;
     const int slot = blockIdx.x >> 3, which = slot % p.roles, unit = (slot / p.roles) * 8 + (blockIdx.x & 7);
-    if (unit >= p.BH * p.nseg) return;
+    if (unit >= p.BH) return;
     const BwdRole& role = p.role[which];
     const bool rev = role.reversed != 0;
-    const int bh = unit / p.nseg;
-    const int seg = rev ? p.nseg - 1 - unit % p.nseg : unit % p.nseg;
-    const int h = bh % p.H;
-
-    const int tok_begin = seg * p.seg_chunks * kChunk;
-    const int tok_end = (seg == p.nseg - 1) ? p.N : tok_begin + p.seg_chunks * kChunk;
-    const int nchunks = (tok_end - tok_begin + kChunk - 1) / kChunk;
+    const int nchunks = (p.N + kChunk - 1) / kChunk;
 
     // token t of the walk is row t, or N - 1 - t, of the sequence
-    const size_t seq = (size_t)bh * p.N * D;
+    const size_t seq = (size_t)unit * p.N * D;
     const uint16_t *xb = static_cast<const uint16_t*>(role.x) + seq, *yb = static_cast<const uint16_t*>(role.y) + seq;
     const uint16_t* zb = static_cast<const uint16_t*>(role.z) + seq;
     uint16_t* ob = static_cast<uint16_t*>(role.out) + seq;
@@ -442,9 +436,9 @@ __global__ __launch_bounds__(D * 4, 2) void tiles16_kernel(BwdParams p) {
     } ahead;
     const int j_own = tid / PR, cc = tid % PR;
     auto fetch = [&](int t) {  // zeros behind the last chunk
-        const int tok0 = tok_begin + t * kChunk, shift = max(0, tok0 + kChunk - tok_end);
-        const auto xr = chunk_rows(xb, D, rev, p.N, tok0, tok_end), yr = chunk_rows(yb, D, rev, p.N, tok0, tok_end);
-        const auto zr = chunk_rows(zb, D, rev, p.N, tok0, tok_end);
+        const int tok0 = t * kChunk, shift = max(0, tok0 + kChunk - p.N);
+        const auto xr = chunk_rows(xb, D, rev, p.N, tok0), yr = chunk_rows(yb, D, rev, p.N, tok0);
+        const auto zr = chunk_rows(zb, D, rev, p.N, tok0);
 #pragma unroll
         for (int r = 0; r < LP; ++r) {
             const int off = row_at(r * LR + j_own, D, rev, shift) + cc * 16;
@@ -465,7 +459,7 @@ __global__ __launch_bounds__(D * 4, 2) void tiles16_kernel(BwdParams p) {
     fetch(0);
 
     if (kDecay) {  // fp64 -> fp32 once per workgroup
-        const double gd = (double)p.gamma[h];
+        const double gd = (double)p.gamma[unit % p.H];
         for (int n = tid; n <= kChunk; n += NT) {
             const float v = (float)pow_int(gd, n);
             sm.pw[n] = v;
@@ -482,20 +476,12 @@ __global__ __launch_bounds__(D * 4, 2) void tiles16_kernel(BwdParams p) {
     for (int i = 0; i < HT; ++i)
 #pragma unroll
         for (int r = 0; r < 16; ++r) S[i][r] = 0.0f;
-    if (seg > 0) {
-        const float* src = role.slots + ((size_t)bh * (p.nseg - 1) + seg - 1) * D * D + (size_t)c_own * role.slot_col;
-#pragma unroll
-        for (int i = 0; i < HT; ++i)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) S[i][r] = src[dk_of(i, r) * role.slot_row];
-    }
     if (role.enter) {
-        const float* src = role.enter + (size_t)bh * D * D + (size_t)c_own * role.enter_col;
-        const float left = kDecay ? (float)pow_int((double)p.gamma[h], tok_begin) : 1.0f;
+        const float* src = role.enter + (size_t)unit * D * D + (size_t)c_own * role.enter_col;
 #pragma unroll
         for (int i = 0; i < HT; ++i)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) S[i][r] += left * src[dk_of(i, r) * role.enter_row];
+            for (int r = 0; r < 16; ++r) S[i][r] = src[dk_of(i, r) * role.enter_row];
     }
 
     // Offsets (elements).  Operands along a row: piece 2s + g of row ln; the state's pieces of column ln likewise.
@@ -562,8 +548,8 @@ __global__ __launch_bounds__(D * 4, 2) void tiles16_kernel(BwdParams p) {
     scores(0);
 
     auto chunk = [&](int t, int buf) {
-        const int tok0 = tok_begin + t * kChunk;
-        const int Lc = min(kChunk, tok_end - tok0);
+        const int tok0 = t * kChunk;
+        const int Lc = min(kChunk, p.N - tok0);
         const int shift = kChunk - Lc;  // a ragged last chunk is right-aligned in the tile, rows above are zero
 
         __syncthreads();  // this chunk's scores and state are there, the last chunk's tiles are done with
@@ -639,7 +625,7 @@ __global__ __launch_bounds__(D * 4, 2) void tiles16_kernel(BwdParams p) {
 
         // O^T: lane = token 32it + ln, registers 4q..4q+3 = columns 32c + 8q + 4g + (0..3).  Lanes of the two halves swap
         // words, and a lane has eight neighbouring columns of its row.
-        const auto to = chunk_rows(ob, D, rev, p.N, tok0, tok_end);
+        const auto to = chunk_rows(ob, D, rev, p.N, tok0);
         const int off = row_at(32 * it + ln, D, rev, shift) + (32 * c + 8 * g) * 2;
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
@@ -663,8 +649,8 @@ __global__ __launch_bounds__(D * 4, 2) void tiles16_kernel(BwdParams p) {
     }
     if (t < nchunks) chunk(t, 0);
 
-    if (seg == p.nseg - 1 && role.leave) {
-        float* dst = role.leave + (size_t)bh * D * D;
+    if (role.leave) {
+        float* dst = role.leave + (size_t)unit * D * D;
 #pragma unroll
         for (int i = 0; i < HT; ++i)
 #pragma unroll
@@ -674,7 +660,7 @@ __global__ __launch_bounds__(D * 4, 2) void tiles16_kernel(BwdParams p) {
 
 template <typename E>
 static hipError_t launch_tiles(const BwdParams& p, bool fine, hipStream_t stream) {
-    const dim3 grid((p.BH * p.nseg + 7) / 8 * 8 * p.roles), block(512);
+    const dim3 grid((p.BH + 7) / 8 * 8 * p.roles), block(512);
     if (!p.gamma) hipLaunchKernelGGL((tiles16_kernel<128, E, false, 1>), grid, block, 0, stream, p);
     else if (fine) hipLaunchKernelGGL((tiles16_kernel<128, E, true, 3>), grid, block, 0, stream, p);
     else hipLaunchKernelGGL((tiles16_kernel<128, E, true, 2>), grid, block, 0, stream, p);
