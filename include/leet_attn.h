@@ -345,8 +345,8 @@ int leet_attn_query_plan_rd(int B, int H, int N, int r, int dv, int dtype, int s
  *                always the caller's, so calls on several streams and captured graphs share nothing.  Scratch
  *   segments     as for leet_attn_forward_ex
  * Shapes as for leet_attn_forward_rd, `dtype` any leet_dtype, `mask` a leet_mask (gamma may be NULL for LEET_MASK_CAUSAL).
- * Inside, scores and, as operands of products, states are rounded to the input type, as in the forward pass; states are
- * carried in fp32, and dstate_in is exact to fp32's products.  In fp16 scores and states beyond 65504 are infinite.  A value
+ * Inside, scores and, as operands of products, states are rounded to the input type, as in the forward pass (of at most 128
+ * tokens to twice its bits); states are carried in fp32, and dstate_in is exact to fp32's products.  In fp16 scores and states beyond 65504 are infinite.  A value
  * that is not finite may make all gradients of its sequence so.
  * Outputs and workspace that share memory with one another or with an input are LEET_ERR_INVALID_ARG.  N = 0 is legal and
  * hands the state's gradient on.

@@ -93,7 +93,8 @@ bool make_plan(long BH, int N, int r, int dv, int dtype, int segments, Plan* pla
     // The kernel that takes a compute unit a sequence: no more workgroups than an XCD has compute units.  A
     // chunk takes it 2.3 us in a few workgroups, 2.7 in 192.  us, here against the best of the other: BH 4 N 512 24 26, N 1024 43
     // 30; BH 32 N 1024 43 46, N 2048 83 68; BH 64 N 4096 177 200, N 16384 715 740; BH 85 N 4096 (a second round) 302 270.
-    plan->tiles = r == 128 && dv == 128 && dtype != LEET_F32 && 3 * ((BH + 7) / 8) <= 32 &&
+    // (Sequences of one or two chunks go to the other, which takes their scores and states in two terms.)
+    plan->tiles = r == 128 && dv == 128 && dtype != LEET_F32 && nchunks > 2 && 3 * ((BH + 7) / 8) <= 32 &&
                   (segments == 0 ? nchunks * (2.3 + 0.0065 * BH) + 5.0 < best : plan->nseg == 1);
     if (plan->tiles) {
         plan->nseg = 1;

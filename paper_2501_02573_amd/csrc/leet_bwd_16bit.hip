@@ -63,6 +63,16 @@ __device__ __forceinline__ u32x4 pack_half(const f32x16& acc, int h) {
     return r;
 }
 
+// what pack_half rounded off, as a 16-bit operand of its own
+template <typename E>
+__device__ __forceinline__ u32x4 pack_rest(const f32x16& acc, u32x4 packed, int h) {
+    u32x4 r;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        r[e] = E::pack2(acc[8 * h + 2 * e] - E::lo(packed[e]), acc[8 * h + 2 * e + 1] - E::hi(packed[e]));
+    return r;
+}
+
 // Eight 16-bit values times eight fp32 weights as kTerms 16-bit values that add up to the product.  What is left for the next
 // term is taken from the packed word itself: the compiler may form the fp16 of a product in two ways, once from the product
 // rounded to fp32 and once not, and the two differ now and then by a step.
@@ -106,7 +116,11 @@ __device__ __forceinline__ constexpr int tile_it(int n) { return n == 0 ? 0 : 1;
 // kTerms: of Gam Z, whose rounding to one would be as large as the outputs' own (two: the outputs' error falls from 1.65 to 1.4
 // times that of outputs that are rounded alone; B4 H16 N4096 d128 bf16 155 -> 173 us).  Three give a leaving state to fp32's
 // precision.
-template <int D, int DV, bool kOut, typename E, bool kDecay, int kTerms>
+// kFew: scores and states, rounded to 16 bits as operands elsewhere, are taken in two terms; sequences of one or two chunks.  Over
+// a few tokens their errors do not average out (an output is one or two products), and one token's gradients were off by up to
+// 2.5 times what outputs that are rounded alone are.  From 128 tokens on one term makes it 1.42 to 1.45 times.  Takes 12 to 18 %
+// longer (B16 H32 N128 bf16: d 64 18.8 -> 22.1 us, d 128 38.0 -> 44.2).
+template <int D, int DV, bool kOut, typename E, bool kDecay, int kTerms, bool kFew>
 __global__ __launch_bounds__(DV * 2, D > 128 || DV > 128 ? 1 : 2) void walk16_kernel(BwdParams p) {
     constexpr int NT = DV * 2;   // threads: one wave per 32 columns of z and out
     constexpr int NW = DV / 32;  // waves
@@ -254,6 +268,7 @@ __global__ __launch_bounds__(DV * 2, D > 128 || DV > 128 ? 1 : 2) void walk16_ke
         if (t + 1 < nchunks) prefetch(tok0 + kChunk);  // in flight during the MFMA work below
 
         f32x16 o[2];
+        u32x4 rest[kFew ? (3 + NW - 1) / NW : 1][2];
         if (kOut) {
             // P^T = Y X^T, masked, for the score tiles this wave produces
 #pragma unroll
@@ -271,8 +286,12 @@ __global__ __launch_bounds__(DV * 2, D > 128 || DV > 128 ? 1 : 2) void walk16_ke
 #pragma unroll
                     for (int r = 0; r < 16; ++r) acc[r] *= wt[r];
                 }
-                sm.pfrag[n][0][l] = pack_half<E>(acc, 0);
-                sm.pfrag[n][1][l] = pack_half<E>(acc, 1);
+#pragma unroll
+                for (int hh = 0; hh < 2; ++hh) {
+                    const u32x4 packed = pack_half<E>(acc, hh);
+                    sm.pfrag[n][hh][l] = packed;
+                    if (kFew) rest[n / NW][hh] = pack_rest<E>(acc, packed, hh);
+                }
             }
 
             // O^T = S^T X^T, rows of O scaled by Lam
@@ -288,8 +307,13 @@ __global__ __launch_bounds__(DV * 2, D > 128 || DV > 128 ? 1 : 2) void walk16_ke
 #pragma unroll
             for (int s = 0; s < D / 16; ++s) {
                 const u32x4 sa = pack_half<E>(S[s >> 1], s & 1);
+                const u32x4 sb = kFew ? pack_rest<E>(S[s >> 1], sa, s & 1) : sa;
 #pragma unroll
-                for (int it = 0; it < 2; ++it) o[it] = E::mfma32(sa, frag16(x_row + 32 * it * RS + 16 * s), o[it]);
+                for (int it = 0; it < 2; ++it) {
+                    const u32x4 xf = frag16(x_row + 32 * it * RS + 16 * s);
+                    o[it] = E::mfma32(sa, xf, o[it]);
+                    if (kFew) o[it] = E::mfma32(sb, xf, o[it]);
+                }
             }
             if (kDecay) {
 #pragma unroll
@@ -312,6 +336,21 @@ __global__ __launch_bounds__(DV * 2, D > 128 || DV > 128 ? 1 : 2) void walk16_ke
 #pragma unroll
                 for (int hh = 0; hh < 2; ++hh)
                     o[tile_it(n)] = E::mfma32(zf[2 * tile_jt(n) + hh], sm.pfrag[n][hh][l], o[tile_it(n)]);
+            if (kFew) {  // the same with what the scores were rounded by
+                __syncthreads();
+#pragma unroll
+                for (int n = 0; n < 3; ++n) {
+                    if (n % NW != w) continue;
+#pragma unroll
+                    for (int hh = 0; hh < 2; ++hh) sm.pfrag[n][hh][l] = rest[n / NW][hh];
+                }
+                __syncthreads();
+#pragma unroll
+                for (int n = 0; n < 3; ++n)
+#pragma unroll
+                    for (int hh = 0; hh < 2; ++hh)
+                        o[tile_it(n)] = E::mfma32(zf[2 * tile_jt(n) + hh], sm.pfrag[n][hh][l], o[tile_it(n)]);
+            }
 
             // O^T: lane = token 32it + ln, registers 4q..4q+3 = columns 32w + 8q + 4g + (0..3).  Through a wave-private LDS
             // tile so that a store covers whole 64-byte row pieces: lane -> (row l/4, 16 bytes l%4).
@@ -671,9 +710,17 @@ template <int D, int DV, bool kOut, typename E, bool kDecay>
 static void launch_terms(const BwdParams& p, bool fine, hipStream_t stream) {
     const int units = p.BH * (kOut ? p.nseg : p.nseg - 1);
     const dim3 grid((units + 7) / 8 * 8 * p.roles), block(DV * 2);
-    if constexpr (!kDecay) hipLaunchKernelGGL((walk16_kernel<D, DV, kOut, E, false, 1>), grid, block, 0, stream, p);
-    else if (fine) hipLaunchKernelGGL((walk16_kernel<D, DV, kOut, E, true, 3>), grid, block, 0, stream, p);
-    else hipLaunchKernelGGL((walk16_kernel<D, DV, kOut, E, true, 2>), grid, block, 0, stream, p);
+    if constexpr (kOut) {
+        if (p.N <= 2 * kChunk) {
+            if constexpr (!kDecay) hipLaunchKernelGGL((walk16_kernel<D, DV, true, E, false, 1, true>), grid, block, 0, stream, p);
+            else if (fine) hipLaunchKernelGGL((walk16_kernel<D, DV, true, E, true, 3, true>), grid, block, 0, stream, p);
+            else hipLaunchKernelGGL((walk16_kernel<D, DV, true, E, true, 2, true>), grid, block, 0, stream, p);
+            return;
+        }
+    }
+    if constexpr (!kDecay) hipLaunchKernelGGL((walk16_kernel<D, DV, kOut, E, false, 1, false>), grid, block, 0, stream, p);
+    else if (fine) hipLaunchKernelGGL((walk16_kernel<D, DV, kOut, E, true, 3, false>), grid, block, 0, stream, p);
+    else hipLaunchKernelGGL((walk16_kernel<D, DV, kOut, E, true, 2, false>), grid, block, 0, stream, p);
 }
 
 template <int D, int DV, bool kOut>

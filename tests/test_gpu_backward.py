@@ -279,3 +279,18 @@ def test_a_value_that_is_not_finite_stays_in_its_sequence(leet, dtype):
     for a, b in zip(want, got):
         assert torch.equal(a[:, 0::2], b[:, 0::2])
     assert bool(got[0][0, 1, 70:].isnan().all()) and bool(got[1][0, 1, 70].isnan().all())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("d,dv", [(64, 64), (128, 128), (128, 256)])
+def test_a_few_tokens_lose_nothing_but_the_outputs_rounding(leet, dtype, d, dv):
+    for N in (1, 2, 3, 17, 64, 65, 128):
+        do, q, k, v, s, ds = inputs(1, 2, N, d, dv, dtype, N % 2 == 1, N)
+        gamma = decays(2)
+        got = leet.leet_attn_backward(*on(do, q, k, v, gamma), state_in=on(s)[0], dstate_out=on(ds)[0])
+        want = forms.attention_backward(*wide(do, q, k, v), gamma.double(), *wide(s, ds), dtype=dtype)
+        for a, (b, _) in zip(got, want):
+            # operands in two terms are off by eps^2 / 4 (fp16: by half of its least number, 2^-25, where values are some 2^-9
+            # or more, a sixteenth of eps / 2); all else is the one rounding at the store, a tenth of it let through
+            alone = float((b.to(dtype).double() - b).norm())
+            assert float((a.double().cpu() - b).norm()) <= 1.1 * alone, N
