@@ -359,7 +359,8 @@ size_t leet_attn_backward_workspace_bytes(int B, int H, int N, int r, int dv, in
 
 /* ------------------------------------------------------------------------------------------------
  * Operators beside the attention: what makes its queries and keys (position rotation, norms of each
- * head), and the element-wise recurrence with a decay of its own for every token and channel.
+ * head), the element-wise recurrence with a decay of its own for every token and channel, norms of a
+ * residual stream, and the clipping of a model's gradients.
  * Of the conventions above these differ: tensors may have strides (in ELEMENTS; the elements of a
  * head row, or the channels of a token row, are adjacent), pointers need only their element's
  * alignment, and a workspace, where one is needed, is always the caller's, so that calls on several

@@ -970,8 +970,8 @@ def leet_attn_qk_norm_rope_backward(dout_q: torch.Tensor, dout_k: torch.Tensor, 
                                     dq_weight: Optional[torch.Tensor] = None, dk_weight: Optional[torch.Tensor] = None,
                                     workspace: Optional[torch.Tensor] = None):
     """Gradients of ``leet_attn_qk_norm_rope``: (dx_q, dx_k, dq_weight, dk_weight) from those of its outputs and its
-    inputs.  A weight that is None has the gradient None.  The attention here has no backward pass: where its q and k
-    are what was normed, their gradients come from the caller's own."""
+    inputs.  A weight that is None has the gradient None.  (Those of q and k come from ``leet_attn_backward`` where the
+    attention reads what was normed.)"""
     B, Hq, Hk, N, d = _heads_pair(q, k, "leet_attn_qk_norm_rope_backward")
     weight_dtype = _weights(q, q_weight, k_weight, d)
     grads = []

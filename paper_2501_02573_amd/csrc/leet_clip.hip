@@ -4,7 +4,8 @@
 //
 // Bound by memory: the gradients are read for the norm and, once it is known, read again and written.  Two launches for up to 64
 // tensors, whose addresses travel as kernel arguments; each workgroup of the second adds up the first one's sums by itself.  The
-// second launch goes through the tensors from the last to the first, whose end the last-level cache still holds.
+// second launch goes through the tensors from the last to the first, whose end the last-level cache still holds.  453 MB of bf16
+// into buffers of their own: 80 and 153 us, 5.7 and 5.9 TB/s; twenty small tensors 5 and 8 us.
 // Squares are added in fp64, which neither overflows nor loses the small ones, each workgroup's in an order of its own that
 // does not depend on timing.
 #include "leet_clip.hpp"
@@ -40,7 +41,7 @@ __device__ __forceinline__ int tensor_of(const ClipParams& p, int tile) {
 template <int kElem>
 struct Tile {
     static constexpr int kBytes = Io<kElem>::kBytes, kWords = kElem == 0 ? 2 : 1;
-    using Word = typename std::conditional<kElem == 0, u32x4, u32x4>::type;
+    using Word = typename std::conditional<kElem == 0, u32x4, u32x4>::type;  // a dependent type, for an alignment that is one
     typedef Word Anywhere __attribute__((aligned(kBytes), may_alias));
     Word word[kClipPieces][kWords];
 
