@@ -1258,12 +1258,17 @@ def leet_attn_clip_gradients(grads, limit: Optional[float] = None, outs=None, no
     """Norm over all tensors of ``grads`` together, and the tensors times min(1, limit / norm): in place, or into ``outs``
     (tensors of the same sizes and types).  Returns the norm, float32 [1] on their device; without a ``limit`` that is all.
 
-    All tensors must be dense (any order of dimensions, an output the same one).  A norm that is not finite clips nothing."""
+    All tensors must be dense (any order of dimensions, an output the same one).  A norm that is not finite clips nothing.
+    A limit is a float32 number; one that no norm of such tensors reaches, 2^160 or more, is none."""
     grads = list(grads)
     if not grads:
         raise ValueError("no gradients")
-    if outs is not None and (limit is None or limit == float("inf")):
-        raise ValueError("outs without a limit")
+    limit = float("inf") if limit is None or limit >= 2.0 ** 160 else float(limit)
+    if limit == float("inf"):
+        if outs is not None:
+            raise ValueError("outs without a limit")
+    elif ctypes.c_float(limit).value == float("inf"):  # which the library would take as none
+        raise ValueError("limit is beyond float32")
     targets = grads if outs is None else list(outs)
     if len(targets) != len(grads):
         raise ValueError("outs must be as many as grads")
@@ -1285,8 +1290,7 @@ def leet_attn_clip_gradients(grads, limit: Optional[float] = None, outs=None, no
     elif norm.dtype != torch.float32 or norm.numel() != 1:
         raise ValueError("norm must be one float32")
     ws, ws_bytes, keep = _scratch(clip_gradients_workspace_bytes() if workspace is None else 0, workspace, dev)
-    st = _call_on(dev, lib.leet_attn_clip_gradients, b"".join(packed), len(grads), float("inf") if limit is None else limit,
-                  _ptr(norm), ws, ws_bytes)
+    st = _call_on(dev, lib.leet_attn_clip_gradients, b"".join(packed), len(grads), limit, _ptr(norm), ws, ws_bytes)
     if st != LEET_OK:
         raise LeetAttnError(st, "leet_attn_clip_gradients")
     return norm
