@@ -410,7 +410,7 @@ __global__ __launch_bounds__(DV * 2, D > 128 || DV > 128 ? 1 : 2) void walk16_ke
     }
 }
 
-// ---- both widths alike: a wave for each 32 x 32 tile of the outputs ----
+// ---- both widths 128: a wave for each 32 x 32 tile of the outputs ----
 //
 // What bounds a walk that has a compute unit to itself is the time that one chunk takes after the other, so here twice as many
 // waves share it, two a SIMD: wave (c, it) forms O^T[32 columns c][32 rows it] and carries the half `it` of the state's rows
@@ -429,13 +429,10 @@ __global__ __launch_bounds__(DV * 2, D > 128 || DV > 128 ? 1 : 2) void walk16_ke
 //
 // A tile's rows are unpadded; 16-byte piece p of row r sits at piece p ^ turn(r).  Reads of one piece of 16 rows (operands
 // along a row) and transposing reads of four rows and four pieces meet every bank once.
-template <int PR>
-__device__ __forceinline__ constexpr int turn(int row) {
-    return PR == 16 ? 4 * (row & 3) + ((row >> 2) & 3) : 4 * ((row >> 1) & 1) + ((row >> 2) & 3);
-}
+__device__ __forceinline__ constexpr int turn(int row) { return 4 * (row & 3) + ((row >> 2) & 3); }
 
-template <int D>
 struct SmemTiles {
+    static constexpr int D = 128;
     uint16_t x[2][kChunk * D], y[2][kChunk * D], z[2][kChunk * D];
     uint16_t st[D * D];               // S^T[c][dk], turned as the tiles are
     u32x4 pfrag[2][3][2][64];         // masked score tiles as B operands: [buffer][tile][register half][lane]
@@ -444,15 +441,16 @@ struct SmemTiles {
     float gw[kChunk];                 // Gam
 };
 
-template <int D, typename E, bool kDecay, int kTerms>
-__global__ __launch_bounds__(D * 4, 2) void tiles16_kernel(BwdParams p) {
+template <typename E, bool kDecay, int kTerms>
+__global__ __launch_bounds__(SmemTiles::D * 4, 2) void tiles16_kernel(BwdParams p) {
+    constexpr int D = SmemTiles::D;
     constexpr int NT = D * 4;         // threads
     constexpr int CT = D / 32;        // column tiles
     constexpr int HT = D / 64;        // 32-row tiles of the state that a wave carries
     constexpr int PR = D / 8;         // 16-byte pieces per row
     constexpr int LP = kChunk * PR / NT;  // pieces per thread per tensor per chunk (= 2)
     constexpr int LR = NT / PR;           // rows apart (= 32)
-    __shared__ __attribute__((aligned(16))) SmemTiles<D> sm;
+    __shared__ __attribute__((aligned(16))) SmemTiles sm;
 
     const int tid = threadIdx.x;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, ln = l & 31, g = l >> 5;
@@ -486,7 +484,7 @@ __global__ __launch_bounds__(D * 4, 2) void tiles16_kernel(BwdParams p) {
             ahead.z[r] = __builtin_amdgcn_raw_buffer_load_b128(zr, off, 0, 0);
         }
     };
-    const int to_own = (j_own * PR + (cc ^ turn<PR>(j_own))) * 8;
+    const int to_own = (j_own * PR + (cc ^ turn(j_own))) * 8;
     auto put = [&](const Ahead& a, int buf) {
 #pragma unroll
         for (int r = 0; r < LP; ++r) {
@@ -526,13 +524,13 @@ __global__ __launch_bounds__(D * 4, 2) void tiles16_kernel(BwdParams p) {
     // Offsets (elements).  Operands along a row: piece 2s + g of row ln; the state's pieces of column ln likewise.
     int at_row[D / 16];
 #pragma unroll
-    for (int s = 0; s < D / 16; ++s) at_row[s] = ln * D + (((2 * s) ^ g ^ turn<PR>(ln)) * 8);
+    for (int s = 0; s < D / 16; ++s) at_row[s] = ln * D + (((2 * s) ^ g ^ turn(ln)) * 8);
     // Transposing reads: row 4g + s16/4 (+ 8 rd + 16 f), four columns.  Eight rows on, a row's turn differs by 2.
     const int s16 = l & 15, half = (l >> 4) & 1, r_tr = 4 * g + (s16 >> 2);
     int z_tr[2], y_tr[HT][2];
 #pragma unroll
     for (int rd = 0; rd < 2; ++rd) {
-        const int t = turn<PR>(r_tr + 8 * rd), at = (r_tr + 8 * rd) * D;
+        const int t = turn(r_tr + 8 * rd), at = (r_tr + 8 * rd) * D;
         z_tr[rd] = at + ((4 * c + 2 * half + ((s16 >> 1) & 1)) ^ t) * 8 + 4 * (s16 & 1);
 #pragma unroll
         for (int i = 0; i < HT; ++i) y_tr[i][rd] = at + ((4 * (HT * it + i) + 2 * half + (s16 & 1)) ^ t) * 8 + 4 * ((s16 >> 1) & 1);
@@ -545,7 +543,7 @@ __global__ __launch_bounds__(D * 4, 2) void tiles16_kernel(BwdParams p) {
             for (int hh = 0; hh < 2; ++hh) {
                 // eight consecutive dk, piece 2 (2 tile + hh) + g of the column
                 const int s2 = 2 * (2 * (HT * it + i) + hh);
-                *reinterpret_cast<u32x4*>(&sm.st[32 * c * D + ln * D + ((s2 ^ g ^ turn<PR>(ln)) * 8)]) = pack_half<E>(S[i], hh);
+                *reinterpret_cast<u32x4*>(&sm.st[32 * c * D + ln * D + ((s2 ^ g ^ turn(ln)) * 8)]) = pack_half<E>(S[i], hh);
             }
     };
     publish();
@@ -556,8 +554,7 @@ __global__ __launch_bounds__(D * 4, 2) void tiles16_kernel(BwdParams p) {
     // The score tile that this wave forms, if any: 0 = (jt 0, it 0), 1 = (1, 1), 2 = (0, 1), by waves of its rows on SIMDs of
     // their own.  Decay weights: on the diagonal i - j = ln - jr (zero above it), below it 32 + ln - jr.
     const int later = rev ? 0 : 1;
-    constexpr bool kOneEach = CT > 2;
-    const int tile = kOneEach ? (it == 0 ? (c == 0 ? 0 : -1) : c == 1 ? 1 : c == 2 ? 2 : -1) : it == 0 ? (c == 0 ? 0 : -1) : c == 0 ? 1 : 2;
+    const int tile = it == 0 ? (c == 0 ? 0 : -1) : c == 1 ? 1 : c == 2 ? 2 : -1;
     f32x16 wgt;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
@@ -699,10 +696,10 @@ __global__ __launch_bounds__(D * 4, 2) void tiles16_kernel(BwdParams p) {
 
 template <typename E>
 static hipError_t launch_tiles(const BwdParams& p, bool fine, hipStream_t stream) {
-    const dim3 grid((p.BH + 7) / 8 * 8 * p.roles), block(512);
-    if (!p.gamma) hipLaunchKernelGGL((tiles16_kernel<128, E, false, 1>), grid, block, 0, stream, p);
-    else if (fine) hipLaunchKernelGGL((tiles16_kernel<128, E, true, 3>), grid, block, 0, stream, p);
-    else hipLaunchKernelGGL((tiles16_kernel<128, E, true, 2>), grid, block, 0, stream, p);
+    const dim3 grid((p.BH + 7) / 8 * 8 * p.roles), block(SmemTiles::D * 4);
+    if (!p.gamma) hipLaunchKernelGGL((tiles16_kernel<E, false, 1>), grid, block, 0, stream, p);
+    else if (fine) hipLaunchKernelGGL((tiles16_kernel<E, true, 3>), grid, block, 0, stream, p);
+    else hipLaunchKernelGGL((tiles16_kernel<E, true, 2>), grid, block, 0, stream, p);
     return hipGetLastError();
 }
 
