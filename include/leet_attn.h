@@ -346,8 +346,10 @@ int leet_attn_query_plan_rd(int B, int H, int N, int r, int dv, int dtype, int s
  *   segments     as for leet_attn_forward_ex
  * Shapes as for leet_attn_forward_rd, `dtype` any leet_dtype, `mask` a leet_mask (gamma may be NULL for LEET_MASK_CAUSAL).
  * Inside, scores and, as operands of products, states are rounded to the input type, as in the forward pass (of at most 128
- * tokens to twice its bits); states are carried in fp32, and dstate_in is exact to fp32's products.  In fp16 scores and states beyond 65504 are infinite.  A value
- * that is not finite may make all gradients of its sequence so.
+ * tokens to twice its bits), in fp16 times powers of two that keep them within its range, whatever the inputs' size: gradients
+ * are infinite only where they themselves leave their type.  States are carried in fp32, and dstate_in is exact to fp32's
+ * products (in fp16 to those of a q whose numbers below 2^-14 count as 2^-14).  A value that is not finite may make all
+ * gradients of its sequence so.
  * Outputs and workspace that share memory with one another or with an input are LEET_ERR_INVALID_ARG.  N = 0 is legal and
  * hands the state's gradient on.
  */

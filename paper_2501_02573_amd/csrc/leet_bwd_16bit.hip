@@ -23,6 +23,8 @@
 // Near memory's rate where the device is full: B16 H32 N2048 d128 bf16 takes 582 us, its ten tensors at 4.6 TB/s (with one term 530,
 // 5.1).  Few sequences are bound by a chunk's latency, or by segments' pre-pass, which reads four tensors again.  B4 H16 N4096: 174
 // to 179 us, of which its ten tensors are 131 at 5.1 TB/s; with dstate_in wanted and three terms 207.
+#include <type_traits>
+
 #include "leet_backward.hpp"
 #include "leet_common.hpp"
 
@@ -41,7 +43,102 @@ struct Smem16 {
     u32x4 pfrag[3][2][64];   // masked score tiles as B operands: [tile][register half][lane]
     float pw[kChunk + 4];    // gamma^n, n = 0..64
     float gw[kChunk];        // Gam
+    float back[3][32];       // fp16: what undoes the scaling of a score tile's tokens
+    float gw_held[DV / 32][kChunk];  // fp16: Gam times a wave's scale of z
 };
+
+// fp16's normal numbers reach from 2^-14 to 65504, fp32's values that become its operands lie anywhere: gradients of 2^-18 lost most
+// of their bits below, scores and states of large ones became infinite where every gradient is finite.  So fp16 has powers of two:
+//   * scores are brought to [2^14, 2^15) for each token of a tile as they become operands, and the product back;
+//   * a state is kept times `held`, which Gam carries: the largest z of a chunk is brought to [2^8, 2^9), in three terms to [2^14,
+//     2^15); where the largest of a wave's state then lies outside [4, 2^15) the state itself is brought to [2^14, 2^15).
+// A rounding to one term is 2^-11 of the value, or 2^-25 of a number of that scale: 2^-39 of a token's largest score, 2^-27 of the
+// largest of a state; what is added to a state is off by 2^-33 of the largest z (three terms 2^-39) or 2^-22 of itself (2^-24).
+// The matrix instructions add products of numbers below 2^-14 as if these had that exponent.
+// fp16 takes 7 to 18 % longer by it.  us before and after: B16 H32 N2048 d128 593 650, B4 H16 N4096 d128 180 214, B2 H16 130 136, B4
+// H16 N4096 d64 97 105, B3 H12 N1777 d64 34.7 38.5, B16 H32 N128 d64 25.8 30.4, B2 H16 N2048 128/256 150 164.  (Scaling each state
+// as it becomes an operand, and each column of z by itself: 223 instead of 214.)
+template <typename E>
+constexpr bool kNarrow = std::is_same<E, ElemF16>::value;
+
+// m >= 0: the power of two that brings values of up to m, 2^kLeast at least, to [2^kTo, 2^(kTo + 1)).  Infinities stay infinite.
+template <int kTo, int kLeast>
+__device__ __forceinline__ float power_to(float m) {
+    return __uint_as_float(((254u + kTo) << 23) - max(__float_as_uint(m) & 0x7f800000u, (127u + kLeast) << 23));
+}
+// 1 / x of a power of two
+__device__ __forceinline__ float inverse_of(float x) { return __uint_as_float((254u << 23) - __float_as_uint(x)); }
+// Smaller scores are not brought up further, so that sums of them with what is not small (times 2^60) stay finite: rounded to 2^-85
+// they add 2^-63 to an output at most, whose least number is 2^-24.
+__device__ __forceinline__ float power_of_scores(float m) { return power_to<14, -46>(m); }
+
+__device__ __forceinline__ float most_of(const f32x16& v, float m) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) m = fmaxf(m, fabsf(v[r]));
+    return m;
+}
+// The larger one of lanes l and l ^ 32; numbers >= 0 as their bits, of which NaNs are the largest.
+__device__ __forceinline__ uint32_t most_of_halves(uint32_t m) {
+    const u32x2 both = __builtin_amdgcn_permlane32_swap(m, m, false, false);
+    return max(both[0], both[1]);
+}
+template <int kCtrl>
+__device__ __forceinline__ uint32_t most_dpp(uint32_t m) {
+    return max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, kCtrl, 0xf, 0xf, true));
+}
+// the largest of a wave's lanes, the same in all of them
+__device__ __forceinline__ uint32_t most_of_wave(uint32_t m) {
+    m = most_dpp<0xB1>(m);   // quad_perm 1 0 3 2
+    m = most_dpp<0x4E>(m);   // quad_perm 2 3 0 1
+    m = most_dpp<0x141>(m);  // row_half_mirror
+    m = most_dpp<0x140>(m);  // row_mirror
+    const u32x2 both = __builtin_amdgcn_permlane16_swap(m, m, false, false);
+    return __builtin_amdgcn_readfirstlane(most_of_halves(max(both[0], both[1])));
+}
+// of a score tile's column, a token
+__device__ __forceinline__ float most_of_token(const f32x16& v) {
+    return __uint_as_float(most_of_halves(__float_as_uint(most_of(v, 0.0f))));
+}
+// of all lanes but those that are infinite or NaN: finite columns of a state keep their bits beside others
+__device__ __forceinline__ float most_finite(float m) {
+    return __uint_as_float(most_of_wave(m < __builtin_inff() ? __float_as_uint(m) : 0u));
+}
+// The largest finite one of fp16 values, in a wave: 2^10 more than their bits, where infinities and NaNs wrap to less.
+template <int kCount>
+__device__ __forceinline__ float most_of_rows(const u32x4 (&v)[kCount]) {
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    u16x2 m = {0, 0};
+#pragma unroll
+    for (int f = 0; f < kCount; ++f)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t word = v[f][e];
+            m = __builtin_elementwise_max(m, (__builtin_bit_cast(u16x2, word) + (uint16_t)0x400) & (uint16_t)0x7fff);
+        }
+    const uint32_t most = max(most_of_wave(max(m[0], m[1])), 0x400u) - 0x400u;
+    return (float)__builtin_bit_cast(_Float16, (uint16_t)most);
+}
+// The scale of z in a chunk, no more than leaves a state of up to 2^15 / held finite.
+template <int kTerms>
+__device__ __forceinline__ float power_of_z(float most, float held) {
+    return fminf(power_to<kTerms < 3 ? 8 : 14, -24>(most), 0x1p85f * held);
+}
+// Brings a wave's state, of which it holds `held` times, into fp16's range.
+template <int kTiles>
+__device__ __forceinline__ void keep_in_range(f32x16 (&S)[kTiles], float& held) {
+    float m = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i) m = most_of(S[i], m);
+    m = most_finite(m);
+    if (m >= 0x1p15f || (m < 4.0f && m > 0.0f)) {  // the same in all lanes
+        const float by = fminf(power_to<14, -99>(m), 0x1p100f * inverse_of(held));  // so that `held` stays finite
+        held *= by;
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) S[i][r] *= by;
+    }
+}
 
 __device__ __forceinline__ u32x4 frag16(const uint16_t* p) { return *reinterpret_cast<const u32x4*>(p); }
 
@@ -91,6 +188,14 @@ __device__ __forceinline__ void scaled(u32x4 x, f32x4 w0, f32x4 w1, u32x4 (&out)
             b -= E::hi(word);
         }
     }
+}
+
+// Eight 16-bit values times a power of two
+template <typename E>
+__device__ __forceinline__ u32x4 times_power(u32x4 x, float by) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = E::pack2(E::lo(x[e]) * by, E::hi(x[e]) * by);
+    return x;
 }
 
 // The rows of a sequence that hold tokens tok0 .. tok0 + L - 1 of a walk (rows of `width` elements; `seq`: its first row), L = 64
@@ -165,8 +270,9 @@ __global__ __launch_bounds__(DV * 2, D > 128 || DV > 128 ? 1 : 2) void walk16_ke
         }
     }
 
-    // state slice: S[t][r] = S[dk = 32t + pi(m(r, g))][c = 32w + ln]
+    // state slice: S[t][r] = S[dk = 32t + pi(m(r, g))][c = 32w + ln]; in fp16 times `held`
     f32x16 S[DT];
+    float held = 1.0f;  // the same in all lanes
     const int c_own = 32 * w + ln;
     auto dk_of = [&](int t, int r) {
         // m = 8(r/4) + 4g + r%4 ; pi swaps the 4- and 8-bits: dk = 16(r/8) + 8g + 4((r/4)&1) + r%4
@@ -199,6 +305,7 @@ __global__ __launch_bounds__(DV * 2, D > 128 || DV > 128 ? 1 : 2) void walk16_ke
     // transposing reads: lane supplies row 4g + s16/4 (+ 8*rd + 16*f) and four consecutive columns
     const uint16_t* z_tr = &sm.z[(4 * g + (s16 >> 2)) * RSZ + 32 * w + 16 * half + 4 * (s16 & 3)];
     const uint16_t* y_tr = &sm.y[(4 * g + (s16 >> 2)) * RS + 16 * half + 8 * (s16 & 1) + 4 * ((s16 >> 1) & 1)];
+    float* gw = kNarrow<E> ? sm.gw_held[w] : sm.gw;
 
     __syncthreads();  // tables visible
 
@@ -268,6 +375,7 @@ __global__ __launch_bounds__(DV * 2, D > 128 || DV > 128 ? 1 : 2) void walk16_ke
         if (t + 1 < nchunks) prefetch(tok0 + kChunk);  // in flight during the MFMA work below
 
         f32x16 o[2];
+        float lam[2];
         u32x4 rest[kFew ? (3 + NW - 1) / NW : 1][2];
         if (kOut) {
             // P^T = Y X^T, masked, for the score tiles this wave produces
@@ -286,6 +394,12 @@ __global__ __launch_bounds__(DV * 2, D > 128 || DV > 128 ? 1 : 2) void walk16_ke
 #pragma unroll
                     for (int r = 0; r < 16; ++r) acc[r] *= wt[r];
                 }
+                if (kNarrow<E>) {
+                    const float up = power_of_scores(most_of_token(acc));
+                    sm.back[n][ln] = inverse_of(up);
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) acc[r] *= up;
+                }
 #pragma unroll
                 for (int hh = 0; hh < 2; ++hh) {
                     const u32x4 packed = pack_half<E>(acc, hh);
@@ -295,7 +409,8 @@ __global__ __launch_bounds__(DV * 2, D > 128 || DV > 128 ? 1 : 2) void walk16_ke
             }
 
             // O^T = S^T X^T, rows of O scaled by Lam
-            float lam[2] = {lam_full[0], lam_full[1]};
+            lam[0] = lam_full[0];
+            lam[1] = lam_full[1];
             if (kDecay && shift) {
                 lam[0] = sm.pw[max(ln + later - shift, 0)];
                 lam[1] = sm.pw[max(32 + ln + later - shift, 0)];
@@ -304,6 +419,11 @@ __global__ __launch_bounds__(DV * 2, D > 128 || DV > 128 ? 1 : 2) void walk16_ke
             for (int it = 0; it < 2; ++it)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) o[it][r] = 0.0f;
+            if constexpr (kNarrow<E>) {
+                keep_in_range(S, held);
+                lam[0] *= inverse_of(held);
+                lam[1] *= inverse_of(held);
+            }
 #pragma unroll
             for (int s = 0; s < D / 16; ++s) {
                 const u32x4 sa = pack_half<E>(S[s >> 1], s & 1);
@@ -315,7 +435,7 @@ __global__ __launch_bounds__(DV * 2, D > 128 || DV > 128 ? 1 : 2) void walk16_ke
                     if (kFew) o[it] = E::mfma32(sb, xf, o[it]);
                 }
             }
-            if (kDecay) {
+            if (kDecay && !kNarrow<E>) {
 #pragma unroll
                 for (int it = 0; it < 2; ++it)
 #pragma unroll
@@ -331,11 +451,31 @@ __global__ __launch_bounds__(DV * 2, D > 128 || DV > 128 ? 1 : 2) void walk16_ke
         if (kOut) {
             __syncthreads();  // score fragments visible; the z tile is dead: its fragments are in registers
             // O^T += Z^T P^T over the tiles (jt <= it)
+            // (fp16: the sums are brought to a tile's scale before it and, behind the last, back)
+            auto add_tiles = [&](float first0, float first1) {
+                float to[2] = {first0, first1};
 #pragma unroll
-            for (int n = 0; n < 3; ++n)
+                for (int n = 0; n < 3; ++n) {
+                    f32x16& sum = o[tile_it(n)];
+                    if (kNarrow<E>) {
+                        const float down = sm.back[n][ln];
+                        // (sums that this limit leaves too small are far beyond 65504 all the same; it keeps zeros from becoming NaN)
+                        const float by = fminf(to[tile_it(n)] * inverse_of(down), 0x1p127f);
+                        to[tile_it(n)] = down;
 #pragma unroll
-                for (int hh = 0; hh < 2; ++hh)
-                    o[tile_it(n)] = E::mfma32(zf[2 * tile_jt(n) + hh], sm.pfrag[n][hh][l], o[tile_it(n)]);
+                        for (int r = 0; r < 16; ++r) sum[r] *= by;
+                    }
+#pragma unroll
+                    for (int hh = 0; hh < 2; ++hh) sum = E::mfma32(zf[2 * tile_jt(n) + hh], sm.pfrag[n][hh][l], sum);
+                }
+                if (kNarrow<E>) {
+#pragma unroll
+                    for (int it = 0; it < 2; ++it)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) o[it][r] *= to[it];
+                }
+            };
+            add_tiles(lam[0], lam[1]);
             if (kFew) {  // the same with what the scores were rounded by
                 __syncthreads();
 #pragma unroll
@@ -345,11 +485,7 @@ __global__ __launch_bounds__(DV * 2, D > 128 || DV > 128 ? 1 : 2) void walk16_ke
                     for (int hh = 0; hh < 2; ++hh) sm.pfrag[n][hh][l] = rest[n / NW][hh];
                 }
                 __syncthreads();
-#pragma unroll
-                for (int n = 0; n < 3; ++n)
-#pragma unroll
-                    for (int hh = 0; hh < 2; ++hh)
-                        o[tile_it(n)] = E::mfma32(zf[2 * tile_jt(n) + hh], sm.pfrag[n][hh][l], o[tile_it(n)]);
+                add_tiles(1.0f, 1.0f);
             }
 
             // O^T: lane = token 32it + ln, registers 4q..4q+3 = columns 32w + 8q + 4g + (0..3).  Through a wave-private LDS
@@ -375,8 +511,14 @@ __global__ __launch_bounds__(DV * 2, D > 128 || DV > 128 ? 1 : 2) void walk16_ke
         }
 
         // S = gamma^L S + Y^T (Gam Z)
-        if (kDecay) {
-            const float gl = sm.pw[Lc];
+        if (kDecay || kNarrow<E>) {
+            float gl = kDecay ? sm.pw[Lc] : 1.0f;
+            if constexpr (kNarrow<E>) {
+                const float next = power_of_z<kTerms>(most_of_rows(zf), kOut ? held : 1.0f);
+                gl *= next * inverse_of(held);
+                held = next;
+                if (kDecay) gw[l] = sm.gw[l] * held;  // read by this wave alone
+            }
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
@@ -386,8 +528,9 @@ __global__ __launch_bounds__(DV * 2, D > 128 || DV > 128 ? 1 : 2) void walk16_ke
         for (int f = 0; f < 4; ++f) {
             u32x4 zs[kTerms];
             if (kDecay)
-                scaled<E, kTerms>(zf[f], *reinterpret_cast<const f32x4*>(&sm.gw[16 * f + 4 * g]),
-                                  *reinterpret_cast<const f32x4*>(&sm.gw[16 * f + 8 + 4 * g]), zs);
+                scaled<E, kTerms>(zf[f], *reinterpret_cast<const f32x4*>(&gw[16 * f + 4 * g]),
+                                  *reinterpret_cast<const f32x4*>(&gw[16 * f + 8 + 4 * g]), zs);
+            else if (kNarrow<E>) zs[0] = times_power<E>(zf[f], held);
             else zs[0] = zf[f];
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt) {
@@ -403,10 +546,11 @@ __global__ __launch_bounds__(DV * 2, D > 128 || DV > 128 ? 1 : 2) void walk16_ke
     if (!kOut) dst = role.slots + ((size_t)bh * (p.nseg - 1) + seg) * D * DV;
     else if (seg == p.nseg - 1 && role.leave) dst = role.leave + (size_t)bh * D * DV;
     if (dst) {
+        const float real = kNarrow<E> ? inverse_of(held) : 1.0f;
 #pragma unroll
         for (int t = 0; t < DT; ++t)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) dst[dk_of(t, r) * DV + c_own] = S[t][r];
+            for (int r = 0; r < 16; ++r) dst[dk_of(t, r) * DV + c_own] = kNarrow<E> ? S[t][r] * real : S[t][r];
     }
 }
 
@@ -440,6 +584,14 @@ struct SmemTiles {
     float pw[kChunk + 4];             // gamma^n, n = 0..64
     float gw[kChunk];                 // Gam
 };
+// fp16 has also
+struct SmemScales {
+    float back[2][3][32];             // what undoes the scaling of a score tile's tokens
+    float st_back[2][2][4];           // and of a wave's state; two, as `scale` reads the one before the last chunk
+    float z_most[2][8];               // a chunk's largest z, by wave
+    float gw[2][kChunk];              // Gam times the scale of the chunk's z
+    float held[2];                    // that scale
+};
 
 template <typename E, bool kDecay, int kTerms>
 __global__ __launch_bounds__(SmemTiles::D * 4, 2) void tiles16_kernel(BwdParams p) {
@@ -451,6 +603,7 @@ __global__ __launch_bounds__(SmemTiles::D * 4, 2) void tiles16_kernel(BwdParams 
     constexpr int LP = kChunk * PR / NT;  // pieces per thread per tensor per chunk (= 2)
     constexpr int LR = NT / PR;           // rows apart (= 32)
     __shared__ __attribute__((aligned(16))) SmemTiles sm;
+    __shared__ __attribute__((aligned(16))) typename std::conditional<kNarrow<E>, SmemScales, int>::type scales;
 
     const int tid = threadIdx.x;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, ln = l & 31, g = l >> 5;
@@ -492,6 +645,23 @@ __global__ __launch_bounds__(SmemTiles::D * 4, 2) void tiles16_kernel(BwdParams 
             *reinterpret_cast<u32x4*>(&sm.y[buf][to_own + r * LR * D]) = a.y[r];
             *reinterpret_cast<u32x4*>(&sm.z[buf][to_own + r * LR * D]) = a.z[r];
         }
+        if constexpr (kNarrow<E>) scales.z_most[buf][w] = most_of_rows(a.z);
+    };
+    // fp16: what the chunk in buffer buf is scaled by, from its z and the states before the last chunk; a wave without a score tile
+    auto scale = [&](int buf, int from) {
+        if constexpr (kNarrow<E>) {
+            if (w != 3) return;
+            const f32x4 *z = reinterpret_cast<const f32x4*>(scales.z_most[buf]), *st = reinterpret_cast<const f32x4*>(scales.st_back[from]);
+            float zm = 0.0f, back = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                zm = fmaxf(zm, z[i / 4][i % 4]);
+                back = fmaxf(back, st[i / 4][i % 4]);
+            }
+            const float next = power_of_z<kTerms>(zm, inverse_of(back));
+            scales.held[buf] = next;
+            if (kDecay) scales.gw[buf][l] = sm.gw[l] * next;
+        }
     };
     fetch(0);
 
@@ -505,8 +675,9 @@ __global__ __launch_bounds__(SmemTiles::D * 4, 2) void tiles16_kernel(BwdParams 
         }
     }
 
-    // state: S[i][r] = S[dk = 32 (HT it + i) + pi(m(r, g))][column 32c + ln]
+    // state: S[i][r] = S[dk = 32 (HT it + i) + pi(m(r, g))][column 32c + ln]; in fp16 times `held`
     f32x16 S[HT];
+    float held = 1.0f;  // the same in all lanes
     const int c_own = 32 * c + ln;
     auto dk_of = [&](int i, int r) { return 32 * (HT * it + i) + 16 * (r >> 3) + 8 * g + 4 * ((r >> 2) & 1) + (r & 3); };
 #pragma unroll
@@ -535,8 +706,15 @@ __global__ __launch_bounds__(SmemTiles::D * 4, 2) void tiles16_kernel(BwdParams 
 #pragma unroll
         for (int i = 0; i < HT; ++i) y_tr[i][rd] = at + ((4 * (HT * it + i) + 2 * half + (s16 & 1)) ^ t) * 8 + 4 * ((s16 >> 1) & 1);
     }
-    auto gam_of = [&](int f, int more) { return *reinterpret_cast<const f32x4*>(&sm.gw[16 * f + 4 * g + more]); };
-    auto publish = [&]() {
+    auto gam_of = [&](int buf, int f, int more) {
+        if constexpr (kNarrow<E>) return *reinterpret_cast<const f32x4*>(&scales.gw[buf][16 * f + 4 * g + more]);
+        else return *reinterpret_cast<const f32x4*>(&sm.gw[16 * f + 4 * g + more]);
+    };
+    auto publish = [&](int buf) {
+        if constexpr (kNarrow<E>) {
+            keep_in_range(S, held);
+            scales.st_back[buf][it][c] = inverse_of(held);
+        }
 #pragma unroll
         for (int i = 0; i < HT; ++i)
 #pragma unroll
@@ -546,7 +724,7 @@ __global__ __launch_bounds__(SmemTiles::D * 4, 2) void tiles16_kernel(BwdParams 
                 *reinterpret_cast<u32x4*>(&sm.st[32 * c * D + ln * D + ((s2 ^ g ^ turn(ln)) * 8)]) = pack_half<E>(S[i], hh);
             }
     };
-    publish();
+    publish(0);
     put(ahead, 0);
     fetch(1);
     __syncthreads();  // tables and the first chunk visible
@@ -578,10 +756,17 @@ __global__ __launch_bounds__(SmemTiles::D * 4, 2) void tiles16_kernel(BwdParams 
         for (int s = 0; s < D / 16; ++s) acc = E::mfma32(frag16(y_row + at_row[s]), xf[s], acc);
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[r] *= wgt[r];
+        if constexpr (kNarrow<E>) {
+            const float up = power_of_scores(most_of_token(acc));
+            scales.back[buf][tile][ln] = inverse_of(up);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[r] *= up;
+        }
         sm.pfrag[buf][tile][0][l] = pack_half<E>(acc, 0);
         sm.pfrag[buf][tile][1][l] = pack_half<E>(acc, 1);
     };
     scores(0);
+    scale(0, 0);
 
     auto chunk = [&](int t, int buf) {
         const int tok0 = t * kChunk;
@@ -603,7 +788,8 @@ __global__ __launch_bounds__(SmemTiles::D * 4, 2) void tiles16_kernel(BwdParams 
             mine[i] = z_frag(f);
             if constexpr (kTerms < 3) {
                 u32x4 zs[kTerms] = {mine[i]};
-                if (kDecay) scaled<E, kTerms>(mine[i], gam_of(f, 0), gam_of(f, 8), zs);
+                if (kDecay) scaled<E, kTerms>(mine[i], gam_of(buf, f, 0), gam_of(buf, f, 8), zs);
+                else if constexpr (kNarrow<E>) zs[0] = times_power<E>(mine[i], scales.held[buf]);
                 sm.zfrag[c][f][l] = zs[0];
                 if (kTerms > 1) rest[(c * 4 + f) * 64 + l] = zs[kTerms - 1];
             }
@@ -616,18 +802,37 @@ __global__ __launch_bounds__(SmemTiles::D * 4, 2) void tiles16_kernel(BwdParams 
         f32x16 o;
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[r] = 0.0f;
+        auto lam_own = [&]() { return !kDecay ? 1.0f : shift ? sm.pw[max(32 * it + ln + later - shift, 0)] : lam_full; };
+        if constexpr (kNarrow<E>) {  // the halves of the state's rows are scaled apart
+            f32x16 o1 = o;
 #pragma unroll
-        for (int s = 0; s < D / 16; ++s) o = E::mfma32(frag16(&sm.st[32 * c * D] + at_row[s]), xf[s], o);
-        if (kDecay) {
-            const float lam = shift ? sm.pw[max(32 * it + ln + later - shift, 0)] : lam_full;
+            for (int s = 0; s < D / 32; ++s) {
+                o = E::mfma32(frag16(&sm.st[32 * c * D] + at_row[s]), xf[s], o);
+                o1 = E::mfma32(frag16(&sm.st[32 * c * D] + at_row[D / 32 + s]), xf[D / 32 + s], o1);
+            }
+            const float lam = lam_own(), lam0 = scales.st_back[buf][0][c] * lam, lam1 = scales.st_back[buf][1][c] * lam;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) o[r] *= lam;
+            for (int r = 0; r < 16; ++r) o[r] = fmaf(o1[r], lam1, o[r] * lam0);
+        } else {
+#pragma unroll
+            for (int s = 0; s < D / 16; ++s) o = E::mfma32(frag16(&sm.st[32 * c * D] + at_row[s]), xf[s], o);
+            if (kDecay) {
+                const float lam = lam_own();
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[r] *= lam;
+            }
         }
         __syncthreads();  // scaled rows and the next tiles are there, everyone has read the state
+        scale(buf ^ 1, buf);
 
         // S = gamma^L S + Y^T (Gam Z)
-        if (kDecay) {
-            const float gl = sm.pw[Lc];
+        if (kDecay || kNarrow<E>) {
+            float gl = kDecay ? sm.pw[Lc] : 1.0f;
+            if constexpr (kNarrow<E>) {
+                const float next = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(scales.held[buf])));
+                gl *= next * inverse_of(held);
+                held = next;
+            }
 #pragma unroll
             for (int i = 0; i < HT; ++i)
 #pragma unroll
@@ -640,7 +845,7 @@ __global__ __launch_bounds__(SmemTiles::D * 4, 2) void tiles16_kernel(BwdParams 
                 b[0] = sm.zfrag[c][f][l];
                 if (kTerms > 1) b[kTerms - 1] = rest[(c * 4 + f) * 64 + l];
             } else {  // LDS has no room for the third: each wave forms all four anew
-                scaled<E, kTerms>(z_frag(f), gam_of(f, 0), gam_of(f, 8), b);
+                scaled<E, kTerms>(z_frag(f), gam_of(buf, f, 0), gam_of(buf, f, 8), b);
             }
 #pragma unroll
             for (int i = 0; i < HT; ++i) {
@@ -650,14 +855,26 @@ __global__ __launch_bounds__(SmemTiles::D * 4, 2) void tiles16_kernel(BwdParams 
                 for (int u = 0; u < kTerms; ++u) S[i] = E::mfma32(a, b[u], S[i]);
             }
         }
-        publish();
+        publish(buf ^ 1);
 
         // O^T += Z^T P^T
+        auto add_tile = [&](const u32x4 (&z)[2], int n) {
+            if constexpr (kNarrow<E>) {
+                f32x16 acc;
 #pragma unroll
-        for (int hh = 0; hh < 2; ++hh) o = E::mfma32(mine[hh], sm.pfrag[buf][it][hh][l], o);
-        if (it == 1)
+                for (int r = 0; r < 16; ++r) acc[r] = 0.0f;
 #pragma unroll
-            for (int hh = 0; hh < 2; ++hh) o = E::mfma32(other[hh], sm.pfrag[buf][2][hh][l], o);
+                for (int hh = 0; hh < 2; ++hh) acc = E::mfma32(z[hh], sm.pfrag[buf][n][hh][l], acc);
+                const float down = scales.back[buf][n][ln];
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[r] = fmaf(acc[r], down, o[r]);
+            } else {
+#pragma unroll
+                for (int hh = 0; hh < 2; ++hh) o = E::mfma32(z[hh], sm.pfrag[buf][n][hh][l], o);
+            }
+        };
+        add_tile(mine, it);
+        if (it == 1) add_tile(other, 2);
 
         // O^T: lane = token 32it + ln, registers 4q..4q+3 = columns 32c + 8q + 4g + (0..3).  Lanes of the two halves swap
         // words, and a lane has eight neighbouring columns of its row.
@@ -687,10 +904,11 @@ __global__ __launch_bounds__(SmemTiles::D * 4, 2) void tiles16_kernel(BwdParams 
 
     if (role.leave) {
         float* dst = role.leave + (size_t)unit * D * D;
+        const float real = kNarrow<E> ? inverse_of(held) : 1.0f;
 #pragma unroll
         for (int i = 0; i < HT; ++i)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) dst[dk_of(i, r) * D + c_own] = S[i][r];
+            for (int r = 0; r < 16; ++r) dst[dk_of(i, r) * D + c_own] = kNarrow<E> ? S[i][r] * real : S[i][r];
     }
 }
 
