@@ -55,9 +55,9 @@ struct Smem16 {
 // A rounding to one term is 2^-11 of the value, or 2^-25 of a number of that scale: 2^-39 of a token's largest score, 2^-27 of the
 // largest of a state; what is added to a state is off by 2^-33 of the largest z (three terms 2^-39) or 2^-22 of itself (2^-24).
 // The matrix instructions add products of numbers below 2^-14 as if these had that exponent.
-// fp16 takes 7 to 18 % longer by it.  us before and after: B16 H32 N2048 d128 593 650, B4 H16 N4096 d128 180 214, B2 H16 130 136, B4
-// H16 N4096 d64 97 105, B3 H12 N1777 d64 34.7 38.5, B16 H32 N128 d64 25.8 30.4, B2 H16 N2048 128/256 150 164.  (Scaling each state
-// as it becomes an operand, and each column of z by itself: 223 instead of 214.)
+// fp16 takes 6 to 18 % longer by it.  us before and after: B16 H32 N2048 d128 594 642, B4 H16 N4096 d128 178 210, B2 H16 130 137, B4
+// H16 N4096 d64 96.5 103.6, B3 H12 N1777 d64 34.5 37.5, B16 H32 N128 d64 25.7 29.7, B2 H16 N2048 128/256 150 160.  (Scaling each
+// state as it becomes an operand, and each column of z by itself: 223 instead of 210.)
 template <typename E>
 constexpr bool kNarrow = std::is_same<E, ElemF16>::value;
 
@@ -103,20 +103,37 @@ __device__ __forceinline__ float most_of_token(const f32x16& v) {
 __device__ __forceinline__ float most_finite(float m) {
     return __uint_as_float(most_of_wave(m < __builtin_inff() ? __float_as_uint(m) : 0u));
 }
-// The largest finite one of fp16 values, in a wave: 2^10 more than their bits, where infinities and NaNs wrap to less.
-template <int kCount>
+// The largest finite one of a wave's fp16 values; kColumns: a lane's values are of one column, which is lost where one of them is
+// infinite or NaN, and are left out then.
+template <bool kColumns, int kCount>
 __device__ __forceinline__ float most_of_rows(const u32x4 (&v)[kCount]) {
-    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-    u16x2 m = {0, 0};
+    typedef _Float16 Pair __attribute__((ext_vector_type(2)));
+    typedef uint16_t Bits __attribute__((ext_vector_type(2)));
+    Pair high = {0, 0}, low = {0, 0};
 #pragma unroll
     for (int f = 0; f < kCount; ++f)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const uint32_t word = v[f][e];
-            m = __builtin_elementwise_max(m, (__builtin_bit_cast(u16x2, word) + (uint16_t)0x400) & (uint16_t)0x7fff);
+            high = __builtin_elementwise_maximum(high, __builtin_bit_cast(Pair, word));
+            low = __builtin_elementwise_minimum(low, __builtin_bit_cast(Pair, word));
         }
-    const uint32_t most = max(most_of_wave(max(m[0], m[1])), 0x400u) - 0x400u;
-    return (float)__builtin_bit_cast(_Float16, (uint16_t)most);
+    Bits most = __builtin_bit_cast(Bits, __builtin_elementwise_maximum(high, -low));
+    uint32_t m = max(most[0], most[1]);
+    if (kColumns) {
+        m = m < 0x7c00u ? m : 0u;
+    } else if (__builtin_expect(m >= 0x7c00u, 0)) {  // 2^10 more than their bits wraps to less than any finite number's
+        most = Bits{0, 0};
+#pragma unroll
+        for (int f = 0; f < kCount; ++f)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t word = v[f][e];
+                most = __builtin_elementwise_max(most, (__builtin_bit_cast(Bits, word) + (uint16_t)0x400) & (uint16_t)0x7fff);
+            }
+        m = max((uint32_t)max(most[0], most[1]), 0x400u) - 0x400u;
+    }
+    return (float)__builtin_bit_cast(_Float16, (uint16_t)most_of_wave(m));
 }
 // The scale of z in a chunk, no more than leaves a state of up to 2^15 / held finite.
 template <int kTerms>
@@ -514,7 +531,7 @@ __global__ __launch_bounds__(DV * 2, D > 128 || DV > 128 ? 1 : 2) void walk16_ke
         if (kDecay || kNarrow<E>) {
             float gl = kDecay ? sm.pw[Lc] : 1.0f;
             if constexpr (kNarrow<E>) {
-                const float next = power_of_z<kTerms>(most_of_rows(zf), kOut ? held : 1.0f);
+                const float next = power_of_z<kTerms>(most_of_rows<true>(zf), kOut ? held : 1.0f);
                 gl *= next * inverse_of(held);
                 held = next;
                 if (kDecay) gw[l] = sm.gw[l] * held;  // read by this wave alone
@@ -645,7 +662,7 @@ __global__ __launch_bounds__(SmemTiles::D * 4, 2) void tiles16_kernel(BwdParams 
             *reinterpret_cast<u32x4*>(&sm.y[buf][to_own + r * LR * D]) = a.y[r];
             *reinterpret_cast<u32x4*>(&sm.z[buf][to_own + r * LR * D]) = a.z[r];
         }
-        if constexpr (kNarrow<E>) scales.z_most[buf][w] = most_of_rows(a.z);
+        if constexpr (kNarrow<E>) scales.z_most[buf][w] = most_of_rows<false>(a.z);
     };
     // fp16: what the chunk in buffer buf is scaled by, from its z and the states before the last chunk; a wave without a score tile
     auto scale = [&](int buf, int from) {
