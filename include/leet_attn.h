@@ -587,7 +587,8 @@ int leet_attn_add_rms_norm_q8(const leet_attn_rows *x, const leet_attn_rows *res
  *   dx, dh     g in `dtype`, g in residual_dtype; either may be NULL.  Each may be dout, h or dresidual (same data, strides and type)
  *   dweight    [C] of weight_dtype, or NULL: not wanted.  Written when all inputs have been read, so it may be the weight
  *   workspace  leet_attn_add_rms_norm_workspace_bytes bytes, 256-byte aligned; may be NULL without dweight.  Scratch
- * The sums over rows are taken in fp32 in a fixed order: no atomics, equal from call to call.
+ * The sums over rows are taken in fp32 in a fixed order: no atomics, equal from call to call.  Products of w, dout and h have to
+ * stay within fp32's range.
  */
 int leet_attn_add_rms_norm_backward(const leet_attn_rows *dout, const leet_attn_rows *h, const leet_attn_rows *dresidual,
                                     const leet_attn_rows *dx, const leet_attn_rows *dh, const void *weight, void *dweight,

@@ -35,8 +35,9 @@ struct Plan {
 // `resident` of them on 32 compute units: a chunk takes them alone_us while each has a unit to itself, full_us when all are there.
 // A call is its walk and, with segments, the pre-pass over the states and the scan, each the smooth maximum
 // (x^p + y^p)^(1/p) of that and of its memory traffic.  Fitted (3 to 8 % rms) to runs of BH 1..512, N 64..32768 and 1 to 64
-// segments; the picks are 0.4 % (16-bit, 128), 1.2 % (16-bit, 64) and 0.7 % (fp32) slower than the best of each run on average.  Width
-// 256 by fewer runs (BH 32 N 2048, 1 to 8 segments: 291 221 168 140 178 153 us).
+// segments; the picks are 0.4 % (16-bit, 128), 1.2 % (16-bit, 64) and 0.7 % (fp32) slower than the best of each run on average.  16-bit
+// is bf16; fp16, 6 to 18 % slower, has the same picks, 0.8 % (128) and 2.9 % (64) off the best of 15 shapes (BH 128 N 4096, 64: 222 us,
+// 180 with two segments; bf16 192 and 170).  Width 256 by fewer runs (BH 32 N 2048, 1 to 8 segments: 291 221 168 140 178 153 us).
 struct CostModel {
     double call_us, segments_us, segment_us;  // fixed: of a call, of having segments, of each of them
     double alone_us, full_us, round_us;       // walk: a chunk; what a round of workgroups begins with

@@ -16,13 +16,14 @@
 // In the order of the tokens S is the transposed state before a chunk: Lam = gamma^(i+1), Gam = gamma^(L-1-j).  Reversed, S
 // is the gradient of the state that the chunk's last token leaves: Lam = gamma^i, Gam = gamma^(L-j).
 //
-// The three walks read seven tensors' worth (dout three times, v, q and k twice each, less what dK and dV, side by side on an XCD,
-// take from its L2) and write three.  Two kernels: walk16_kernel, many small workgroups, for any number of segments; and
+// The three walks ask for nine tensors' worth (dout three times, v, q and k twice each) and read 6.8 to 7.3, as dK and dV, side by
+// side on an XCD, meet in its L2; they write three.  Two kernels: walk16_kernel, many small workgroups, for any number of segments; and
 // tiles16_kernel, one large workgroup a sequence, where there are few sequences.  With segments a pre-pass over the states
 // of both directions (walk16_kernel without outputs) and the scan of their boundaries come first.
-// Near memory's rate where the device is full: B16 H32 N2048 d128 bf16 takes 582 us, its ten tensors at 4.6 TB/s (with one term 530,
+// Near memory's rate where the device is full: B16 H32 N2048 d128 bf16 takes 582 us, ten tensors at 4.6 TB/s (with one term 530,
 // 5.1).  Few sequences are bound by a chunk's latency, or by segments' pre-pass, which reads four tensors again.  B4 H16 N4096: 174
-// to 179 us, of which its ten tensors are 131 at 5.1 TB/s; with dstate_in wanted and three terms 207.
+// to 181 us in a run of calls (190 to 220 on a device that was idle), of which its 9.8 tensors are 128 at 5.1 TB/s; with dstate_in
+// wanted and three terms 207 to 217.
 #include <type_traits>
 
 #include "leet_backward.hpp"
