@@ -52,13 +52,14 @@ struct Smem16 {
 // of their bits below, scores and states of large ones became infinite where every gradient is finite.  So fp16 has powers of two:
 //   * scores are brought to [2^14, 2^15) for each token of a tile as they become operands, and the product back;
 //   * a state is kept times `held`, which Gam carries: the largest z of a chunk is brought to [2^8, 2^9), in three terms to [2^14,
-//     2^15); where the largest of a wave's state then lies outside [4, 2^15) the state itself is brought to [2^14, 2^15).
+//     2^15), and without decay z is taken 256 times where that is finite; where the largest of a wave's state then lies outside [4, 2^15) the state itself is brought to [2^14, 2^15).
 // A rounding to one term is 2^-11 of the value, or 2^-25 of a number of that scale: 2^-39 of a token's largest score, 2^-27 of the
-// largest of a state; what is added to a state is off by 2^-33 of the largest z (three terms 2^-39) or 2^-22 of itself (2^-24).
+// largest of a state; what is added to a state is off by 2^-33 of the largest z (three terms 2^-39) or 2^-22 of itself (2^-24); without decay by nothing.
 // The matrix instructions add products of numbers below 2^-14 as if these had that exponent.
-// fp16 takes 6 to 18 % longer by it.  us before and after: B16 H32 N2048 d128 594 642, B4 H16 N4096 d128 178 210, B2 H16 130 137, B4
-// H16 N4096 d64 96.5 103.6, B3 H12 N1777 d64 34.5 37.5, B16 H32 N128 d64 25.7 29.7, B2 H16 N2048 128/256 150 160.  (Scaling each
-// state as it becomes an operand, and each column of z by itself: 223 instead of 210.)
+// fp16 takes 6 to 18 % longer by it (a compute unit a sequence without decay 22 %).  us before and after: B16 H32 N2048 d128 594 642,
+// B4 H16 N4096 d128 178 210 (without decay 149 182), B2 H16 130 137, B4 H16 N4096 d64 96.5 103.6, B3 H12 N1777 d64 34.5 37.5, B16 H32
+// N128 d64 25.7 29.7, B2 H16 N2048 128/256 150 160.  (Scaling each state as it becomes an operand, and each column of z by itself:
+// 223 instead of 210.)
 template <typename E>
 constexpr bool kNarrow = std::is_same<E, ElemF16>::value;
 
@@ -136,10 +137,12 @@ __device__ __forceinline__ float most_of_rows(const u32x4 (&v)[kCount]) {
     }
     return (float)__builtin_bit_cast(_Float16, (uint16_t)most_of_wave(m));
 }
-// The scale of z in a chunk, no more than leaves a state of up to 2^15 / held finite.
+// The scale of z in a chunk, no more than leaves a state of up to 2^15 / held finite.  Without decay (kTerms 1) it is 2^8 or 1, which
+// lose no bit, and mostly the last chunk's.
 template <int kTerms>
 __device__ __forceinline__ float power_of_z(float most, float held) {
-    return fminf(power_to<kTerms < 3 ? 8 : 14, -24>(most), 0x1p85f * held);
+    const float by = kTerms == 1 ? (most < 128.0f ? 256.0f : 1.0f) : power_to<kTerms == 2 ? 8 : 14, -24>(most);
+    return fminf(by, 0x1p85f * held);
 }
 // Brings a wave's state, of which it holds `held` times, into fp16's range.
 template <int kTiles>
@@ -208,12 +211,10 @@ __device__ __forceinline__ void scaled(u32x4 x, f32x4 w0, f32x4 w1, u32x4 (&out)
     }
 }
 
-// Eight 16-bit values times a power of two
-template <typename E>
+// eight fp16 values times a power of two
 __device__ __forceinline__ u32x4 times_power(u32x4 x, float by) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = E::pack2(E::lo(x[e]) * by, E::hi(x[e]) * by);
-    return x;
+    const f16x8 v = __builtin_bit_cast(f16x8, x) * (_Float16)by;
+    return __builtin_bit_cast(u32x4, v);
 }
 
 // The rows of a sequence that hold tokens tok0 .. tok0 + L - 1 of a walk (rows of `width` elements; `seq`: its first row), L = 64
@@ -537,10 +538,12 @@ __global__ __launch_bounds__(DV * 2, D > 128 || DV > 128 ? 1 : 2) void walk16_ke
                 held = next;
                 if (kDecay) gw[l] = sm.gw[l] * held;  // read by this wave alone
             }
+            if (kDecay || gl != 1.0f) {  // the same in all lanes
 #pragma unroll
-            for (int dt = 0; dt < DT; ++dt)
+                for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) S[dt][r] *= gl;
+                    for (int r = 0; r < 16; ++r) S[dt][r] *= gl;
+            }
         }
 #pragma unroll
         for (int f = 0; f < 4; ++f) {
@@ -548,7 +551,7 @@ __global__ __launch_bounds__(DV * 2, D > 128 || DV > 128 ? 1 : 2) void walk16_ke
             if (kDecay)
                 scaled<E, kTerms>(zf[f], *reinterpret_cast<const f32x4*>(&gw[16 * f + 4 * g]),
                                   *reinterpret_cast<const f32x4*>(&gw[16 * f + 8 + 4 * g]), zs);
-            else if (kNarrow<E>) zs[0] = times_power<E>(zf[f], held);
+            else if (kNarrow<E>) zs[0] = times_power(zf[f], held);
             else zs[0] = zf[f];
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt) {
@@ -807,7 +810,7 @@ __global__ __launch_bounds__(SmemTiles::D * 4, 2) void tiles16_kernel(BwdParams 
             if constexpr (kTerms < 3) {
                 u32x4 zs[kTerms] = {mine[i]};
                 if (kDecay) scaled<E, kTerms>(mine[i], gam_of(buf, f, 0), gam_of(buf, f, 8), zs);
-                else if constexpr (kNarrow<E>) zs[0] = times_power<E>(mine[i], scales.held[buf]);
+                else if constexpr (kNarrow<E>) zs[0] = times_power(mine[i], scales.held[buf]);
                 sm.zfrag[c][f][l] = zs[0];
                 if (kTerms > 1) rest[(c * 4 + f) * 64 + l] = zs[kTerms - 1];
             }
@@ -851,10 +854,12 @@ __global__ __launch_bounds__(SmemTiles::D * 4, 2) void tiles16_kernel(BwdParams 
                 gl *= next * inverse_of(held);
                 held = next;
             }
+            if (kDecay || gl != 1.0f) {  // the same in all lanes
 #pragma unroll
-            for (int i = 0; i < HT; ++i)
+                for (int i = 0; i < HT; ++i)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) S[i][r] *= gl;
+                    for (int r = 0; r < 16; ++r) S[i][r] *= gl;
+            }
         }
 #pragma unroll
         for (int f = 0; f < 4; ++f) {

@@ -174,3 +174,18 @@ def test_states_that_fade(leet, r, dv, segments):
         got = leet.leet_attn_backward(*on(*ts, gamma), dstate_in=left, segments=segments)
         for name, a, b in zip(("dq", "dk", "dv", "dstate_in"), got + (left,), want):
             held(name, a, b)
+
+
+@pytest.mark.parametrize("r,dv", SHAPES)
+@pytest.mark.parametrize("decay", [True, False])
+@pytest.mark.parametrize("segments", [1, 2])
+def test_the_states_gradient_of_small_channels(leet, r, dv, decay, segments):
+    """Channels of dout that lie 2^21 apart: those of the state's gradient are off by 2^-39 of the largest, no more."""
+    do, q, k, v, _, _ = inputs(300, r, dv, (1.0, 1.0, 1.0, 1.0), states=False)
+    do = (do * 2.0 ** (10 - torch.arange(dv) % 22.0)).half()
+    gamma = decays(3) if decay else None
+    left = torch.empty((1, 3, r, dv), device="cuda")
+    leet.leet_attn_backward(*on(do, q, k, v, gamma), dstate_in=left, segments=segments,
+                            mask=leet.LEET_MASK_DECAY if decay else leet.LEET_MASK_CAUSAL)
+    want = bounded(*wide(do, q, k, v), gamma.double() if decay else torch.ones(3, dtype=torch.float64), None, None)
+    held("dstate_in", left, want[3])
