@@ -189,3 +189,23 @@ def test_the_states_gradient_of_small_channels(leet, r, dv, decay, segments):
                             mask=leet.LEET_MASK_DECAY if decay else leet.LEET_MASK_CAUSAL)
     want = bounded(*wide(do, q, k, v), gamma.double() if decay else torch.ones(3, dtype=torch.float64), None, None)
     held("dstate_in", left, want[3])
+
+
+@pytest.mark.parametrize("r,dv", SHAPES)
+@pytest.mark.parametrize("size", [2.0 ** -60, 1e30])
+@pytest.mark.parametrize("N,segments", [(70, 0), (200, 1), (200, 2)])
+def test_states_of_any_size_without_decay(leet, r, dv, size, N, segments):
+    do, q, k, v, s, ds = inputs(N, r, dv, (2.0 ** -12, 1.0, 1.0, 1.0))
+    zero, ones = torch.zeros_like, torch.ones(3, dtype=torch.float64)
+    left = torch.empty_like(ds, device="cuda")
+    causal = leet.LEET_MASK_CAUSAL
+    got = leet.leet_attn_backward(*on(do, q, zero(k), zero(v)), None, dstate_out=on(ds * size)[0], dstate_in=left, segments=segments,
+                                  mask=causal)
+    want = bounded(*wide(do, q, zero(k), zero(v)), ones, None, (ds * size).double())
+    assert not got[0].any() and not got[1].any() and not got[2].any()
+    held("dstate_in", left, want[3])
+    got = leet.leet_attn_backward(*on(do, q, k, v), None, state_in=on(s * 2.0 ** -20)[0], segments=segments, mask=causal)
+    for name, a, b in zip(("dq", "dk", "dv"), got, bounded(*wide(do, q, k, v), ones, (s * 2.0 ** -20).double(), None)):
+        held(name, a, b)
+    got = leet.leet_attn_backward(*on(zero(do), q, k, v), None, state_in=on(s * size)[0], segments=segments, mask=causal)
+    assert not got[0].any() and not got[1].any() and not got[2].any()
